@@ -1,0 +1,654 @@
+"""Serving after the prefill: the paged cache, the attention that reads it, and block selection.
+
+Each case is one pass of a serving program through one of three groups of operators:
+
+  branch   sequences of the cache are forked and the branches grow: released, shared, copied on write
+  accept   drafted tokens are appended, the accepted path of each tree is compacted
+  ingest   packed prompts go into the cache, with the summaries of their pages
+  tree     attention of drafted tokens (trees, single tokens, causal chunks) over the cache
+  select   single tokens choose pages by a cheap score and attend to those
+  prompt   prompts choose key blocks for each query block, and attend to those
+
+A cache is pages of 64 tokens [P, Hkv, 64, d] in bf16 (with a leading axis of layers where a call
+takes all layers at once), a page table [S, M] (-1: none), lengths [S] and reference counts [P].
+``run`` computes the plain form with torch operations, or calls the library's operators.
+"""
+from __future__ import annotations
+
+import random
+
+import torch
+
+own = False
+
+PAGE = 64
+DEV = "cuda" if torch.cuda.is_available() else "cpu"
+
+
+def _binding():
+    from paper_2505_11254_amd import binding  # (the plain forms run without the library)
+    return binding
+
+
+# ------------------------------------------------------------------------------------- the cases
+
+def listed():
+    llama = dict(Hq=32, Hkv=8, d=128)
+    return [
+        # One short conversation splits in two, in a small two-layer model: latency alone.
+        dict(name="branch_2", kind="branch", layers=2, prompts=1, fan=2, len=333, add=1, Hkv=2, d=64),
+        # Parallel sampling: 32 prompts with 8 branches each, 16 layers of an 8B-shaped model.
+        dict(name="branch_256", kind="branch", layers=16, prompts=32, fan=8, len=1900, add=1, Hkv=8, d=128),
+        # One step of speculative decoding of a batch: 16 drafts each, four layers at a time.
+        dict(name="accept_64", kind="accept", layers=4, B=64, len=2000, n=16, Hkv=8, d=128),
+        # The keys and values of a packed batch of prompts after their prefill.
+        dict(name="ingest_80k", kind="ingest", B=5, len=24011, Hkv=8, d=128),
+        # A single token of a single short sequence: the smallest call.
+        dict(name="decode_1", kind="tree", B=1, n=1, len=777, tree=False, Hq=8, Hkv=2, d=64),
+        # Everyday decoding of a ragged batch in an 8B-shaped layer.
+        dict(name="decode_64", kind="tree", B=64, n=1, len=8192, tree=False, **llama),
+        # Dense decode over the cache that a long prefill has left.
+        dict(name="decode_131k", kind="tree", B=1, n=1, len=131072, tree=False, **llama),
+        # Verification of small draft trees for a batch.
+        dict(name="tree_16x24", kind="tree", B=16, n=24, len=6000, tree=True, **llama),
+        # Large trees over long contexts, 64 heads on 8.
+        dict(name="tree_4x64", kind="tree", B=4, n=64, len=40000, tree=True, Hq=64, Hkv=8, d=128),
+        # Sparse decoding of a batch at tens of thousands of tokens.
+        dict(name="select_16", kind="select", B=16, n=1, len=50000, top_k=64, Hq=32, Hkv=8, d=128),
+        # Sparse decoding of one sequence of a million tokens.
+        dict(name="select_1m", kind="select", B=1, n=1, len=1048576, top_k=128, Hq=32, Hkv=8, d=128),
+        # Block lists from the prompt's own queries and keys, and the attention over them.
+        dict(name="prompt_16k", kind="prompt", B=1, len=16384, top_k=32, block_q=64, **llama),
+    ]
+
+
+def draw(rng):
+    def log(lo, hi):
+        return min(hi, int(lo * (hi / lo) ** rng.random() + 0.5))
+
+    heads = rng.choice([(32, 8, 128), (8, 2, 64), (16, 16, 128), (28, 4, 128), (64, 8, 128), (16, 2, 64),
+                        (20, 4, 64), (12, 3, 128)])
+    Hq, Hkv, d = heads
+    kind = rng.choice(["branch", "accept", "ingest", "tree", "tree", "select", "select", "prompt"])
+    if kind == "branch":
+        return dict(kind=kind, layers=log(1, 16), prompts=log(1, 32), fan=log(1, 8), len=log(20, 1900),
+                    add=log(1, 80), Hkv=rng.randint(1, 8), d=d)
+    if kind == "accept":
+        return dict(kind=kind, layers=log(1, 4), B=log(1, 64), len=log(1, 2000), n=log(1, 64), Hkv=rng.randint(1, 8), d=d)
+    if kind == "ingest":
+        return dict(kind=kind, B=log(1, 5), len=log(50, 24000), Hkv=rng.randint(1, 8), d=d)
+    if kind == "tree":
+        tree = rng.random() < 0.5
+        n = log(2, 64) if tree else rng.choice([1, 1, 1, log(2, 40)])
+        B = log(1, 48)
+        return dict(kind=kind, B=B, n=n, len=log(n, max(n + 1, min(100000, 700000 // (B * n) + 200))), tree=tree,
+                    Hq=Hq, Hkv=Hkv, d=d)
+    if kind == "select":
+        B = log(1, 32)
+        return dict(kind=kind, B=B, n=rng.choice([1, 1, 3]), len=log(100, 800000 // B), top_k=log(8, 128), Hq=Hq, Hkv=Hkv, d=d)
+    bq = rng.choice([64, 128, 256]) if (Hq // Hkv) % 4 == 0 else 256
+    return dict(kind=kind, B=rng.choice([1, 1, 2, 3]), len=log(300, 6000), top_k=log(4, 40), block_q=bq, Hq=Hq,
+                Hkv=Hkv, d=d)
+
+
+def _lens(case):
+    """The sequences' lengths: the first has `len`, the others between a quarter of it and all of it."""
+    B = case.get("B") or case["prompts"]
+    return [max(1, int(case["len"] * (1.0 if b == 0 else 0.25 + 0.75 * (b * 0.618034 % 1.0)))) for b in range(B)]
+
+
+def _news(case):
+    """Drafted or new tokens of each sequence: `n` for the first, at least one for each."""
+    return [max(1, case["n"] - (3 * b) % max(1, case["n"] // 2)) for b in range(case["B"])]
+
+
+def _pages(n):
+    return -(-n // PAGE)
+
+
+def work(case):
+    """What a pass cannot do without: inputs read once, outputs written once."""
+    kind, d, Hkv = case["kind"], case["d"], case["Hkv"]
+    row = 2 * Hkv * d * 2  # the key and the value of a token, bf16
+    lens = _lens(case)
+    if kind == "branch":
+        rows = sum(case["fan"] * (n % PAGE) for n in lens)
+        ints = sum(case["fan"] * (_pages(n) * 4 * 4 + 16) for n in lens)
+        return {"bytes": 2 * rows * row * case["layers"] + ints, "flops": 0}
+    if kind == "accept":
+        new = sum(_news(case))
+        return {"bytes": 2 * new * row * case["layers"] + len(lens) * 40, "flops": 0}
+    if kind == "ingest":
+        whole = sum(n // PAGE for n in lens)
+        return {"bytes": 2 * sum(lens) * row + whole * Hkv * (d + 4), "flops": whole * PAGE * Hkv * d}
+    Hq = case["Hq"]
+    if kind == "tree":
+        news = _news(case)
+        tok = sum(news)
+        # a tree's rows see the context and their ancestors, a chunk's the context and the rows before
+        pairs = sum(m * max(0, n) for n, m in zip(lens, news))
+        return {"bytes": sum(max(n, m) for n, m in zip(lens, news)) * row + 2 * tok * Hq * d * 2, "flops": 4 * pairs * Hq * d}
+    if kind == "select":
+        b = f = 0
+        for n, m in zip(lens, _news(case)):
+            cand = n // PAGE
+            keys = min(case["top_k"], cand) * PAGE + n % PAGE
+            b += cand * Hkv * (d + 4) + m * keys * row + 2 * m * Hq * d * 2
+            f += 2 * m * cand * Hq * d + 4 * m * keys * Hq * d
+        return {"bytes": b, "flops": f}
+    b = f = 0
+    R = case["block_q"] // PAGE
+    for n in lens:
+        nqb = -(-n // case["block_q"])
+        b += 2 * n * Hq * d * 2 + n * row
+        for qb in range(nqb):
+            rows = min(case["block_q"], n - qb * case["block_q"])
+            pairs = rows * min(case["top_k"], qb * R) * PAGE + rows * (rows + 1) // 2
+            f += (2 * rows * qb * R + 4 * pairs) * Hq * d
+    return {"bytes": b, "flops": f}
+
+
+# ------------------------------------------------------------------------------- what is in hand
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(int(seed))
+
+
+def _randn(g, *shape, std=1.0, offset=None):
+    """Normal bf16 values; `offset` [Hkv, 1, d] shifts keys as trained models do."""
+    out = torch.empty(shape, dtype=torch.bfloat16, device=DEV)
+    flat = out.view(shape[0], -1)
+    step = max(1, (1 << 27) // max(1, flat.shape[1]))
+    for i in range(0, shape[0], step):
+        x = torch.randn((min(step, shape[0] - i),) + tuple(shape[1:]), generator=g, device=DEV) * std
+        out[i:i + step] = x if offset is None else x + offset
+    return out
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def _cu(v):
+    cu = [0]
+    for n in v:
+        cu.append(cu[-1] + n)
+    return _ints(cu)
+
+
+def _cache(g, layers, Hkv, d, lens, slots, M, spare):
+    """A cache whose first len(lens) slots hold sequences of these lengths, in pages scattered over the pool."""
+    used = sum(_pages(n) for n in lens)
+    P = used + spare
+    shape = (P, Hkv, PAGE, d) if layers is None else (layers, P, Hkv, PAGE, d)
+    off = torch.randn((Hkv, 1, d), generator=g, device=DEV) * 0.5
+    perm = torch.randperm(P, generator=g, device=DEV).to(torch.int32)
+    table = torch.full((slots, M), -1, dtype=torch.int32, device=DEV)
+    at = 0
+    for i, n in enumerate(lens):
+        table[i, :_pages(n)] = perm[at:at + _pages(n)]
+        at += _pages(n)
+    refs = torch.zeros(P, dtype=torch.int32, device=DEV)
+    refs[perm[:used].long()] = 1
+    return dict(k_pages=_randn(g, *shape, offset=off), v_pages=_randn(g, *shape), table=table,
+                lens=_ints(list(lens) + [0] * (slots - len(lens))), refs=refs)
+
+
+def _parents(r, n):
+    """A draft tree in the order its nodes are drafted: the parent of each node, -1 under the context."""
+    return [r.randint(max(-1, i - 1 - r.randint(0, 5)), i - 1) for i in range(n)]
+
+
+def _tree_masks(parents_of, words):
+    """Bit j of row i: draft j is i or an ancestor of it."""
+    rows = []
+    for parents in parents_of:
+        bits = []
+        for i, p in enumerate(parents):
+            bits.append((bits[p] if p >= 0 else 0) | 1 << i)
+        for x in bits:
+            w = [x >> 64 * k & (1 << 64) - 1 for k in range(words)]
+            rows.append([v - (1 << 64) if v >> 63 else v for v in w])
+    return torch.tensor(rows, dtype=torch.int64, device=DEV)
+
+
+def prepare(case, seed):
+    g, r = _gen(seed), random.Random(seed)
+    kind, Hkv, d = case["kind"], case["Hkv"], case["d"]
+    lens = _lens(case)
+    s = dict(case=case)
+    if kind == "branch":
+        fan, add = case["fan"], case["add"]
+        n = len(lens)
+        M = _pages(max(lens) + add) + 1
+        s.update(_cache(g, case["layers"], Hkv, d, lens, n + n * fan, M, n * fan * (_pages(add) + 1) + 7))
+        order = list(range(n, n + n * fan))
+        r.shuffle(order)  # the slots that are free come in no order
+        s.update(src=_ints([i // fan for i in range(n * fan)]), dst=_ints(order),
+                 new_lens=_ints([lens[i // fan] + add for i in range(n * fan)]))
+    elif kind == "accept":
+        news = _news(case)
+        M = _pages(max(a + b for a, b in zip(lens, news))) + 1
+        s.update(_cache(g, case["layers"], Hkv, d, lens, len(lens), M, 2 * len(lens) + sum(map(_pages, news))))
+        keep = []
+        for n in news:
+            parents = _parents(r, n)
+            path, i = [], r.randint(-1, n - 1)
+            while i >= 0:
+                path.append(i)
+                i = parents[i]
+            keep.append(path[::-1])
+        T = sum(news)
+        s.update(slots=_ints(r.sample(range(len(lens)), len(lens))), cu=_cu(news), max_new=max(news),
+                 k=_randn(g, case["layers"], T, Hkv, d), v=_randn(g, case["layers"], T, Hkv, d),
+                 keep=_ints([i for p in keep for i in p] or [0]), cu_keep=_cu([len(p) for p in keep]))
+        s["start"] = s["lens"][s["slots"].long()].clone()
+        s["new_lens"] = s["start"] + s["cu"][1:] - s["cu"][:-1]
+    elif kind == "ingest":
+        M = _pages(max(lens))
+        s.update(_cache(g, None, Hkv, d, [], len(lens), M, sum(map(_pages, lens)) + 9))
+        P = s["refs"].numel()
+        s.update(slots=_ints(list(range(len(lens)))), new_lens=_ints(lens), cu=_cu(lens), max_new=max(lens),
+                 k=_randn(g, sum(lens), Hkv, d, offset=torch.randn((Hkv, d), generator=g, device=DEV) * 0.5),
+                 v=_randn(g, sum(lens), Hkv, d),
+                 codes=torch.zeros((P, Hkv, d), dtype=torch.int8, device=DEV),
+                 scales=torch.zeros((P, Hkv), dtype=torch.float32, device=DEV))
+    elif kind in ("tree", "select"):
+        news = _news(case)
+        lens = [max(n, m) for n, m in zip(lens, news)]
+        s.update(_cache(g, None, Hkv, d, lens, len(lens), _pages(max(lens)), 5))
+        s.update(q=_randn(g, sum(news), case["Hq"], d), cu=_cu(news), max_q=max(news), max_len=max(lens), mask=None)
+        if kind == "tree" and case["tree"]:
+            s["mask"] = _tree_masks([_parents(r, n) for n in news], -(-max(news) // 64))
+        if kind == "select":  # the program keeps the summaries up to date as pages fill
+            s["codes"], s["scales"] = _summary(s["k_pages"])
+    else:
+        off = torch.randn((Hkv, d), generator=g, device=DEV) * 0.5
+        T = sum(lens)
+        s.update(q=_randn(g, T, case["Hq"], d), k=_randn(g, T, Hkv, d, offset=off), v=_randn(g, T, Hkv, d), cu=_cu(lens),
+                 lens=_ints(lens), max_len=max(lens))
+    return s
+
+
+# -------------------------------------------------------------------------------- the plain forms
+
+def _summary(x):
+    """8-bit codes and scales of the mean keys of blocks x [..., 64, d]; the sums in 64 bits."""
+    sums = x.double().sum(-2) if x.numel() < 1 << 28 else torch.cat([y.double().sum(-2) for y in x.split(1024)])
+    top = sums.abs().amax(-1, keepdim=True)
+    codes = torch.where(top > 0, torch.round(sums * 127 / top.clamp(min=1e-300)), sums * 0).to(torch.int8)
+    return codes, (top[..., 0] / (127 * PAGE)).float()
+
+
+def _select(q, codes, scales, cand, top_k, n_sink, n_recent):
+    """The blocks that groups of query rows q [..., rows, d] choose among the first `cand` of codes
+    [..., blocks, d]: ascending, -1 behind the last. Scores are exact whole numbers times a scale."""
+    q = q.float()
+    top = q.abs().amax((-1, -2), keepdim=True)
+    q8 = torch.where(top > 0, torch.round(q * 127 / torch.where(top > 0, top, 1)), q * 0)
+    best = (q8 @ codes.float().transpose(-1, -2)).amax(-2)
+    score = best * scales + 0.0
+    at = torch.arange(codes.shape[-2], device=q.device)
+    cand = cand[..., None]
+    score = torch.where((at < n_sink) | (at >= cand - n_recent), float("inf"), score)
+    score = torch.where(at < cand, score, float("-inf"))
+    order = torch.sort(score, dim=-1, descending=True, stable=True).indices[..., :top_k]
+    if order.shape[-1] < top_k:
+        order = torch.nn.functional.pad(order, (0, top_k - order.shape[-1]), value=1 << 30)
+    order = torch.where(torch.arange(top_k, device=q.device) < cand, order, 1 << 30)
+    order = torch.sort(order, dim=-1).values
+    return torch.where(order < 1 << 30, order, -1).to(torch.int32)
+
+
+def _softmax_v(scores, vis, v):
+    """softmax over the visible keys of scores [..., rows, keys] times v [..., keys, d]; rows that see none: 0."""
+    scores = scores.masked_fill(~vis, float("-inf"))
+    top = scores.amax(-1, keepdim=True)
+    p = torch.exp(scores - torch.where(top > float("-inf"), top, 0.0))
+    p = p.masked_fill(~vis, 0.0)
+    return (p @ v) / p.sum(-1, keepdim=True).clamp(min=1e-30)
+
+
+def _rows(s):
+    """The sequence of each query row, its place among the sequence's rows, and its position."""
+    cu = s["cu"].long()
+    t = torch.arange(s["q"].shape[0], device=DEV)
+    b = torch.searchsorted(cu[1:], t, right=True)
+    i = t - cu[b]
+    return b, i, s["lens"].long()[b] - (cu[b + 1] - cu[b]) + i
+
+
+def _plain_tree(s):
+    q, table, lens, cu = s["q"], s["table"].long(), s["lens"].long(), s["cu"].long()
+    T, Hq, d = q.shape
+    B, Hkv, N = lens.numel(), s["k_pages"].shape[1], s["max_q"]
+    b, i, _ = _rows(s)
+    new = cu[1:] - cu[:-1]
+    qs = torch.zeros((B, N, Hq, d), device=DEV)
+    qs[b, i] = q.float()
+    qs = qs.view(B, N, Hkv, Hq // Hkv, d).permute(0, 2, 1, 3, 4).reshape(B, Hkv, -1, d)
+    pages = table.clamp(min=0)
+    k = s["k_pages"][pages].transpose(1, 2).reshape(B, Hkv, -1, d).float()
+    v = s["v_pages"][pages].transpose(1, 2).reshape(B, Hkv, -1, d).float()
+    pos = torch.arange(k.shape[2], device=DEV)
+    j = pos - (lens - new)[:, None]  # place among the drafted tokens
+    if s["mask"] is None:
+        vis = j[:, None] <= torch.arange(N, device=DEV)[:, None]
+    else:
+        bits = torch.zeros((B, N, s["mask"].shape[1]), dtype=torch.int64, device=DEV)
+        bits[b, i] = s["mask"]
+        jc = j.clamp(min=0, max=64 * bits.shape[2] - 1)[:, None].expand(B, N, -1)
+        vis = (torch.gather(bits, 2, jc // 64) >> jc % 64 & 1).bool() | (j < 0)[:, None]
+    vis &= (pos < lens[:, None])[:, None]
+    vis = vis[:, None, :, None].expand(B, 1, N, Hq // Hkv, -1).reshape(B, 1, -1, pos.numel())
+    out = _softmax_v(qs @ k.transpose(-1, -2) * d ** -0.5, vis, v)
+    out = out.view(B, Hkv, N, Hq // Hkv, d).permute(0, 2, 1, 3, 4).reshape(B, N, Hq, d)
+    return out[b, i].to(q.dtype)
+
+
+def _plain_select(s):
+    c, q, table = s["case"], s["q"], s["table"].long()
+    T, Hq, d = q.shape
+    Hkv = s["k_pages"].shape[1]
+    b, _, pos = _rows(s)
+    pages = table.clamp(min=0)
+    codes, scales = s["codes"][pages].transpose(1, 2)[b], s["scales"][pages].transpose(1, 2)[b]
+    qg = q.view(T, Hkv, Hq // Hkv, d)
+    cand = (pos // PAGE)[:, None].expand(T, Hkv)
+    lists = _select(qg, codes, scales, cand, c["top_k"], 1, 2)
+    at = torch.cat([lists.long(), cand[..., None]], -1)
+    page = torch.gather(pages[b][:, None].expand(T, Hkv, -1), 2, at.clamp(min=0))
+    h = torch.arange(Hkv, device=DEV)[:, None]
+    k = s["k_pages"][page, h].flatten(2, 3).float()
+    v = s["v_pages"][page, h].flatten(2, 3).float()
+    keys = (at[..., None] * PAGE + torch.arange(PAGE, device=DEV)).flatten(2, 3)
+    vis = (keys >= 0) & (keys <= pos[:, None, None])
+    out = _softmax_v(qg.float() @ k.transpose(-1, -2) * d ** -0.5, vis[:, :, None], v)
+    return {"pages": lists, "out": out.reshape(T, Hq, d).to(q.dtype)}
+
+
+def _plain_prompt(s):
+    c, q = s["case"], s["q"]
+    T, Hq, d = q.shape
+    Hkv, bq, top_k = c["Hkv"], c["block_q"], c["top_k"]
+    B, N, R = s["lens"].numel(), s["max_len"], bq // PAGE
+    nqb = -(-N // bq)
+    b, i, _ = _rows(s)
+
+    def padded(x):
+        p = torch.zeros((B, nqb * bq) + tuple(x.shape[1:]), dtype=x.dtype, device=DEV)
+        p[b, i] = x
+        return p
+
+    qp = padded(q).view(B, nqb, bq, Hkv, Hq // Hkv, d).permute(0, 3, 1, 2, 4, 5).flatten(3, 4)
+    kp = padded(s["k"]).view(B, nqb * R, PAGE, Hkv, d).permute(0, 3, 1, 2, 4)
+    vp = padded(s["v"]).view(B, nqb * R, PAGE, Hkv, d).permute(0, 3, 1, 2, 4)
+    codes, scales = _summary(kp)
+    first = torch.arange(nqb, device=DEV) * R  # the tiles before each query block
+    lists = _select(qp, codes[:, :, None], scales[:, :, None], first.expand(B, Hkv, nqb), top_k, 1, 1)
+    inside = first * PAGE < s["lens"].long()[:, None]  # query blocks that hold rows
+    lists = torch.where(inside[:, None, :, None], lists, -1)
+    count = first.clamp(max=top_k)
+    before = torch.cumsum(count, 0) - count
+    total = int(sum(min(top_k, x * R) for x in range(nqb)))
+    held = torch.cumsum(torch.where(inside, count, 0), 1)
+    ptr = torch.cat([torch.zeros_like(held[:, :1]), held], 1)[:, None]
+    ptr = ptr + torch.arange(B * Hkv, device=DEV).view(B, Hkv, 1) * total
+    idx = torch.full((B, Hkv, total + 1), -1, dtype=torch.int32, device=DEV)
+    j = torch.arange(top_k, device=DEV)
+    place = torch.where(j < count[:, None], before[:, None] + j, total).flatten()
+    idx.scatter_(2, place.expand(B, Hkv, -1), lists.flatten(2))
+    at = torch.cat([lists.long(), (first[:, None] + torch.arange(R, device=DEV)).expand(B, Hkv, nqb, R)], -1)
+    bi, hi = torch.arange(B, device=DEV).view(B, 1, 1, 1), torch.arange(Hkv, device=DEV).view(1, Hkv, 1, 1)
+    k = kp[bi, hi, at.clamp(min=0)].flatten(3, 4).float()
+    v = vp[bi, hi, at.clamp(min=0)].flatten(3, 4).float()
+    keys = (at[..., None] * PAGE + torch.arange(PAGE, device=DEV)).flatten(3, 4)
+    rowpos = (torch.arange(nqb * bq, device=DEV).view(nqb, bq)[..., None].expand(nqb, bq, Hq // Hkv)).reshape(nqb, -1)
+    vis = (keys >= 0)[:, :, :, None] & (keys[:, :, :, None] <= rowpos[..., None])
+    out = _softmax_v(qp.float() @ k.transpose(-1, -2) * d ** -0.5, vis, v)
+    out = out.view(B, Hkv, nqb, bq, Hq // Hkv, d).permute(0, 2, 3, 1, 4, 5).reshape(B, nqb * bq, Hq, d)
+    return {"ptr": ptr.to(torch.int32), "idx": idx[:, :, :total].reshape(-1), "out": out[b, i].to(q.dtype)}
+
+
+def _plain_resize(s, slots, new):
+    """Sequences `slots` get the lengths `new`: pages past the end are given back, a shared page
+    that will be written is copied, missing pages are taken, the lowest free ones first."""
+    kp, vp, table, lens, refs = s["k_pages"], s["v_pages"], s["table"], s["lens"], s["refs"]
+    sl, P, M = slots.long(), s["refs"].numel(), table.shape[1]
+    cols = torch.arange(M, device=DEV)
+    old, new, rows = lens[sl].long(), new.long(), table[sl].long()
+    need = (new + PAGE - 1) // PAGE
+    drop = (rows >= 0) & (cols >= need[:, None])
+    refs.scatter_add_(0, rows.clamp(min=0).flatten(), -drop.int().flatten())
+    rows = torch.where(drop, -1, rows)
+    part = (new > old) & (old % PAGE > 0)
+    last = (old // PAGE).clamp(max=M - 1)
+    mine = torch.where(part, torch.gather(rows, 1, last[:, None])[:, 0], -1)
+    earlier = ((mine[:, None] == mine) & part & part[:, None]).tril(-1).sum(1)
+    copy = part & (refs[mine.clamp(min=0)] - earlier > 1)
+    miss = (rows < 0) & (cols < need[:, None])
+    want = torch.cat([copy[:, None], miss], 1)
+    rank = torch.cumsum(want.flatten().long(), 0).view(want.shape)
+    refused = (new > old) & (rank[:, -1] > (refs == 0).sum())
+    free = torch.sort((refs != 0).int(), stable=True).indices
+    give = torch.where(want & ~refused[:, None], free[(rank - 1).clamp(min=0, max=P - 1)], -1)
+    copy &= ~refused
+    rows = torch.where(miss & ~refused[:, None], give[:, 1:], rows)
+    rows = torch.where(copy[:, None] & (cols == last[:, None]), give[:, :1], rows)
+    refs.scatter_add_(0, mine.clamp(min=0), -copy.int())
+    extra = torch.cat([refs, refs.new_zeros(1)])
+    extra[torch.where(give >= 0, give, P).flatten()] = 1
+    refs.copy_(extra[:P])
+    # the rows of the copied pages; every other request rewrites a page of its own with itself
+    frm = torch.where(copy, mine, rows[:, 0].clamp(min=0))
+    to = torch.where(copy, give[:, 0], frm)
+    below = (torch.arange(PAGE, device=DEV) < (old % PAGE)[:, None])[:, None, :, None]
+    kp[:, to] = torch.where(below, kp[:, frm], kp[:, to])
+    vp[:, to] = torch.where(below, vp[:, frm], vp[:, to])
+    table[sl] = rows.int()
+    lens[sl] = torch.where(refused, old, new).int()
+
+
+def _plain_fork(s):
+    table, lens, refs, src, dst = s["table"], s["lens"], s["refs"], s["src"].long(), s["dst"].long()
+    rows = table[src]
+    used = torch.arange(table.shape[1], device=DEV) * PAGE < lens[src][:, None]
+    rows = torch.where(used, rows, -1)
+    refs.scatter_add_(0, rows.clamp(min=0).flatten().long(), (rows >= 0).int().flatten())
+    table[dst] = rows
+    lens[dst] = lens[src]
+
+
+def _plain_append(s, kp, vp):
+    """New tokens k, v [layers, T, Hkv, d] become the last ones of the sequences `slots`."""
+    cu, sl = s["cu"].long(), s["slots"].long()
+    k, v = (x if x.dim() == 4 else x[None] for x in (s["k"], s["v"]))
+    t = torch.arange(k.shape[1], device=DEV)
+    b = torch.searchsorted(cu[1:], t, right=True)
+    pos = s["lens"].long()[sl[b]] - (cu[b + 1] - t)
+    page = s["table"].long()[sl[b], pos // PAGE]
+    kp[:, page, :, pos % PAGE] = k.transpose(0, 1)
+    vp[:, page, :, pos % PAGE] = v.transpose(0, 1)
+
+
+def _plain_compact(s):
+    """The kept ones of the tokens from `start` on move up to it."""
+    sl, cu, start = s["slots"].long(), s["cu_keep"].long(), s["start"].long()
+    t = torch.arange(s["keep"].numel(), device=DEV)
+    real = t < cu[-1]
+    b = torch.searchsorted(cu[1:], t, right=True).clamp(max=sl.numel() - 1)
+    to = start[b] + torch.where(real, t - cu[b], 0)
+    frm = torch.where(real, start[b] + s["keep"].long(), to)
+    table = s["table"].long()
+    fp, tp = table[sl[b], frm // PAGE], table[sl[b], to // PAGE]
+    for pages in (s["k_pages"], s["v_pages"]):
+        pages[:, tp, :, to % PAGE] = pages[:, fp, :, frm % PAGE]
+    s["lens"][sl] = (start + cu[1:] - cu[:-1]).int()
+
+
+def _plain_page_summary(s):
+    table, P = s["table"].long(), s["refs"].numel()
+    whole = (torch.arange(table.shape[1], device=DEV) + 1) * PAGE <= s["lens"].long()[:, None]
+    codes, scales = _summary(s["k_pages"][table.clamp(min=0).flatten()])
+    at = torch.where(whole & (table >= 0), table, P).flatten()
+    for name, x in (("codes", codes), ("scales", scales)):
+        wide = torch.cat([s[name], s[name][:1]])
+        wide[at] = x
+        s[name].copy_(wide[:P])
+
+
+# ------------------------------------------------------------------------------------ one pass
+
+def run(s):
+    kind = s["case"]["kind"]
+    state = ("table", "lens", "refs", "k_pages", "v_pages")
+    if kind == "branch":
+        if own:
+            b = _binding()
+            cache = (s["k_pages"], s["v_pages"], s["table"], s["lens"], s["refs"])
+            b.pages_resize(*cache, s["dst"])  # what the slots held is released
+            b.pages_fork(s["table"], s["lens"], s["refs"], s["src"], s["dst"])
+            b.pages_resize(*cache, s["dst"], s["new_lens"])
+        else:
+            _plain_resize(s, s["dst"], s["new_lens"] * 0)
+            _plain_fork(s)
+            _plain_resize(s, s["dst"], s["new_lens"])
+        return {x: s[x] for x in state}
+    if kind == "accept":
+        if own:
+            b = _binding()
+            cache = (s["k_pages"], s["v_pages"], s["table"], s["lens"], s["refs"])
+            b.pages_resize(*cache, s["slots"], s["new_lens"])
+            b.pages_append(s["k"], s["v"], s["k_pages"], s["v_pages"], s["table"], s["lens"], slots=s["slots"],
+                           cu_seqlens=s["cu"], max_seqlen=s["max_new"])
+            b.pages_compact(*cache, s["slots"], s["start"], s["keep"], s["cu_keep"])
+        else:
+            _plain_resize(s, s["slots"], s["new_lens"])
+            _plain_append(s, s["k_pages"], s["v_pages"])
+            _plain_compact(s)
+        return {x: s[x] for x in state}
+    if kind == "ingest":
+        if own:
+            b = _binding()
+            b.pages_resize(s["k_pages"], s["v_pages"], s["table"], s["lens"], s["refs"], s["slots"], s["new_lens"])
+            b.pages_append(s["k"], s["v"], s["k_pages"], s["v_pages"], s["table"], s["lens"], slots=s["slots"],
+                           cu_seqlens=s["cu"], max_seqlen=s["max_new"])
+            b.page_summary(s["k_pages"], s["table"], s["lens"], s["codes"], s["scales"])
+        else:
+            wide = dict(s, k_pages=s["k_pages"][None], v_pages=s["v_pages"][None])
+            _plain_resize(wide, s["slots"], s["new_lens"])
+            _plain_append(s, s["k_pages"][None], s["v_pages"][None])
+            _plain_page_summary(s)
+        return dict({x: s[x] for x in state}, summary=s["codes"].float() * s["scales"][..., None])
+    if kind == "tree":
+        if own:
+            return _binding().tree_attn_paged(s["q"], s["k_pages"], s["v_pages"], s["table"], s["lens"], mask=s["mask"],
+                                              cu_seqlens=s["cu"], max_seqlen=s["max_q"], max_len=s["max_len"])
+        return _plain_tree(s)
+    if kind == "select":
+        if own:
+            b, c = _binding(), s["case"]
+            at = dict(cu_seqlens=s["cu"], max_seqlen=s["max_q"])
+            pages = b.select_pages(s["q"], s["codes"], s["scales"], s["table"], s["lens"], top_k=c["top_k"], n_sink=1,
+                                   n_recent=2, max_len=s["max_len"], **at)
+            return {"pages": pages, "out": b.selected_attn_paged(s["q"], s["k_pages"], s["v_pages"], s["table"], s["lens"],
+                                                                 pages, **at)}
+        return _plain_select(s)
+    if own:
+        b, c = _binding(), s["case"]
+        at = dict(cu_seqlens=s["cu"], max_seqlen=s["max_len"])
+        codes, scales = b.key_summary(s["k"], **at)
+        ptr, idx = b.select_blocks(s["q"], codes, scales, top_k=c["top_k"], block_q=c["block_q"], n_sink=1, n_recent=1, **at)
+        return {"ptr": ptr, "idx": idx, "out": b.blocksparse_attn_prefill(s["q"], s["k"], s["v"], block_q=c["block_q"],
+                                                                          block_ptr=ptr, block_idx=idx, **at)}
+    return _plain_prompt(s)
+
+
+# ------------------------------------------------------------------------ the definition, in 64 bits
+
+def _attend(q, k, v, vis):
+    """One group's rows q [rows, d] over keys k, v [keys, d] where vis [rows, keys], in 64 bits."""
+    a = (q.double() @ k.double().T) / q.shape[1] ** 0.5
+    a = torch.where(vis, a, torch.full_like(a, -1e300))
+    a = torch.where(vis, torch.exp(a - a.max(1, keepdim=True).values), torch.zeros_like(a))
+    z = a.sum(1, keepdim=True)
+    return torch.where(z > 0, a @ v.double() / torch.where(z > 0, z, torch.ones_like(z)), torch.zeros_like(z))
+
+
+def _chosen(rows, keys, n, top_k, sinks, recent):
+    """The blocks that query rows [rows, d] choose among the first n blocks of keys [n * 64, d]."""
+    if n <= top_k:
+        return list(range(n))
+    mean = keys[:n * PAGE].double().view(n, PAGE, -1).sum(1)
+    big = mean.abs().max(1).values
+    unit = torch.where(big > 0, big, torch.ones_like(big))
+    code = torch.round(mean * 127 / unit[:, None])
+    a = rows.double().abs().max()
+    q8 = torch.round(rows.double() * 127 / a) if a > 0 else rows.double() * 0
+    best = (q8 @ code.T).max(0).values
+    # the score is a whole number times the scale, both as 32-bit values, rounded once to 32 bits
+    score = (best * (big / (127 * PAGE)).float().double()).float().tolist()
+    forced = set(range(sinks)) | set(range(n - recent, n))
+    return sorted(sorted(range(n), key=lambda x: (x not in forced, -score[x], x))[:top_k])
+
+
+def exact(case, seed):
+    kind = case["kind"]
+    if kind in ("branch", "accept"):
+        return None  # whole numbers and copies
+    s = prepare(case, seed)
+    if kind == "ingest":  # all pages are free: the sequences take them one after the other
+        want = torch.zeros(s["codes"].shape, dtype=torch.float64, device=DEV)
+        page = 0
+        for b, L in enumerate(s["new_lens"].tolist()):
+            x = s["k"][s["cu"][b]:s["cu"][b] + L // PAGE * PAGE].double().view(L // PAGE, PAGE, *s["k"].shape[1:]).sum(1)
+            big = x.abs().amax(-1, keepdim=True)
+            unit = torch.where(big > 0, big, torch.ones_like(big))
+            want[page:page + L // PAGE] = torch.round(x * 127 / unit) * (big / (127 * PAGE)).float().double()
+            page += _pages(L)
+        return dict(dict.fromkeys(("table", "lens", "refs", "k_pages", "v_pages")), summary=want)
+    q, cu = s["q"], s["cu"].tolist()
+    Hkv, G = case["Hkv"], case["Hq"] // case["Hkv"]
+    out = torch.zeros(q.shape, dtype=torch.float64, device=DEV)
+    lens = s["lens"].tolist()
+    if sum(lens) * Hkv > 12_000_000:
+        return None
+    for b, L in enumerate(lens):
+        m = cu[b + 1] - cu[b]
+        if kind != "prompt":
+            pages = s["table"][b, :_pages(L)].long()
+        for g in range(Hkv):
+            if kind == "prompt":
+                k, v = s["k"][cu[b]:cu[b + 1], g], s["v"][cu[b]:cu[b + 1], g]
+            else:
+                k, v = (s[x][pages, g].reshape(-1, case["d"])[:L] for x in ("k_pages", "v_pages"))
+            hs = slice(g * G, (g + 1) * G)
+            if kind == "tree":
+                vis = torch.ones((m, L), dtype=torch.bool, device=DEV)
+                for i in range(m):
+                    if s["mask"] is None:
+                        seen = [j <= i for j in range(m)]
+                    else:
+                        w = s["mask"][cu[b] + i].tolist()
+                        seen = [bool(w[j // 64] >> j % 64 & 1) for j in range(m)]
+                    vis[i, L - m:] = torch.tensor(seen, device=DEV)
+                rows = q[cu[b]:cu[b + 1], hs].reshape(m * G, -1)
+                out[cu[b]:cu[b + 1], hs] = _attend(rows, k, v, vis.repeat_interleave(G, 0)).view(m, G, -1)
+                continue
+            step = case["block_q"] if kind == "prompt" else 1
+            sinks, recent = (1, 1) if kind == "prompt" else (1, 2)
+            for r0 in range(0, m, step):
+                r1 = min(m, r0 + step)
+                p0 = L - m + r0  # the position of the first row
+                n = p0 // PAGE
+                rows = q[cu[b] + r0:cu[b] + r1, hs]
+                blocks = _chosen(rows.reshape(-1, case["d"]), k, n, case["top_k"], sinks, recent)
+                at = torch.tensor(blocks + list(range(n, -(-(L - m + r1) // PAGE))), device=DEV)
+                keys = (at[:, None] * PAGE + torch.arange(PAGE, device=DEV)).flatten()
+                keys = keys[keys < L]
+                pos = torch.arange(p0, L - m + r1, device=DEV).repeat_interleave(G)
+                o = _attend(rows.reshape(-1, case["d"]), k[keys], v[keys], keys <= pos[:, None])
+                out[cu[b] + r0:cu[b] + r1, hs] = o.view(r1 - r0, G, -1)
+    if kind == "tree":
+        return out
+    return {"pages": None, "out": out} if kind == "select" else {"ptr": None, "idx": None, "out": out}
