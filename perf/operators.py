@@ -472,7 +472,7 @@ def _plain_append(s, kp, vp):
 
 
 def _plain_compact(s):
-    """The kept ones of the tokens from `start` on move up to it."""
+    """The kept ones of the tokens from `start` on move up to it; pages past the new end are given back."""
     sl, cu, start = s["slots"].long(), s["cu_keep"].long(), s["start"].long()
     t = torch.arange(s["keep"].numel(), device=DEV)
     real = t < cu[-1]
@@ -483,7 +483,12 @@ def _plain_compact(s):
     fp, tp = table[sl[b], frm // PAGE], table[sl[b], to // PAGE]
     for pages in (s["k_pages"], s["v_pages"]):
         pages[:, tp, :, to % PAGE] = pages[:, fp, :, frm % PAGE]
-    s["lens"][sl] = (start + cu[1:] - cu[:-1]).int()
+    new = start + cu[1:] - cu[:-1]
+    rows = table[sl]
+    drop = (rows >= 0) & (torch.arange(rows.shape[1], device=DEV) >= ((new + PAGE - 1) // PAGE)[:, None])
+    s["refs"].scatter_add_(0, rows.clamp(min=0).flatten(), -drop.int().flatten())
+    s["table"][sl] = torch.where(drop, -1, rows).int()
+    s["lens"][sl] = new.int()
 
 
 def _plain_page_summary(s):
