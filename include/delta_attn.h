@@ -369,6 +369,182 @@ da_status da_launch_workgroups(int B, int max_seqlen, int packed, int Hq, int Hk
                                int window, int n_sink, int gamma, int block_q, int mode,
                                da_workgroups* w);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Serving after the prefill: a paged cache, the attention of new tokens over it,
+ * and the selection of key blocks.
+ *
+ * A cache is pages of DA_PAGE_TOKENS tokens (the attention kernels' key tile):
+ *   k_pages, v_pages  [P, Hkv, 64, d] bf16, or [layers, P, Hkv, 64, d] for the calls
+ *                     that take `layers` (one page id names the page of every layer)
+ *   table             int32 [S, M]: page ids of each sequence ("slot"), -1: none
+ *   lens              int32 [S]: tokens of each slot, 0: empty
+ *   refs              int32 [P]: how many slots hold each page, 0: free
+ * all on the device.  Token j of slot s is row j % 64 of page table[s][j / 64].  A
+ * slot of L tokens holds exactly its first ceil(L / 64) entries, the others are -1;
+ * a cache starts with table -1, lens 0 and refs 0, and the da_pages_* calls keep
+ * that.  What a page holds past the last token does not matter (any bits, NaN
+ * included) and is left as it is.
+ *
+ * Requests of one call (n of them, at most DA_PAGES_MAX_REQUESTS) are served as if
+ * in order, with results that do not depend on timing.  A request that cannot be
+ * served is refused: its result is negative and its slot stays as it was.  The
+ * kernels check every slot, length and page id they read against S, M and P, so a
+ * wrong one is refused or skipped, never followed.  B sequences of a batch take the
+ * slots slots[0 .. B-1] (distinct, where the call writes), or 0 .. B-1 when `slots`
+ * is NULL (then B <= S).  cu_seqlens and max_seqlen name the new tokens of each
+ * sequence as in the prefill calls; rows of a sequence past max_seqlen are ignored.
+ * Other conventions (streams, validation, errors) are those above; integer arrays
+ * are 4-byte aligned, `result` of resize and compact 16-byte.  Only bf16, d 64 or
+ * 128, any Hq / Hkv.
+ */
+#define DA_PAGE_TOKENS 64
+#define DA_PAGES_MAX_REQUESTS 1024
+
+/*
+ * Slot dst[i] becomes a copy of slot src[i] that shares all its pages (no token is
+ * copied; da_pages_resize copies a shared page before it is written).
+ * result[i] = the length, or -1: a slot out of range, dst[i] not empty or named
+ * before in the call, or src[i] the destination of some request of the call.
+ */
+da_status da_pages_fork(int32_t* table, int32_t* lens, int32_t* refs, int S, int M, int P,
+                        const int32_t* src, const int32_t* dst, int n, int32_t* result,
+                        void* stream);
+
+/*
+ * Slot slots[i] gets new_lens[i] tokens; new_lens NULL: 0 (the slots are freed).  First
+ * all pages past new ends are given back.  Then slots that grow, in order, get the
+ * lowest free pages; where the page that holds the slot's last token is not full and
+ * other slots hold it too, the slot first gets a page of its own with a copy of its
+ * tokens (all layers).  Of several slots of the call that share such a page the last
+ * keeps it when no other slot does.  New tokens' rows hold whatever the pages held.
+ * result [n, 4]: {new length, the page copied from or -1, the page copied to or -1,
+ * tokens copied}; a new length of -1: a slot out of range or named before, a length
+ * outside [0, 64 M], or too few free pages (then every later slot of the call that
+ * would grow is refused as well).
+ */
+da_status da_pages_resize(void* k_pages, void* v_pages, int layers, int Hkv, int d,
+                          int32_t* table, int32_t* lens, int32_t* refs, int S, int M, int P,
+                          const int32_t* slots, const int32_t* new_lens, int n, int32_t* result,
+                          void* stream);
+
+/*
+ * Writes the keys and values k, v [layers, T, Hkv, d] of new tokens as the last ones of
+ * their slots, which da_pages_resize has made room for: row i of the m rows of
+ * sequence b goes to token lens[slot] - m + i.
+ */
+da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
+                          int layers, int Hkv, int d, const int32_t* table, const int32_t* lens,
+                          int S, int M, int P, const int32_t* slots, const int32_t* cu_seqlens,
+                          int B, int max_seqlen, void* stream);
+
+/*
+ * Keeps some of a slot's tokens from start[i] on: those at start[i] + keep[j], j in
+ * [cu_keep[i], cu_keep[i + 1]), ascending, move up to start[i], in every layer, the
+ * rest is dropped and pages past the new end are given back (the accepted path of a
+ * draft tree, or tokens that stay when others are evicted).
+ * result [n, 4]: {tokens kept from start on, ...}, the rest for the call's own use; -1: a
+ * slot out of range or named before, a start outside the slot, places that do not
+ * ascend or lie outside it, offsets outside [0, n_keep], or a page that would be
+ * written while another slot holds it.
+ */
+da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, int d,
+                           int32_t* table, int32_t* lens, int32_t* refs, int S, int M, int P,
+                           const int32_t* slots, const int32_t* start, const int32_t* keep,
+                           int64_t n_keep, const int32_t* cu_keep, int n, int32_t* result,
+                           void* stream);
+
+/*
+ * Attention of the last m tokens of each sequence (drafted tokens, whose keys and
+ * values are in the cache already: lens counts them).  Row i (token L - m + i, L
+ * the slot's length) sees every token before the m new ones, and of the new ones
+ *   mask NULL: those up to itself (single tokens, causal chunks);
+ *   mask [T, mask_words] of 64-bit words: new token j where bit j % 64 of word j / 64
+ *     is set (64 * mask_words >= max_seqlen), itself included or not.
+ * A row that sees no token is 0.  Keys and values of all L tokens must be finite.
+ * max_len: no slot is longer; tokens past it are ignored.  lse (fp32 [T, Hq], may be
+ * NULL): log of the sum of exp(q.k / sqrt d), -inf for a row that sees nothing.
+ * workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, 0) bytes
+ * (may be 0).
+ */
+da_status tree_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out,
+                          float* lse, const int32_t* table, const int32_t* lens, int S, int M,
+                          int P, const int32_t* slots, const int32_t* cu_seqlens, int B,
+                          int max_seqlen, int max_len, int Hq, int Hkv, int d,
+                          const uint64_t* mask, int mask_words, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Summaries of whole blocks of 64 keys, for the selections below: the mean key as 8-bit
+ * codes and one scale.  With S_c the sum of the 64 keys' channel c and A = max_c |S_c|:
+ *   code_c = round(127 S_c / A) (ties to even, 0 if A is 0), scale = A / (127 * 64).
+ * da_key_summary: of k [T, Hkv, d], into codes int8 [blocks, Hkv, d] and scales fp32
+ * [blocks, Hkv]; block j of sequence b has the place floor(base / 64) + b + j, base its
+ * first token, and da_key_summary_blocks(T, B) places are enough (places that no
+ * whole block has are left as they are).
+ * da_page_summary: of pages, into [P, Hkv, d] and [P, Hkv]: the whole pages of each
+ * sequence from the page of token first[b] (first NULL: 0) on, up to max_new tokens
+ * further.
+ */
+da_status da_key_summary(const void* k, const int32_t* cu_seqlens, int B, int max_seqlen,
+                         int Hkv, int d, void* codes, float* scales, void* stream);
+int64_t da_key_summary_blocks(int64_t T, int B);
+da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* table,
+                          const int32_t* lens, int S, int M, int P, const int32_t* slots,
+                          const int32_t* first, int B, int max_new, void* codes, float* scales,
+                          void* stream);
+
+/*
+ * The blocks that a group of query rows attends to: of its n candidates the last
+ * n_recent, the first n_sink and those with the highest scores, top_k in all (n where n
+ * <= top_k), ties to the lowest.  With a the largest |q| of the group,
+ *   score = scale * max over the group's rows of sum_c round(127 q_c / a) code_c,
+ * the sum a whole number and the product rounded once to fp32, so that the choice
+ * is the same however it is computed.  n_sink + n_recent <= top_k.
+ *
+ * da_select_blocks (prefill): a group is the rows of a query block of block_q rows (64,
+ * 128 or 256) in the heads of one kv head, its candidates the key tiles before the
+ * block.  Writes lists for blocksparse_attn_prefill and
+ * delta_attn_prefill_blocksparse: block_ptr [B, Hkv, ceil(max_seqlen / block_q) + 1]
+ * and block_idx of da_select_blocks_entries(B, max_seqlen, Hkv, top_k, block_q) entries
+ * (-1 where a shorter sequence has no lists; may be 0).  Up to 1,572,864 tokens.
+ *
+ * da_select_pages (decode): a group is one token in the heads of one kv head, its
+ * candidates the pages before the token's own.  Writes page positions (indices into
+ * the slot's table row) pages [T, Hkv, top_k], ascending, -1 behind the last.
+ * workspace: da_select_pages_workspace_bytes() bytes; none when max_len / 64 <= top_k.
+ */
+int64_t da_select_blocks_entries(int B, int max_seqlen, int Hkv, int top_k, int block_q);
+da_status da_select_blocks(const void* q, const void* codes, const float* scales,
+                           const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv,
+                           int d, int top_k, int n_sink, int n_recent, int block_q,
+                           int32_t* block_ptr, int32_t* block_idx, void* stream);
+size_t da_select_pages_workspace_bytes(int B, int max_seqlen, int Hkv, int max_len);
+da_status da_select_pages(const void* q, const void* codes, const float* scales,
+                          const int32_t* table, const int32_t* lens, int S, int M, int P,
+                          const int32_t* slots, const int32_t* cu_seqlens, int B, int max_seqlen,
+                          int max_len, int Hq, int Hkv, int d, int top_k, int n_sink,
+                          int n_recent, int32_t* pages, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Attention of the last m tokens of each sequence over selected pages: the row of
+ * token p in kv head g sees the whole pages pages[row][g][0 .. top_k-1] (positions below
+ * p / 64, each at most once; other values are skipped) and its own page up to itself.
+ * lse as tree_attn_paged; workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d,
+ * 1, top_k) bytes.
+ */
+da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out,
+                              float* lse, const int32_t* table, const int32_t* lens, int S, int M,
+                              int P, const int32_t* slots, const int32_t* cu_seqlens, int B,
+                              int max_seqlen, int Hq, int Hkv, int d, const int32_t* pages,
+                              int top_k, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of tree_attn_paged (top_k 0) and selected_attn_paged (max_len 1); 0 if none is
+ * needed or the sizes are invalid.  One of a longer max_len serves shorter ones. */
+size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len,
+                                int top_k);
+
 /* Static, NUL-terminated name of a status code. */
 const char* da_status_string(da_status s);
 

@@ -36,6 +36,16 @@ SIGNATURES = {
     "delta_attn_prefill_blocksparse": "pppppiiiiiippipzpu",
     "da_check_inputs": "piiiipplpp",
     "delta_attn_prefill_noalloc": "pppppiiiiiiiip",
+    "da_pages_fork": "pppiiippipp",
+    "da_pages_resize": "ppiiipppiiippipp",
+    "da_pages_append": "pplppiiippiiippiip",
+    "da_pages_compact": "ppiiipppiiippplpipp",
+    "tree_attn_paged": "pppppppiiippiiiiiipipzp",
+    "selected_attn_paged": "pppppppiiippiiiiipipzp",
+    "da_key_summary": "ppiiiippp",
+    "da_page_summary": "piippiiippiippp",
+    "da_select_blocks": "ppppiiiiiiiiippp",
+    "da_select_pages": "pppppiiippiiiiiiiiippzp",
 }
 
 
@@ -95,6 +105,14 @@ def load_library(path: str = LIB_PATH, check_abi: bool = True):
     lib.da_workspace_bytes.restype = ctypes.c_size_t
     lib.da_workspace_bytes_correction.argtypes = [ctypes.c_int] * 7
     lib.da_workspace_bytes_correction.restype = ctypes.c_size_t
+    lib.da_paged_workspace_bytes.argtypes = [ctypes.c_int] * 7
+    lib.da_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.da_select_pages_workspace_bytes.argtypes = [ctypes.c_int] * 4
+    lib.da_select_pages_workspace_bytes.restype = ctypes.c_size_t
+    lib.da_select_blocks_entries.argtypes = [ctypes.c_int] * 5
+    lib.da_select_blocks_entries.restype = ctypes.c_int64
+    lib.da_key_summary_blocks.argtypes = [ctypes.c_int64, ctypes.c_int]
+    lib.da_key_summary_blocks.restype = ctypes.c_int64
     lib.da_fused_supported.argtypes = [ctypes.c_int] * 3
     lib.da_fused_supported.restype = ctypes.c_int
     lib.da_fused_supported_blocksparse.argtypes = [ctypes.c_int] * 4
@@ -405,3 +423,382 @@ def check_inputs(*, max_seqlen, B=None, cu_seqlens=None, Hkv=None, block_q=None,
         raise DeltaAttnError("da_check_inputs", rc, lib.da_last_hip_error())
     return int(result.item())
 
+
+
+# ---------------------------------------------------------------------------------------------
+# Serving after the prefill: the paged cache (see include/delta_attn.h for its layout and rules),
+# the attention over it and the selection of key blocks.
+#
+# k_pages / v_pages are [P, Hkv, 64, d] bf16, or [layers, P, Hkv, 64, d] where a call moves the
+# tokens of all layers; table int32 [S, M], lens int32 [S], refs int32 [P].  A batch of new tokens
+# is packed like a prefill's: B sequences of T / B rows, or cu_seqlens and max_seqlen; sequence b
+# is slot slots[b] (default b).  Calls run on the device of their tensors, whichever is current.
+
+PAGE_TOKENS = 64
+
+
+class _On:
+    """The device of a call and its stream: sets the device where another is current, and takes
+    new tensors from that stream's memory."""
+
+    def __init__(self, dev, stream):
+        if dev.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU (got {dev})")
+        self.dev = dev
+        self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
+        self.other = (dev.index if dev.index is not None else 0) != torch.cuda.current_device()
+        self.aside = stream is not None
+
+    def call(self, name, *args):
+        if self.other:
+            with torch.cuda.device(self.dev):
+                _call(name, *args, self.stream.cuda_stream)
+        else:
+            _call(name, *args, self.stream.cuda_stream)
+
+    def empty(self, shape, dtype):
+        if not self.aside:
+            return torch.empty(shape, dtype=dtype, device=self.dev)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.dev)
+
+    def workspace(self, given, nbytes):
+        """(pointer, size) of the caller's workspace or of one that lasts for this call."""
+        if given is None:
+            if not nbytes:
+                return None, None, 0
+            given = self.empty(nbytes, torch.uint8)
+        else:
+            _on_device("workspace", given, self.dev, None)
+        return given, given.data_ptr(), given.numel() * given.element_size()
+
+
+def _ints(name, t, dev, shape=None):
+    _on_device(name, t, dev, torch.int32)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
+
+
+def _table(table, lens, dev):
+    _ints("table", table, dev)
+    if table.dim() != 2:
+        raise ValueError("table must be [S, M]")
+    _ints("lens", lens, dev, (table.shape[0],))
+    return table.shape
+
+
+def _pages(k_pages, v_pages, layered=False):
+    """(dev, layers, P, Hkv, d) of a cache's pages."""
+    dev = k_pages.device
+    _on_device("k_pages", k_pages, dev, torch.bfloat16)
+    if v_pages is not None:
+        _on_device("v_pages", v_pages, dev, torch.bfloat16)
+        if v_pages.shape != k_pages.shape:
+            raise ValueError("k_pages and v_pages must have the same shape")
+    n = k_pages.dim()
+    if n != 4 and not (layered and n == 5):
+        raise ValueError("pages must be [P, Hkv, 64, d]" + (" or [layers, P, Hkv, 64, d]" if layered else ""))
+    if k_pages.shape[-2] != PAGE_TOKENS:
+        raise ValueError(f"pages must hold {PAGE_TOKENS} tokens")
+    P, Hkv, _, d = k_pages.shape[-4:]
+    return dev, (k_pages.shape[0] if n == 5 else 1), P, Hkv, d
+
+
+def _slots(slots, B, S, dev):
+    if slots is None:
+        if B > S:
+            raise ValueError(f"{B} sequences without slots, but the table has {S}")
+        return None
+    _ints("slots", slots, dev, (B,))
+    return slots.data_ptr()
+
+
+def _new_rows(T, B, cu_seqlens, max_seqlen, dev):
+    """(B, rows per sequence, at most) of a batch of T new rows."""
+    if cu_seqlens is None:
+        B = 1 if B is None else int(B)
+        if B < 1 or T < 1 or T % B != 0:
+            raise ValueError("the number of rows must be a multiple of B for a fixed-length batch")
+        return B, T // B
+    _ints("cu_seqlens", cu_seqlens, dev)
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        raise ValueError("cu_seqlens must be 1-D with B + 1 >= 2 entries")
+    if max_seqlen is None:
+        raise ValueError("max_seqlen is required with cu_seqlens")
+    return cu_seqlens.numel() - 1, int(max_seqlen)
+
+
+def _requests(n, result, shape, on):
+    if result is None:
+        return on.empty(shape, torch.int32)
+    _ints("result", result, on.dev, shape)
+    return result
+
+
+def pages_fork(table, lens, refs, src, dst, *, result=None, stream=None):
+    """Slots ``dst`` become copies of slots ``src`` that share their pages.  Returns ``result``
+    int32 [n]: the lengths, -1 where a request was refused (da_pages_fork)."""
+    on = _On(table.device, stream)
+    S, M = _table(table, lens, on.dev)
+    _ints("refs", refs, on.dev, (refs.numel(),))
+    n = src.numel()
+    _ints("src", src, on.dev, (n,))
+    _ints("dst", dst, on.dev, (n,))
+    result = _requests(n, result, (n,), on)
+    on.call("da_pages_fork", _ptr(table), _ptr(lens), _ptr(refs), S, M, refs.numel(), _ptr(src), _ptr(dst), n,
+            _ptr(result))
+    return result
+
+
+def pages_resize(k_pages, v_pages, table, lens, refs, slots, new_lens=None, *, result=None, stream=None):
+    """Slots get the lengths ``new_lens`` (None: 0, they are freed): pages are given back, taken,
+    and copied where a shared one will be written.  Returns ``result`` int32 [n, 4], whose first
+    column is the new length or -1 where a request was refused (da_pages_resize)."""
+    dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _ints("refs", refs, dev, (P,))
+    n = slots.numel()
+    _ints("slots", slots, dev, (n,))
+    if new_lens is not None:
+        _ints("new_lens", new_lens, dev, (n,))
+    result = _requests(n, result, (n, 4), on)
+    on.call("da_pages_resize", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
+            P, _ptr(slots), _ptr(new_lens), n, _ptr(result))
+    return result
+
+
+def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_seqlens=None, max_seqlen=None,
+                 stream=None):
+    """Writes the keys and values of new tokens, [T, Hkv, d] or [layers, T, Hkv, d], as the last
+    ones of their sequences, which pages_resize has made room for (da_pages_append)."""
+    dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    for name, t in (("k", k), ("v", v)):
+        _on_device(name, t, dev, torch.bfloat16)
+        if t.dim() != k_pages.dim() - 1 or t.shape[-2:] != (Hkv, d) or (t.dim() == 4 and t.shape[0] != layers):
+            raise ValueError(f"{name} must be [T, Hkv, d] for pages of one layer, [layers, T, Hkv, d] for more")
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    T = k.shape[-3]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    on.call("da_pages_append", _ptr(k), _ptr(v), T, _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table),
+            _ptr(lens), S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N)
+
+
+def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_keep, *, result=None, stream=None):
+    """Of the tokens of slots[i] from start[i] on, those at start[i] + keep[cu_keep[i]:cu_keep[i + 1]]
+    move up to start[i]; the rest is dropped.  Returns ``result`` int32 [n, 4], whose first column is
+    the number kept or -1 where a request was refused (da_pages_compact)."""
+    dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _ints("refs", refs, dev, (P,))
+    n = slots.numel()
+    _ints("slots", slots, dev, (n,))
+    _ints("start", start, dev, (n,))
+    _ints("keep", keep, dev, (keep.numel(),))
+    _ints("cu_keep", cu_keep, dev, (n + 1,))
+    result = _requests(n, result, (n, 4), on)
+    if not keep.numel():  # (an empty tensor has no address; no place is read)
+        keep = cu_keep
+        n_keep = 0
+    else:
+        n_keep = keep.numel()
+    on.call("da_pages_compact", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
+            P, _ptr(slots), _ptr(start), _ptr(keep), n_keep, _ptr(cu_keep), n, _ptr(result))
+    return result
+
+
+def _queries(q, out, lse, Hkv, d, on):
+    _on_device("q", q, on.dev, torch.bfloat16)
+    if q.dim() != 3 or q.shape[2] != d or q.shape[1] % Hkv:
+        raise ValueError(f"q must be [T, Hq, {d}] with Hq a multiple of {Hkv}")
+    if out is None:
+        out = on.empty(q.shape, torch.bfloat16)
+    else:
+        _on_device("out", out, on.dev, torch.bfloat16)
+        if out.shape != q.shape:
+            raise ValueError(f"out must have the shape of q {tuple(q.shape)}")
+        o0, o1 = _span(out)
+        t0, t1 = _span(q)
+        if o0 < t1 and t0 < o1:
+            raise ValueError("out must not overlap q")
+    if lse is not None:
+        _on_device("lse", lse, on.dev, torch.float32)
+        if tuple(lse.shape) != tuple(q.shape[:2]):
+            raise ValueError("lse must be [T, Hq]")
+    return out
+
+
+def paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k=0) -> int:
+    """Workspace of tree_attn_paged, or with top_k of selected_attn_paged (da_paged_workspace_bytes)."""
+    return int(load_library().da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k))
+
+
+def tree_attn_paged(q, k_pages, v_pages, table, lens, *, mask=None, slots=None, B=None, cu_seqlens=None,
+                    max_seqlen=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
+    """Attention of the last tokens of each sequence, whose keys and values are in the cache:
+    single tokens or causal chunks, or trees of drafts where ``mask`` int64 [T, words] has a bit for
+    each drafted token that a row sees.  ``max_len`` bounds the lengths (default: the table's room).
+    Returns ``out`` [T, Hq, d] (tree_attn_paged)."""
+    dev, _, P, Hkv, d = _pages(k_pages, v_pages)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    out = _queries(q, out, lse, Hkv, d, on)
+    T, Hq = q.shape[:2]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    words = 0
+    if mask is not None:
+        _on_device("mask", mask, dev, torch.int64)
+        if mask.dim() != 2 or mask.shape[0] != T or mask.shape[1] * 64 < N:
+            raise ValueError("mask must be [T, words] with a bit for each of max_seqlen tokens")
+        words = mask.shape[1]
+    room = M * PAGE_TOKENS
+    max_len = room if max_len is None else min(int(max_len), room)
+    ws, ptr, size = on.workspace(workspace, paged_workspace_bytes(B, N, Hq, Hkv, d, max_len) if workspace is None else 0)
+    on.call("tree_attn_paged", _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), S, M,
+            P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, max_len, Hq, Hkv, d, _ptr(mask), words, ptr, size)
+    return out
+
+
+def selected_attn_paged(q, k_pages, v_pages, table, lens, pages, *, slots=None, B=None, cu_seqlens=None,
+                        max_seqlen=None, out=None, lse=None, workspace=None, stream=None):
+    """Attention of the last tokens of each sequence over the pages that ``pages`` [T, Hkv, top_k]
+    lists for them (as select_pages does) and the page each of them is in.  Returns ``out``
+    [T, Hq, d] (selected_attn_paged)."""
+    dev, _, P, Hkv, d = _pages(k_pages, v_pages)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    out = _queries(q, out, lse, Hkv, d, on)
+    T, Hq = q.shape[:2]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    _ints("pages", pages, dev)
+    if pages.dim() != 3 or tuple(pages.shape[:2]) != (T, Hkv):
+        raise ValueError("pages must be [T, Hkv, top_k]")
+    top_k = pages.shape[2]
+    ws, ptr, size = on.workspace(workspace, paged_workspace_bytes(B, N, Hq, Hkv, d, 1, top_k) if workspace is None else 0)
+    on.call("selected_attn_paged", _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens),
+            S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, Hq, Hkv, d, _ptr(pages), top_k, ptr, size)
+    return out
+
+
+def _summaries(codes, scales, blocks, Hkv, d, dev):
+    _on_device("codes", codes, dev, torch.int8)
+    _on_device("scales", scales, dev, torch.float32)
+    if codes.dim() != 3 or codes.shape[0] < blocks or tuple(codes.shape[1:]) != (Hkv, d):
+        raise ValueError(f"codes must be [{blocks}, {Hkv}, {d}]")
+    if tuple(scales.shape) != tuple(codes.shape[:2]):
+        raise ValueError(f"scales must be [{codes.shape[0]}, {Hkv}]")
+
+
+def key_summary(k, *, B=None, cu_seqlens=None, max_seqlen=None, codes=None, scales=None, stream=None):
+    """8-bit summaries of the whole 64-key blocks of k [T, Hkv, d]: (codes int8 [blocks, Hkv, d],
+    scales fp32 [blocks, Hkv]), for select_blocks (da_key_summary)."""
+    on = _On(k.device, stream)
+    _on_device("k", k, on.dev, torch.bfloat16)
+    if k.dim() != 3:
+        raise ValueError("k must be [T, Hkv, d]")
+    T, Hkv, d = k.shape
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, on.dev)
+    blocks = int(load_library().da_key_summary_blocks(T, B))
+    if codes is None:
+        codes = on.empty((blocks, Hkv, d), torch.int8)
+    if scales is None:
+        scales = on.empty((codes.shape[0], Hkv), torch.float32)
+    _summaries(codes, scales, blocks, Hkv, d, on.dev)
+    on.call("da_key_summary", _ptr(k), _ptr(cu_seqlens), B, N, Hkv, d, _ptr(codes), _ptr(scales))
+    return codes, scales
+
+
+def page_summary(k_pages, table, lens, codes, scales, *, slots=None, first=None, max_new=None, stream=None):
+    """Updates the summaries codes int8 [P, Hkv, d] and scales fp32 [P, Hkv] of the whole pages of
+    each sequence, those from token ``first`` [B] (default 0) on and at most ``max_new`` tokens
+    further (default: all; a decoding step that has added n tokens passes the lengths before it and
+    n) (da_page_summary)."""
+    dev, _, P, Hkv, d = _pages(k_pages, None)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _summaries(codes, scales, P, Hkv, d, dev)
+    B = S if slots is None else slots.numel()
+    if first is not None:
+        _ints("first", first, dev, (B,))
+    on.call("da_page_summary", _ptr(k_pages), Hkv, d, _ptr(table), _ptr(lens), S, M, P, _slots(slots, B, S, dev),
+            _ptr(first), B, M * PAGE_TOKENS if max_new is None else int(max_new), _ptr(codes), _ptr(scales))
+
+
+def select_blocks(q, codes, scales, *, top_k, block_q, n_sink=1, n_recent=1, B=None, cu_seqlens=None, max_seqlen=None,
+                  block_ptr=None, block_idx=None, stream=None):
+    """The key tiles that each query block of block_q rows attends to, by score against key_summary's
+    summaries: (block_ptr, block_idx) for blocksparse_attn_prefill and delta_attn_prefill_blocksparse
+    (da_select_blocks)."""
+    on = _On(q.device, stream)
+    _on_device("q", q, on.dev, torch.bfloat16)
+    if q.dim() != 3 or codes.dim() != 3:
+        raise ValueError("q must be [T, Hq, d] and codes [blocks, Hkv, d]")
+    T, Hq, d = q.shape
+    Hkv = codes.shape[1]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, on.dev)
+    lib = load_library()
+    _summaries(codes, scales, int(lib.da_key_summary_blocks(T, B)), Hkv, d, on.dev)
+    if block_q not in (64, 128, 256):
+        raise ValueError("block_q must be 64, 128 or 256")
+    entries = int(lib.da_select_blocks_entries(B, N, Hkv, top_k, block_q))
+    nqb = -(-N // block_q)
+    if block_ptr is None:
+        block_ptr = on.empty((B, Hkv, nqb + 1), torch.int32)
+    if block_idx is None:
+        block_idx = on.empty(max(entries, 1), torch.int32)[:entries] if entries else on.empty(1, torch.int32)
+    _ints("block_ptr", block_ptr, on.dev, (B, Hkv, nqb + 1))
+    _ints("block_idx", block_idx, on.dev)
+    if block_idx.numel() < max(entries, 1):
+        raise ValueError(f"block_idx must hold {max(entries, 1)} entries (got {block_idx.numel()})")
+    on.call("da_select_blocks", _ptr(q), _ptr(codes), _ptr(scales), _ptr(cu_seqlens), B, N, Hq, Hkv, d, top_k, n_sink,
+            n_recent, block_q, _ptr(block_ptr), _ptr(block_idx))
+    return block_ptr, block_idx
+
+
+def select_pages(q, codes, scales, table, lens, *, top_k, n_sink=1, n_recent=1, slots=None, B=None, cu_seqlens=None,
+                 max_seqlen=None, max_len=None, pages=None, workspace=None, stream=None):
+    """The pages that each of the last tokens of each sequence attends to, by score against
+    page_summary's summaries: ``pages`` int32 [T, Hkv, top_k] for selected_attn_paged, ascending,
+    -1 behind the last (da_select_pages)."""
+    on = _On(q.device, stream)
+    _on_device("q", q, on.dev, torch.bfloat16)
+    if q.dim() != 3 or codes.dim() != 3:
+        raise ValueError("q must be [T, Hq, d] and codes [P, Hkv, d]")
+    T, Hq, d = q.shape
+    P, Hkv = codes.shape[:2]
+    _summaries(codes, scales, P, Hkv, d, on.dev)
+    S, M = _table(table, lens, on.dev)
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, on.dev)
+    room = M * PAGE_TOKENS
+    max_len = room if max_len is None else min(int(max_len), room)
+    if pages is None:
+        pages = on.empty((T, Hkv, top_k), torch.int32)
+    _ints("pages", pages, on.dev, (T, Hkv, top_k))
+    need = int(load_library().da_select_pages_workspace_bytes(B, N, Hkv, max_len)) if workspace is None else 0
+    ws, ptr, size = on.workspace(workspace, need)
+    on.call("da_select_pages", _ptr(q), _ptr(codes), _ptr(scales), _ptr(table), _ptr(lens), S, M, P,
+            _slots(slots, B, S, on.dev), _ptr(cu_seqlens), B, N, max_len, Hq, Hkv, d, top_k, n_sink, n_recent, _ptr(pages),
+            ptr, size)
+    return pages
+
+
+def tree_mask(parents, device="cpu"):
+    """The mask of tree_attn_paged for draft trees: ``parents`` holds for each sequence the parent of
+    each drafted token (an earlier one of the sequence, or -1 under the context); a row sees itself and
+    its ancestors.  Returns int64 [T, words] on ``device``."""
+    words = max(1, -(-max((len(p) for p in parents), default=1) // 64))
+    rows = []
+    for seq in parents:
+        seen = []
+        for i, p in enumerate(seq):
+            if not -1 <= p < i:
+                raise ValueError(f"the parent of token {i} must be an earlier one or -1 (got {p})")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+        for x in seen:
+            w = [(x >> 64 * k) & 0xFFFFFFFFFFFFFFFF for k in range(words)]
+            rows.append([v - (1 << 64) if v >> 63 else v for v in w])
+    return torch.tensor(rows, dtype=torch.int64).reshape(-1, words).to(device)

@@ -17,12 +17,14 @@ namespace {
 constexpr int kCUs = 256;  // of a gfx950
 constexpr int64_t kPartialBudget = (int64_t)8 << 30;  // bytes of the strided rows' partials
 
-thread_local int g_last_hip_error = 0;
-
 // Per-device answer to "is this a gfx950": 0 unknown, 1 yes, 2 no.
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_arch_ok[kMaxDevices];
 thread_local int g_cur_dev = 0;  // the device check_device() last looked at
+
+thread_local int g_last_hip_error = 0;
+
+}  // namespace
 
 da_status fail_hip(hipError_t e) {
   g_last_hip_error = (int)e;
@@ -45,6 +47,8 @@ da_status check_device() {
   g_cur_dev = dev;
   return st == 1 ? DA_OK : DA_ERR_UNSUPPORTED;
 }
+
+namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 

@@ -147,6 +147,11 @@ int heads_per_block(int G, int waves = kAttnWaves);
 // is a multiple of gamma and at most max_rows; 0 when there is none.
 int fused_heads_per_block(int G, int gamma, int max_rows, int waves = kAttnWaves);
 
+// da_api.cpp: whether the current device is a gfx950, and DA_ERR_HIP with the
+// error kept for da_last_hip_error().
+da_status check_device();
+da_status fail_hip(hipError_t e);
+
 // Kernel launchers (da_kernels.hip).  Each returns the hipError_t of the launch.
 hipError_t launch_sparse(const Args& a, hipStream_t s);
 hipError_t launch_dense(const Args& a, hipStream_t s);

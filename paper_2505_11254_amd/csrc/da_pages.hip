@@ -1,0 +1,459 @@
+// da_pages.hip -- the pages of a key/value cache: forking, resizing with copy on
+// write, appending and compacting (gfx950).
+//
+// A sequence ("slot") owns a row of the page table, whose first entries name its
+// pages; refs[p] counts the slots that name page p.  Every call takes a list of
+// requests and behaves as if they were served in the order of the list, so that
+// tables, lengths and counts come out the same on every run: ranks come from
+// prefix sums over the list, never from the order in which atomics land (they only
+// add to counters).  What bounds these kernels is latency where they touch
+// integers only, and HBM where they move rows (16 bytes per lane, whole rows).
+//
+// Nothing on the device is taken on trust that would lead out of bounds: slots,
+// lengths and page ids are checked before use, and a request that does not fit is
+// refused (its result says so) and leaves its sequence as it was.
+#include "da_device.hpp"
+#include "da_paged.hpp"
+
+namespace da {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ bool page_ok(int e, int P) { return (unsigned)e < (unsigned)P; }
+
+// Whether request i is the first of the list to name slot s (all threads of the
+// workgroup together).
+template <int NT>
+__device__ __forceinline__ bool first_to_name(const int32_t* list, int i, int s) {
+  int seen = 0;
+  for (int j = threadIdx.x; j < i; j += NT) seen |= list[j] == s;
+  return !__syncthreads_or(seen);
+}
+
+__device__ __forceinline__ int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
+
+// The workgroup gives back the pages in entries [c0, c1) of slot s.
+__device__ __forceinline__ void give_back(const Table& t, int s, int c0, int c1) {
+  int32_t* const row = t.table + (int64_t)s * t.M;
+  for (int c = c0 + (int)threadIdx.x; c < c1; c += kThreads) {
+    const int e = row[c];
+    if (page_ok(e, t.P)) atomicSub(t.refs + e, 1);
+    row[c] = -1;
+  }
+}
+
+// One request per workgroup: slot dst shares every page of slot src.
+__global__ __launch_bounds__(kThreads) void fork_kernel(Table t, const int32_t* __restrict__ src,
+                                                       const int32_t* __restrict__ dst, int n,
+                                                       int32_t* __restrict__ result) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int from = src[i], to = dst[i];
+  bool ok = (unsigned)from < (unsigned)t.S && (unsigned)to < (unsigned)t.S;
+  // (a slot that some request fills is no source, whatever their order: its row
+  // is being written)
+  int bad = 0;
+  for (int j = tid; j < n; j += kThreads) bad |= dst[j] == from || (j < i && dst[j] == to);
+  ok = !__syncthreads_or(bad) && ok;
+  if (ok) ok = t.lens[to] == 0 && (t.M == 0 || t.table[(int64_t)to * t.M] < 0);
+  if (!ok) {
+    if (tid == 0) result[i] = -1;
+    return;
+  }
+  const int L = min(max(t.lens[from], 0), t.M * kPage);
+  const int pages = pages_of(L);
+  const int32_t* a = t.table + (int64_t)from * t.M;
+  int32_t* b = t.table + (int64_t)to * t.M;
+  __syncthreads();  // (b[0] was read above, by every thread)
+  for (int c = tid; c < pages; c += kThreads) {
+    const int e = a[c];
+    if (page_ok(e, t.P)) {
+      atomicAdd(t.refs + e, 1);
+      b[c] = e;
+    }
+  }
+  if (tid == 0) {
+    t.lens[to] = L;
+    result[i] = L;
+  }
+}
+
+// Resizing, first launch, one request per workgroup: checks the request and gives
+// back the pages past its new end.  result[i] = {0, or -1: refused; -1; -1; 0} for
+// the launches that follow.
+__global__ __launch_bounds__(kThreads) void release_kernel(Table t, const int32_t* __restrict__ slots,
+                                                          const int32_t* __restrict__ new_lens,
+                                                          int32_t* __restrict__ result) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int s = slots[i];
+  const int want = new_lens ? new_lens[i] : 0;
+  bool ok = (unsigned)s < (unsigned)t.S && want >= 0 && want <= t.M * kPage;
+  ok = first_to_name<kThreads>(slots, i, s) && ok;
+  if (ok) {
+    const int old = min(max(t.lens[s], 0), t.M * kPage);
+    give_back(t, s, pages_of(want), pages_of(old));
+    __syncthreads();  // (every thread has read the old length)
+    if (tid == 0 && want < old) t.lens[s] = want;
+  }
+  if (tid == 0) ((int4*)result)[i] = int4{ok ? 0 : -1, -1, -1, 0};
+}
+
+// Inclusive sum over the threads of a workgroup of NT (at most 1024).
+template <int NT>
+__device__ __forceinline__ int block_scan(int x, int* lds, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    const int y = lds[w];
+    before += w < wave ? y : 0;
+    all += y;
+  }
+  *total = all;
+  return x + before;
+}
+
+// Resizing, second launch, one workgroup: a thread per request that grows finds
+// whether the page holding its last token has to be copied (other slots hold it
+// too) and how many pages it lacks; a prefix sum over the list gives each its
+// ranks among the free pages, which a scan of the reference counts hands out in
+// ascending order.  Of the holders of one page that all grow in this call, as many
+// copy as there are others left: the last one keeps the page.
+constexpr int kPlanThreads = 1024;
+constexpr int kRefsPerThread = 16;
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32_t* __restrict__ slots,
+                                                           const int32_t* __restrict__ new_lens, int n, int32_t* __restrict__ result) {
+  __shared__ int part[kMaxRequests];  // the page a request would write into, or -1
+  __shared__ int cum[kMaxRequests];   // pages that the requests up to this one ask for
+  __shared__ int entry[kMaxRequests];  // the entries it holds
+  __shared__ int copied[kMaxRequests];  // 1: the last of them is copied, before new ones follow
+  __shared__ int scan[kPlanThreads / 64];
+  const int i = threadIdx.x;
+  int4* const r = (int4*)result + i;
+  int s = 0, old = 0, want = 0, pg = -1, holders = 0;
+  const bool valid = i < n && r->x == 0;
+  bool grow = false;
+  if (valid) {
+    s = slots[i];
+    want = new_lens[i];
+    old = min(max(t.lens[s], 0), t.M * kPage);  // (a shorter one has its new length already)
+    grow = want > old;
+    if (grow && old % kPage) {
+      pg = t.table[(int64_t)s * t.M + old / kPage];
+      if (page_ok(pg, t.P)) holders = t.refs[pg];
+      else pg = -1;
+    }
+  }
+  part[i] = pg;
+  int rank = 0;
+  if (__syncthreads_or(holders > 1)) {
+    for (int j = 0; j < n; ++j) rank += j < i && part[j] == pg;
+  }
+  const bool copy = pg >= 0 && holders - rank > 1;
+  const int ask = grow ? (copy ? 1 : 0) + pages_of(want) - pages_of(old) : 0;
+  // (sums are held at the pool's size: one more page than that is refused anyway)
+  int total;
+  int upto = ask;
+  {
+    // a sum of n requests of up to M pages each may pass 31 bits: saturate lane by lane
+    const int lane = i & 63, wave = i >> 6;
+    const int cap = t.P + 1;
+    upto = min(upto, cap);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(upto, d);
+      if (lane >= d) upto = min((int64_t)upto + y, (int64_t)cap);
+    }
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      before += w < wave ? scan[w] : 0;
+      all += scan[w];
+    }
+    upto = (int)min(before + upto, (int64_t)cap);
+    total = (int)min(all, (int64_t)cap);
+    __syncthreads();
+  }
+  cum[i] = upto;
+  entry[i] = pages_of(old);
+  copied[i] = copy;
+
+  // free pages, sixteen counts per thread and step
+  constexpr int kStep = kPlanThreads * kRefsPerThread;
+  auto load = [&](int base) -> unsigned {
+    unsigned bits = 0;
+    const int p0 = base + i * kRefsPerThread;
+#pragma unroll
+    for (int j = 0; j < kRefsPerThread; ++j)
+      if (p0 + j < t.P && t.refs[p0 + j] == 0) bits |= 1u << j;
+    return bits;
+  };
+  int avail = 0;
+  for (int base = 0; base < t.P && avail < total; base += kStep) {
+    int all;
+    block_scan<kPlanThreads>(__popc(load(base)), scan, &all);
+    avail += all;
+  }
+  // Served in order until one does not fit; that one and every later one that
+  // grows are refused.
+  const bool served = grow && upto <= avail;
+  if (i < n) {
+    if (served) {
+      t.lens[s] = want;
+      if (copy) atomicSub(t.refs + pg, 1);
+    }
+    // (of a copy, the source and its rows; its new page follows below)
+    if (valid) *r = int4{grow && !served ? -1 : want, served && copy ? pg : -1, -1, served && copy ? old % kPage : 0};
+  }
+  __syncthreads();
+  int seen = 0;
+  // the pages handed out: those asked for by the requests that are served
+  int granted;
+  {
+    int x = served ? upto : 0;
+    for (int d = 32; d; d /= 2) x = max(x, __shfl_xor(x, d));
+    __syncthreads();
+    if ((i & 63) == 0) scan[i >> 6] = x;
+    __syncthreads();
+    granted = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) granted = max(granted, scan[w]);
+  }
+  for (int base = 0; base < t.P && seen < granted; base += kStep) {
+    const unsigned bits = load(base);
+    int all;
+    int k = seen + block_scan<kPlanThreads>(__popc(bits), scan, &all) - __popc(bits);
+    for (unsigned b = bits; b && k < granted; b &= b - 1, ++k) {
+      const int p = base + i * kRefsPerThread + __ffs(b) - 1;
+      // the request that rank k falls to: the first whose sum exceeds it
+      int lo = 0, hi = n - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (cum[mid] > k) hi = mid;
+        else lo = mid + 1;
+      }
+      const int before = lo ? cum[lo - 1] : 0;
+      int32_t* const row = t.table + (int64_t)slots[lo] * t.M + entry[lo] - copied[lo];
+      row[k - before] = p;
+      if (copied[lo] && k == before) result[4 * lo + 2] = p;
+      t.refs[p] = 1;
+    }
+    seen += all;
+  }
+}
+
+// Third launch: the rows of the copied pages, a workgroup per (request, layer, keys
+// or values, kv head).
+__global__ __launch_bounds__(kThreads) void copy_kernel(Pages p, int P, const int32_t* __restrict__ result,
+                                                       int n) {
+  unsigned b = blockIdx.x;
+  const int i = b % (unsigned)n;
+  b /= (unsigned)n;
+  const int4 r = ((const int4*)result)[i];
+  if (r.y < 0 || r.z < 0) return;
+  const int h = b % (unsigned)p.Hkv;
+  b /= (unsigned)p.Hkv;
+  uint16_t* const base = (b & 1) ? p.v : p.k;
+  const int64_t layer = b >> 1;
+  const int64_t head = (int64_t)kPage * p.d;
+  const u32x4* const from = (const u32x4*)(base + ((layer * P + r.y) * p.Hkv + h) * head);
+  u32x4* const to = (u32x4*)(base + ((layer * P + r.z) * p.Hkv + h) * head);
+  const int chunks = r.w * (p.d / 8);
+  for (int c = threadIdx.x; c < chunks; c += kThreads) to[c] = from[c];
+}
+
+// New tokens become the last ones of their sequences: each thread moves 16 bytes
+// of keys or values.  A workgroup takes kAppendChunks of one sequence.
+constexpr int kAppendPer = 4;
+constexpr int kAppendChunks = kThreads * kAppendPer;
+__global__ __launch_bounds__(kThreads) void append_kernel(Table t, Pages p, const uint16_t* __restrict__ k,
+                                                         const uint16_t* __restrict__ v, int64_t T,
+                                                         const int32_t* __restrict__ slots,
+                                                         const int32_t* __restrict__ cu, int B, int N) {
+  const int b = blockIdx.x % (unsigned)B;
+  const unsigned part = blockIdx.x / (unsigned)B;
+  const int64_t layer = blockIdx.y >> 1;
+  const uint16_t* const src = ((blockIdx.y & 1) ? v : k) + layer * T * p.Hkv * p.d;
+  uint16_t* const dst = ((blockIdx.y & 1) ? p.v : p.k) + layer * t.P * p.Hkv * (int64_t)kPage * p.d;
+  const int64_t base = cu ? cu[b] : (int64_t)b * N;
+  const int m = min(cu ? cu[b + 1] - cu[b] : N, N);
+  const int s = slots ? slots[b] : b;
+  if ((unsigned)s >= (unsigned)t.S || base < 0 || base + m > T) return;
+  const int per_head = p.d / 8;
+  const int row = p.Hkv * per_head;  // chunks per token
+  const unsigned chunks = (unsigned)m * row;  // (the host has checked that N tokens' fit)
+  const int pos0 = t.lens[s] - m;
+#pragma unroll
+  for (int j = 0; j < kAppendPer; ++j) {
+    const unsigned c = part * kAppendChunks + j * kThreads + threadIdx.x;
+    if (c >= chunks) break;
+    const int i = c / (unsigned)row, w = c % (unsigned)row;
+    const int pos = pos0 + i;
+    if (pos < 0 || pos >= t.M * kPage) continue;
+    const int e = t.table[(int64_t)s * t.M + pos / kPage];
+    if (!page_ok(e, t.P)) continue;
+    const u32x4 x = *(const u32x4*)(src + (base + i) * (int64_t)p.Hkv * p.d + w * 8);
+    const int h = w / per_head, q = w % per_head;
+    *(u32x4*)(dst + (((int64_t)e * p.Hkv + h) * kPage + pos % kPage) * p.d + q * 8) = x;
+  }
+}
+
+// Compacting, first launch, one request per workgroup: checks the kept places
+// (ascending, inside the sequence, no shared page to be written) and sets the new
+// length.  result[i] = {tokens kept, or -1: refused; the first that moves; the old
+// length; 0}.
+__global__ __launch_bounds__(kThreads) void compact_check_kernel(
+    Table t, const int32_t* __restrict__ slots, const int32_t* __restrict__ start,
+    const int32_t* __restrict__ keep, int64_t n_keep, const int32_t* __restrict__ cu_keep,
+    int32_t* __restrict__ result) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int s = slots[i], st = start[i];
+  const int64_t k0 = cu_keep[i], k1 = cu_keep[i + 1];
+  int4* const r = (int4*)result + i;
+  bool ok = (unsigned)s < (unsigned)t.S && st >= 0 && k0 >= 0 && k1 >= k0 && k1 <= n_keep;
+  ok = first_to_name<kThreads>(slots, i, s) && ok;
+  int len = 0;
+  if (ok) {
+    len = min(max(t.lens[s], 0), t.M * kPage);
+    ok = st <= len && k1 - k0 <= len - st;
+  }
+  if (!ok) {
+    if (tid == 0) *r = int4{-1, 0, 0, 0};
+    return;
+  }
+  const int m = (int)(k1 - k0);
+  int bad = 0, moved = m;  // the first place of this thread's that moves
+  for (int j = tid; j < m; j += kThreads) {
+    const int x = keep[k0 + j];
+    bad |= x < j || x >= len - st || (j > 0 && keep[k0 + j - 1] >= x);
+    if (x != j) moved = min(moved, j);
+  }
+  __shared__ int least;
+  if (tid == 0) least = m;
+  bad = __syncthreads_or(bad);
+  if (!bad && moved < m) atomicMin(&least, moved);
+  __syncthreads();
+  const int j0 = least;
+  if (!bad && j0 < m) {
+    const int32_t* row = t.table + (int64_t)s * t.M;
+    for (int c = (st + j0) / kPage + tid; c <= (st + m - 1) / kPage; c += kThreads) {
+      const int e = row[c];
+      bad |= !page_ok(e, t.P) || t.refs[e] > 1;
+    }
+  }
+  bad = __syncthreads_or(bad);
+  if (tid == 0) {
+    *r = bad ? int4{-1, 0, 0, 0} : int4{m, j0, len, 0};
+    if (!bad) t.lens[s] = st + m;
+  }
+}
+
+// Second launch: a workgroup per (request, layer, keys or values, kv head) moves
+// its rows up, 64 at a time.  Kept places ascend, so a row never moves down and a
+// batch's rows are all read before any of them, or of a later batch's sources, can
+// be written over.
+constexpr int kMoveRows = 64;
+__global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, const int32_t* __restrict__ slots,
+                                                          const int32_t* __restrict__ start,
+                                                          const int32_t* __restrict__ keep,
+                                                          const int32_t* __restrict__ cu_keep, int n,
+                                                          const int32_t* __restrict__ result) {
+  unsigned b = blockIdx.x;
+  const int i = b % (unsigned)n;
+  b /= (unsigned)n;
+  const int4 r = ((const int4*)result)[i];
+  if (r.x <= r.y) return;  // refused (-1), or nothing moves
+  const int h = b % (unsigned)p.Hkv;
+  b /= (unsigned)p.Hkv;
+  const int64_t layer = b >> 1;
+  uint16_t* const base = ((b & 1) ? p.v : p.k) + (layer * t.P * p.Hkv + h) * (int64_t)kPage * p.d;
+  const int64_t page = (int64_t)p.Hkv * kPage * p.d;
+  const int32_t* row = t.table + (int64_t)slots[i] * t.M;
+  const int st = start[i];
+  const int32_t* kp = keep + cu_keep[i];
+  const int per = p.d / 8;             // 16-byte chunks per row
+  const int rows = kThreads / per;     // rows per step of the workgroup
+  const int j_in = threadIdx.x / per, c = threadIdx.x % per;
+  constexpr int kMax = kMoveRows / 16;  // (d = 128: 16 rows per step, d = 64: 32)
+  for (int j0 = r.y; j0 < r.x; j0 += kMoveRows) {
+    u32x4 x[kMax];
+#pragma unroll
+    for (int u = 0; u < kMax; ++u) {
+      const int j = j0 + u * rows + j_in;
+      if (u * rows >= kMoveRows || j >= r.x) continue;
+      const int pos = st + kp[j];
+      const int e = row[pos / kPage];
+      x[u] = page_ok(e, t.P) ? *(const u32x4*)(base + e * page + (pos % kPage) * p.d + c * 8) : u32x4{};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMax; ++u) {
+      const int j = j0 + u * rows + j_in;
+      if (u * rows >= kMoveRows || j >= r.x) continue;
+      const int pos = st + j;
+      const int e = row[pos / kPage];
+      *(u32x4*)(base + e * page + (pos % kPage) * p.d + c * 8) = x[u];
+    }
+    __syncthreads();
+  }
+}
+
+// Third launch: the pages past the new ends are given back.
+__global__ __launch_bounds__(kThreads) void trim_kernel(Table t, const int32_t* __restrict__ slots,
+                                                       const int32_t* __restrict__ start,
+                                                       const int32_t* __restrict__ result) {
+  const int i = blockIdx.x;
+  const int4 r = ((const int4*)result)[i];
+  if (r.x >= 0) give_back(t, slots[i], pages_of(start[i] + r.x), pages_of(r.z));
+}
+
+}  // namespace
+
+hipError_t launch_pages_fork(const Table& t, const int32_t* src, const int32_t* dst, int n,
+                             int32_t* result, hipStream_t s) {
+  hipLaunchKernelGGL(fork_kernel, dim3(n), dim3(kThreads), 0, s, t, src, dst, n, result);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_resize(const Table& t, const Pages& p, const int32_t* slots,
+                               const int32_t* new_lens, int n, int32_t* result, hipStream_t s) {
+  hipLaunchKernelGGL(release_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, new_lens, result);
+  if (new_lens) {
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, t, slots, new_lens, n,
+                       result);
+    hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, p,
+                       t.P, result, n);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_append(const Table& t, const Pages& p, const uint16_t* k,
+                               const uint16_t* v, int64_t T, const int32_t* slots,
+                               const int32_t* cu, int B, int N, hipStream_t s) {
+  const int64_t chunks = (int64_t)N * p.Hkv * (p.d / 8);
+  const int64_t parts = (chunks + kAppendChunks - 1) / kAppendChunks;
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)(parts * B), p.layers * 2), dim3(kThreads), 0, s, t, p, k,
+                     v, T, slots, cu, B, N);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const Table& t, const Pages& p, const int32_t* slots,
+                                const int32_t* start, const int32_t* keep, int64_t n_keep,
+                                const int32_t* cu_keep, int n, int32_t* result, hipStream_t s) {
+  hipLaunchKernelGGL(compact_check_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, start, keep, n_keep,
+                     cu_keep, result);
+  hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, t, p,
+                     slots, start, keep, cu_keep, n, result);
+  hipLaunchKernelGGL(trim_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, start, result);
+  return hipGetLastError();
+}
+
+}  // namespace da
