@@ -11,6 +11,7 @@ A fixed-length batch passes ``B`` (T = B * N); a ragged batch passes
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -440,68 +441,77 @@ PAGE_TOKENS = 64
 class _On:
     """The device of a call and its stream: sets the device where another is current, and takes
     new tensors from that stream's memory."""
+    __slots__ = ("dev", "raw", "stream", "other")
 
     def __init__(self, dev, stream):
         if dev.type != "cuda":
             raise ValueError(f"tensors must be on a GPU (got {dev})")
         self.dev = dev
-        self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
-        self.other = (dev.index if dev.index is not None else 0) != torch.cuda.current_device()
-        self.aside = stream is not None
+        self.stream = stream
+        self.raw = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+        self.other = dev.index != torch._C._cuda_getDevice()
 
     def call(self, name, *args):
         if self.other:
             with torch.cuda.device(self.dev):
-                _call(name, *args, self.stream.cuda_stream)
+                _call(name, *args, self.raw)
         else:
-            _call(name, *args, self.stream.cuda_stream)
+            _call(name, *args, self.raw)
 
     def empty(self, shape, dtype):
-        if not self.aside:
+        if self.stream is None:
             return torch.empty(shape, dtype=dtype, device=self.dev)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.dev)
 
     def workspace(self, given, nbytes):
-        """(pointer, size) of the caller's workspace or of one that lasts for this call."""
+        """(tensor, address, size) of the caller's workspace, or of one that lasts for this call."""
         if given is None:
             if not nbytes:
                 return None, None, 0
             given = self.empty(nbytes, torch.uint8)
-        else:
-            _on_device("workspace", given, self.dev, None)
+            return given, given.data_ptr(), nbytes
+        _on_device("workspace", given, self.dev, None)
         return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 def _ints(name, t, dev, shape=None):
-    _on_device(name, t, dev, torch.int32)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    """t is a contiguous int32 tensor on `dev`, of `shape` if given."""
+    if t.dtype is not torch.int32 or t.device != dev or not t.is_contiguous():
+        _on_device(name, t, dev, torch.int32)
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
 
 
 def _table(table, lens, dev):
     _ints("table", table, dev)
-    if table.dim() != 2:
+    shape = table.shape
+    if len(shape) != 2:
         raise ValueError("table must be [S, M]")
-    _ints("lens", lens, dev, (table.shape[0],))
-    return table.shape
+    _ints("lens", lens, dev, shape[:1])
+    return shape
+
+
+def _halves(name, t, dev):
+    """t is a contiguous bf16 tensor on `dev`."""
+    if t.dtype is not torch.bfloat16 or t.device != dev or not t.is_contiguous():
+        _on_device(name, t, dev, torch.bfloat16)
 
 
 def _pages(k_pages, v_pages, layered=False):
     """(dev, layers, P, Hkv, d) of a cache's pages."""
-    dev = k_pages.device
-    _on_device("k_pages", k_pages, dev, torch.bfloat16)
+    dev, shape = k_pages.device, k_pages.shape
+    _halves("k_pages", k_pages, dev)
     if v_pages is not None:
-        _on_device("v_pages", v_pages, dev, torch.bfloat16)
-        if v_pages.shape != k_pages.shape:
+        _halves("v_pages", v_pages, dev)
+        if v_pages.shape != shape:
             raise ValueError("k_pages and v_pages must have the same shape")
-    n = k_pages.dim()
+    n = len(shape)
     if n != 4 and not (layered and n == 5):
         raise ValueError("pages must be [P, Hkv, 64, d]" + (" or [layers, P, Hkv, 64, d]" if layered else ""))
-    if k_pages.shape[-2] != PAGE_TOKENS:
+    if shape[-2] != PAGE_TOKENS:
         raise ValueError(f"pages must hold {PAGE_TOKENS} tokens")
-    P, Hkv, _, d = k_pages.shape[-4:]
-    return dev, (k_pages.shape[0] if n == 5 else 1), P, Hkv, d
+    return dev, (shape[0] if n == 5 else 1), shape[-4], shape[-3], shape[-1]
 
 
 def _slots(slots, B, S, dev):
@@ -521,14 +531,14 @@ def _new_rows(T, B, cu_seqlens, max_seqlen, dev):
             raise ValueError("the number of rows must be a multiple of B for a fixed-length batch")
         return B, T // B
     _ints("cu_seqlens", cu_seqlens, dev)
-    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
         raise ValueError("cu_seqlens must be 1-D with B + 1 >= 2 entries")
     if max_seqlen is None:
         raise ValueError("max_seqlen is required with cu_seqlens")
-    return cu_seqlens.numel() - 1, int(max_seqlen)
+    return cu_seqlens.shape[0] - 1, int(max_seqlen)
 
 
-def _requests(n, result, shape, on):
+def _requests(result, shape, on):
     if result is None:
         return on.empty(shape, torch.int32)
     _ints("result", result, on.dev, shape)
@@ -540,11 +550,11 @@ def pages_fork(table, lens, refs, src, dst, *, result=None, stream=None):
     int32 [n]: the lengths, -1 where a request was refused (da_pages_fork)."""
     on = _On(table.device, stream)
     S, M = _table(table, lens, on.dev)
-    _ints("refs", refs, on.dev, (refs.numel(),))
+    _ints("refs", refs, on.dev)
     n = src.numel()
     _ints("src", src, on.dev, (n,))
     _ints("dst", dst, on.dev, (n,))
-    result = _requests(n, result, (n,), on)
+    result = _requests(result, (n,), on)
     on.call("da_pages_fork", _ptr(table), _ptr(lens), _ptr(refs), S, M, refs.numel(), _ptr(src), _ptr(dst), n,
             _ptr(result))
     return result
@@ -562,7 +572,7 @@ def pages_resize(k_pages, v_pages, table, lens, refs, slots, new_lens=None, *, r
     _ints("slots", slots, dev, (n,))
     if new_lens is not None:
         _ints("new_lens", new_lens, dev, (n,))
-    result = _requests(n, result, (n, 4), on)
+    result = _requests(result, (n, 4), on)
     on.call("da_pages_resize", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
             P, _ptr(slots), _ptr(new_lens), n, _ptr(result))
     return result
@@ -575,10 +585,10 @@ def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_
     dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
-    for name, t in (("k", k), ("v", v)):
-        _on_device(name, t, dev, torch.bfloat16)
-        if t.dim() != k_pages.dim() - 1 or t.shape[-2:] != (Hkv, d) or (t.dim() == 4 and t.shape[0] != layers):
-            raise ValueError(f"{name} must be [T, Hkv, d] for pages of one layer, [layers, T, Hkv, d] for more")
+    _halves("k", k, dev)
+    _halves("v", v, dev)
+    if k.dim() != k_pages.dim() - 1 or k.shape[-2:] != (Hkv, d) or (k.dim() == 4 and k.shape[0] != layers):
+        raise ValueError("k must be [T, Hkv, d] for pages of one layer, [layers, T, Hkv, d] for more")
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
     T = k.shape[-3]
@@ -600,7 +610,7 @@ def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_ke
     _ints("start", start, dev, (n,))
     _ints("keep", keep, dev, (keep.numel(),))
     _ints("cu_keep", cu_keep, dev, (n + 1,))
-    result = _requests(n, result, (n, 4), on)
+    result = _requests(result, (n, 4), on)
     if not keep.numel():  # (an empty tensor has no address; no place is read)
         keep = cu_keep
         n_keep = 0
@@ -612,13 +622,13 @@ def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_ke
 
 
 def _queries(q, out, lse, Hkv, d, on):
-    _on_device("q", q, on.dev, torch.bfloat16)
+    _halves("q", q, on.dev)
     if q.dim() != 3 or q.shape[2] != d or q.shape[1] % Hkv:
         raise ValueError(f"q must be [T, Hq, {d}] with Hq a multiple of {Hkv}")
     if out is None:
         out = on.empty(q.shape, torch.bfloat16)
     else:
-        _on_device("out", out, on.dev, torch.bfloat16)
+        _halves("out", out, on.dev)
         if out.shape != q.shape:
             raise ValueError(f"out must have the shape of q {tuple(q.shape)}")
         o0, o1 = _span(out)
@@ -632,6 +642,7 @@ def _queries(q, out, lse, Hkv, d, on):
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k=0) -> int:
     """Workspace of tree_attn_paged, or with top_k of selected_attn_paged (da_paged_workspace_bytes)."""
     return int(load_library().da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k))

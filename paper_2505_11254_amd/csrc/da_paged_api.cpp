@@ -53,7 +53,7 @@ constexpr int kMaxPartPages = 1024;  // page ids a workgroup holds
 da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
   const int G = Hq / Hkv;
   const int64_t rows = n_list ? G : (int64_t)N * G;
-  p->row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 ? 4 : 8;
+  p->row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
   p->n_rowgroups = (int)((rows + 32 * p->row_tiles - 1) / (32 * p->row_tiles));
   const int64_t groups = (n_list ? (int64_t)B * N : B) * Hkv;
   if (n_list) pages = n_list + 1;

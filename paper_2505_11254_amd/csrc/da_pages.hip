@@ -33,10 +33,16 @@ __device__ __forceinline__ bool first_to_name(const int32_t* list, int i, int s)
 
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
 
-// The workgroup gives back the pages in entries [c0, c1) of slot s.
-__device__ __forceinline__ void give_back(const Table& t, int s, int c0, int c1) {
+// A count that atomics of this kernel may have changed (they act past the L1 cache).
+__device__ __forceinline__ int load_count(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Thread i of n gives back its share of the pages in entries [c0, c1) of slot s.
+__device__ __forceinline__ void give_back(const Table& t, int s, int c0, int c1, int i = threadIdx.x,
+                                          int n = kThreads) {
   int32_t* const row = t.table + (int64_t)s * t.M;
-  for (int c = c0 + (int)threadIdx.x; c < c1; c += kThreads) {
+  for (int c = c0 + i; c < c1; c += n) {
     const int e = row[c];
     if (page_ok(e, t.P)) atomicSub(t.refs + e, 1);
     row[c] = -1;
@@ -78,22 +84,18 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(Table t, const int32_t* 
   }
 }
 
-// Resizing, first launch, one request per workgroup: checks the request and gives
-// back the pages past its new end.  result[i] = {0, or -1: refused; -1; -1; 0} for
-// the launches that follow.
-__global__ __launch_bounds__(kThreads) void release_kernel(Table t, const int32_t* __restrict__ slots,
-                                                          const int32_t* __restrict__ new_lens,
-                                                          int32_t* __restrict__ result) {
+// Freeing, one request per workgroup.
+__global__ __launch_bounds__(kThreads) void free_kernel(Table t, const int32_t* __restrict__ slots,
+                                                       int32_t* __restrict__ result) {
   const int i = blockIdx.x, tid = threadIdx.x;
   const int s = slots[i];
-  const int want = new_lens ? new_lens[i] : 0;
-  bool ok = (unsigned)s < (unsigned)t.S && want >= 0 && want <= t.M * kPage;
+  bool ok = (unsigned)s < (unsigned)t.S;
   ok = first_to_name<kThreads>(slots, i, s) && ok;
   if (ok) {
     const int old = min(max(t.lens[s], 0), t.M * kPage);
-    give_back(t, s, pages_of(want), pages_of(old));
+    give_back(t, s, 0, pages_of(old));
     __syncthreads();  // (every thread has read the old length)
-    if (tid == 0 && want < old) t.lens[s] = want;
+    if (tid == 0) t.lens[s] = 0;
   }
   if (tid == 0) ((int4*)result)[i] = int4{ok ? 0 : -1, -1, -1, 0};
 }
@@ -121,36 +123,60 @@ __device__ __forceinline__ int block_scan(int x, int* lds, int* total) {
   return x + before;
 }
 
-// Resizing, second launch, one workgroup: a thread per request that grows finds
-// whether the page holding its last token has to be copied (other slots hold it
-// too) and how many pages it lacks; a prefix sum over the list gives each its
-// ranks among the free pages, which a scan of the reference counts hands out in
+// Resizing, one workgroup, a thread per request.  Slots that shrink give back their
+// pages first: a thread its own few, the waves those of longer rests.  A thread whose
+// slot grows then finds whether the page holding its last token has to be copied (other
+// slots hold it too) and how many pages it lacks; a prefix sum over the list gives each
+// its ranks among the free pages, which a scan of the reference counts hands out in
 // ascending order.  Of the holders of one page that all grow in this call, as many
 // copy as there are others left: the last one keeps the page.
 constexpr int kPlanThreads = 1024;
 constexpr int kRefsPerThread = 16;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32_t* __restrict__ slots,
                                                            const int32_t* __restrict__ new_lens, int n, int32_t* __restrict__ result) {
-  __shared__ int part[kMaxRequests];  // the page a request would write into, or -1
-  __shared__ int cum[kMaxRequests];   // pages that the requests up to this one ask for
+  __shared__ int named[kMaxRequests];  // the slots of the requests
+  __shared__ int part[kMaxRequests];   // the page a request would write into, or -1
+  __shared__ int cum[kMaxRequests];    // pages that the requests up to this one ask for
   __shared__ int entry[kMaxRequests];  // the entries it holds
   __shared__ int copied[kMaxRequests];  // 1: the last of them is copied, before new ones follow
   __shared__ int scan[kPlanThreads / 64];
   const int i = threadIdx.x;
   int4* const r = (int4*)result + i;
-  int s = 0, old = 0, want = 0, pg = -1, holders = 0;
-  const bool valid = i < n && r->x == 0;
-  bool grow = false;
-  if (valid) {
+  int s = -1, old = 0, want = -1, pg = -1, holders = 0;
+  if (i < n) {
     s = slots[i];
     want = new_lens[i];
-    old = min(max(t.lens[s], 0), t.M * kPage);  // (a shorter one has its new length already)
-    grow = want > old;
-    if (grow && old % kPage) {
-      pg = t.table[(int64_t)s * t.M + old / kPage];
-      if (page_ok(pg, t.P)) holders = t.refs[pg];
-      else pg = -1;
-    }
+  }
+  named[i] = s;
+  bool valid = (unsigned)s < (unsigned)t.S && want >= 0 && want <= t.M * kPage;
+  if (valid) old = min(max(t.lens[s], 0), t.M * kPage);
+  __syncthreads();
+  for (int j = 0; j < n; ++j) valid &= !(j < i && named[j] == s);
+  if (i < n && !valid) *r = int4{-1, -1, -1, 0};
+
+  // ---- shrinking
+  const bool shrink = valid && want < old;
+  if (__syncthreads_or(shrink)) {
+    constexpr int kOwn = 4;  // pages that a thread gives back itself
+    const int c0 = pages_of(want), c1 = pages_of(old);
+    if (shrink) t.lens[s] = want;
+    if (shrink && c1 - c0 <= kOwn) give_back(t, s, c0, c1, 0, 1);
+    entry[i] = c0;
+    cum[i] = shrink && c1 - c0 > kOwn ? c1 : 0;
+    __syncthreads();
+    for (int j = i >> 6; j < n; j += kPlanThreads / 64)
+      if (cum[j]) give_back(t, named[j], entry[j], cum[j], i & 63, 64);
+    // (counts given back are counts handed out below: by atomics, past this L1)
+    __threadfence();
+    __syncthreads();
+  }
+
+  // ---- growing
+  const bool grow = valid && want > old;
+  if (grow && old % kPage) {
+    pg = t.table[(int64_t)s * t.M + old / kPage];
+    if (page_ok(pg, t.P)) holders = load_count(t.refs + pg);
+    else pg = -1;
   }
   part[i] = pg;
   int rank = 0;
@@ -189,16 +215,27 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
 
   // free pages, sixteen counts per thread and step
   constexpr int kStep = kPlanThreads * kRefsPerThread;
-  auto load = [&](int base) -> unsigned {
+  // (plain loads: no count that is 0 or becomes 0 above can be in the L1 cache yet, and
+  // below none becomes 0)
+  auto load = [&](int64_t base) -> unsigned {
+    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
     unsigned bits = 0;
-    const int p0 = base + i * kRefsPerThread;
+    const int64_t p0 = base + i * kRefsPerThread;
+    if (p0 + kRefsPerThread <= t.P) {
 #pragma unroll
-    for (int j = 0; j < kRefsPerThread; ++j)
-      if (p0 + j < t.P && t.refs[p0 + j] == 0) bits |= 1u << j;
+      for (int j = 0; j < kRefsPerThread; j += 4) {
+        const i32x4u x = *(const i32x4u*)(t.refs + p0 + j);
+        bits |= (unsigned)(x[0] == 0) << j | (unsigned)(x[1] == 0) << (j + 1) | (unsigned)(x[2] == 0) << (j + 2) |
+                (unsigned)(x[3] == 0) << (j + 3);
+      }
+    } else {
+      for (int j = 0; j < kRefsPerThread; ++j)
+        if (p0 + j < t.P && t.refs[p0 + j] == 0) bits |= 1u << j;
+    }
     return bits;
   };
   int avail = 0;
-  for (int base = 0; base < t.P && avail < total; base += kStep) {
+  for (int64_t base = 0; base < t.P && avail < total; base += kStep) {
     int all;
     block_scan<kPlanThreads>(__popc(load(base)), scan, &all);
     avail += all;
@@ -227,12 +264,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
     granted = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) granted = max(granted, scan[w]);
   }
-  for (int base = 0; base < t.P && seen < granted; base += kStep) {
+  for (int64_t base = 0; base < t.P && seen < granted; base += kStep) {
     const unsigned bits = load(base);
     int all;
     int k = seen + block_scan<kPlanThreads>(__popc(bits), scan, &all) - __popc(bits);
     for (unsigned b = bits; b && k < granted; b &= b - 1, ++k) {
-      const int p = base + i * kRefsPerThread + __ffs(b) - 1;
+      const int p = (int)base + i * kRefsPerThread + __ffs(b) - 1;
       // the request that rank k falls to: the first whose sum exceeds it
       int lo = 0, hi = n - 1;
       while (lo < hi) {
@@ -250,7 +287,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   }
 }
 
-// Third launch: the rows of the copied pages, a workgroup per (request, layer, keys
+// Second launch: the rows of the copied pages, a workgroup per (request, layer, keys
 // or values, kv head).
 __global__ __launch_bounds__(kThreads) void copy_kernel(Pages p, int P, const int32_t* __restrict__ result,
                                                        int n) {
@@ -365,12 +402,12 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, con
                                                           const int32_t* __restrict__ start,
                                                           const int32_t* __restrict__ keep,
                                                           const int32_t* __restrict__ cu_keep, int n,
-                                                          const int32_t* __restrict__ result) {
+                                                          int32_t* __restrict__ result) {
   unsigned b = blockIdx.x;
   const int i = b % (unsigned)n;
   b /= (unsigned)n;
   const int4 r = ((const int4*)result)[i];
-  if (r.x <= r.y) return;  // refused (-1), or nothing moves
+  if (r.x < 0) return;  // refused
   const int h = b % (unsigned)p.Hkv;
   b /= (unsigned)p.Hkv;
   const int64_t layer = b >> 1;
@@ -404,15 +441,15 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, con
     }
     __syncthreads();
   }
-}
-
-// Third launch: the pages past the new ends are given back.
-__global__ __launch_bounds__(kThreads) void trim_kernel(Table t, const int32_t* __restrict__ slots,
-                                                       const int32_t* __restrict__ start,
-                                                       const int32_t* __restrict__ result) {
-  const int i = blockIdx.x;
-  const int4 r = ((const int4*)result)[i];
-  if (r.x >= 0) give_back(t, slots[i], pages_of(start[i] + r.x), pages_of(r.z));
+  // The last of a request's workgroups, which all have read the table by then, gives
+  // back the pages past the new end (result[i].w counts them from 0).
+  const int c0 = pages_of(st + r.x), c1 = pages_of(r.z);
+  if (c0 >= c1) return;
+  __shared__ int left;
+  __syncthreads();
+  if (threadIdx.x == 0) left = p.layers * 2 * p.Hkv - 1 - atomicAdd(result + 4 * i + 3, 1);
+  __syncthreads();
+  if (left == 0) give_back(t, slots[i], c0, c1);
 }
 
 }  // namespace
@@ -425,13 +462,13 @@ hipError_t launch_pages_fork(const Table& t, const int32_t* src, const int32_t* 
 
 hipError_t launch_pages_resize(const Table& t, const Pages& p, const int32_t* slots,
                                const int32_t* new_lens, int n, int32_t* result, hipStream_t s) {
-  hipLaunchKernelGGL(release_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, new_lens, result);
-  if (new_lens) {
-    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, t, slots, new_lens, n,
-                       result);
-    hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, p,
-                       t.P, result, n);
+  if (!new_lens) {
+    hipLaunchKernelGGL(free_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, result);
+    return hipGetLastError();
   }
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, t, slots, new_lens, n, result);
+  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, p, t.P,
+                     result, n);
   return hipGetLastError();
 }
 
@@ -452,7 +489,6 @@ hipError_t launch_pages_compact(const Table& t, const Pages& p, const int32_t* s
                      cu_keep, result);
   hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, t, p,
                      slots, start, keep, cu_keep, n, result);
-  hipLaunchKernelGGL(trim_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, start, result);
   return hipGetLastError();
 }
 

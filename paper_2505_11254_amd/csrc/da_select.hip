@@ -110,83 +110,130 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
 
 // ------------------------------------------------------------------- top_k
 //
-// The top_k of n keys by value, ties to the lowest index, found by their bits: four
-// rounds fix eight bits each of the smallest chosen key from a histogram of the
-// keys that share the bits above.  Then one pass ranks the chosen ones in
+// The top_k of n keys by value, ties to the lowest index.  Rounds narrow the range of
+// values that holds the smallest chosen one: its keys' least and greatest value, a
+// histogram of kBins equal steps between them (in LDS, by atomics; steps of a range
+// that fits the keys spread them, where their leading bits alone would pile them up on
+// few counters), and the step that the count from above ends in.  32-bit keys need
+// at most three rounds of 2048 steps, scores two or three.  Then one pass ranks the chosen ones in
 // ascending order: stripes of NT keys, each wave's counts in a table, a prefix sum
-// over (stripe, wave).  emit(rank, index) is called once per chosen key.
-template <int NT>
+// over (stripe, wave).  Thread tid owns keys tid, tid + NT, ...; each(f) calls
+// f(stripe, index, key) for those of all stripes, index >= n where there is none.
+// emit(rank, index) is called once per chosen key.
+constexpr uint32_t kForced = 0xffffffffu;  // always chosen (never more than top_k are)
+constexpr uint32_t kAbsent = 0u;           // chosen last
+
+template <int NT, int MAX>
 struct TopK {
   static constexpr int kWaves = NT / 64;
-  static constexpr int kMaxStripes = (NT == 1024 ? kMaxCandPages : kMaxCandBlocks) / NT;
-  int hist[256];
+  static constexpr int kBins = 2 * NT;
+  static constexpr int kMaxStripes = (MAX + NT - 1) / NT;
+  int hist[kBins];
   int table[2][kMaxStripes * kWaves];
-  int scan[2][kWaves];
-  uint32_t prefix;
+  int scan[3][kWaves];
+  uint32_t ends[2][kWaves];
+  uint32_t bin;
   int need;
 };
 
-template <int NT, typename Emit>
-__device__ __forceinline__ void select_top(TopK<NT>& t, const uint32_t* keys, int n, int top_k,
-                                           Emit emit) {
+template <int NT, int MAX, typename Each, typename Emit>
+__device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, Each each, Emit emit) {
+  using TK = TopK<NT, MAX>;
+  constexpr int W = TK::kWaves;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  constexpr int W = NT / 64;
   if (n <= top_k) {
     for (int i = tid; i < n; i += NT) emit(i, i);
     return;
   }
-  uint32_t prefix = 0, mask = 0;
-  int need = top_k;  // of the keys that share the prefix, this many are chosen
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += NT) t.hist[i] = 0;
+  // members: keys in [lo, hi]; `need` of them are chosen, and every key above
+  uint32_t lo = 1, hi = kForced - 1;
+  int need = top_k;
+  for (bool first = true;; first = false) {
+    uint32_t mn = ~0u, mx = 0;
+    int forced = 0, members = 0;
+    each([&](int, int i, uint32_t x) {
+      if (i >= n) return;
+      const bool in = x >= lo && x <= hi;
+      mn = in ? min(mn, x) : mn;
+      mx = in ? max(mx, x) : mx;
+      members += in;
+      forced += x == kForced;
+    });
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      mn = min(mn, (uint32_t)__shfl_xor((int)mn, d));
+      mx = max(mx, (uint32_t)__shfl_xor((int)mx, d));
+      members += __shfl_xor(members, d);
+      forced += __shfl_xor(forced, d);
+    }
+    if (lane == 0) {
+      t.ends[0][wave] = mn;
+      t.ends[1][wave] = mx;
+      t.scan[0][wave] = members;
+      t.scan[1][wave] = forced;
+    }
+    t.hist[tid] = t.hist[NT + tid] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += NT) {
-      const uint32_t x = keys[i];
-      if ((x & mask) == prefix) atomicAdd(&t.hist[(x >> shift) & 255], 1);
+    members = forced = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      mn = min(mn, t.ends[0][w]);
+      mx = max(mx, t.ends[1][w]);
+      members += t.scan[0][w];
+      forced += t.scan[1][w];
+    }
+    if (first) {
+      if (forced >= need) {  // (scores past the range of floats count as forced: the first of them)
+        lo = kForced;
+        break;
+      }
+      need -= forced;
+      if (members < need) {  // all of them, and the first absent ones
+        lo = kAbsent;
+        need -= members;
+        break;
+      }
+    }
+    const int bits = 32 - __clz((int)(mx - mn));  // 0 for a single value
+    const int sh = max(0, bits - (31 - __clz(TK::kBins)));
+    each([&](int, int i, uint32_t x) {
+      if (i < n && x >= lo && x <= hi) atomicAdd(&t.hist[(x - mn) >> sh], 1);
+    });
+    __syncthreads();
+    // thread tid holds the steps kBins-1 - 2 tid and the one below, the highest first
+    const int c0 = t.hist[TK::kBins - 1 - 2 * tid], c1 = t.hist[TK::kBins - 2 - 2 * tid];
+    int upto = c0 + c1;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 63) t.scan[2][wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += t.scan[2][w];
+    const int before = upto - c0 - c1;
+    if (before < need && upto >= need) {
+      const bool second = before + c0 < need;
+      t.bin = TK::kBins - 1 - 2 * tid - (second ? 1 : 0);
+      t.need = need - before - (second ? c0 : 0);
     }
     __syncthreads();
-    if (wave == 0) {
-      // lane l holds digits 255-4l .. 252-4l, the highest first
-      int c[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j] = t.hist[255 - 4 * lane - j];
-      int upto = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(upto, d);
-        if (lane >= d) upto += y;
-      }
-      int before = upto - sum;
-      if (before < need && upto >= need) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (before < need && before + c[j] >= need) {
-            t.prefix = prefix | (uint32_t)(255 - 4 * lane - j) << shift;
-            t.need = need - before;
-          }
-          before += c[j];
-        }
-      }
-    }
-    __syncthreads();
-    prefix = t.prefix;
     need = t.need;
-    mask |= 255u << shift;
+    lo = mn + (t.bin << sh);
+    if (sh == 0) break;
+    hi = lo + min(mx - lo, (1u << sh) - 1u);
   }
-  // keys above `prefix` are chosen, and the first `need` equal to it
-  const int stripes = (n + NT - 1) / NT;
-  for (int s = 0; s < stripes; ++s) {
-    const int i = s * NT + tid;
-    const uint32_t x = i < n ? keys[i] : 0;
-    const uint64_t above = __ballot(i < n && x > prefix), same = __ballot(i < n && x == prefix);
+  // keys above lo are chosen, and the first `need` equal to it
+  each([&](int s, int i, uint32_t x) {
+    const uint64_t above = __ballot(i < n && x > lo), same = __ballot(i < n && x == lo);
     if (lane == 0) {
       t.table[0][s * W + wave] = __popcll(above);
       t.table[1][s * W + wave] = __popcll(same);
     }
-  }
+  });
   __syncthreads();
   // exclusive prefix sums of the tables: a thread per run of entries
-  const int entries = stripes * W, per = (entries + NT - 1) / NT;
+  const int entries = (n + NT - 1) / NT * W, per = (entries + NT - 1) / NT;
   int sum[2] = {0, 0};
   for (int j = 0; j < per; ++j) {
     const int e = tid * per + j;
@@ -221,15 +268,13 @@ __device__ __forceinline__ void select_top(TopK<NT>& t, const uint32_t* keys, in
     }
   }
   __syncthreads();
-  for (int s = 0; s < stripes; ++s) {
-    const int i = s * NT + tid;
-    const uint32_t x = i < n ? keys[i] : 0;
-    const bool above = i < n && x > prefix, same = i < n && x == prefix;
+  each([&](int s, int i, uint32_t x) {
+    const bool above = i < n && x > lo, same = i < n && x == lo;
     const uint64_t lower = (1ull << lane) - 1;
     const int na = t.table[0][s * W + wave] + __popcll(__ballot(above) & lower);
     const int ns = t.table[1][s * W + wave] + __popcll(__ballot(same) & lower);
     if (above || (same && ns < need)) emit(na + min(ns, need), i);
-  }
+  });
 }
 
 // A score as a whole number that orders as it does (+0 and -0 alike).
@@ -237,27 +282,46 @@ __device__ __forceinline__ uint32_t order_bits(float x) {
   const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-constexpr uint32_t kForced = 0xffffffffu;  // blocks that are always chosen
 
-// 16 channels of a query row as codes.
-__device__ __forceinline__ i32x4 quantise(const uint16_t* q, float top) {
-  const u32x4 lo = *(const u32x4*)q, hi = *(const u32x4*)(q + 8);
-  i32x4 out;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t packed = 0;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t x = w < 2 ? lo[2 * w + j] : hi[2 * (w - 2) + j];
-      const float f0 = bf16_float(x & 0xffffu), f1 = __uint_as_float(x & 0xffff0000u);
-      const int c0 = top > 0.f ? (int)rintf(f0 * 127.f / top) : 0;
-      const int c1 = top > 0.f ? (int)rintf(f1 * 127.f / top) : 0;
-      packed |= (uint32_t)(c0 & 0xff) << (16 * j) | (uint32_t)(c1 & 0xff) << (16 * j + 8);
+// Codes round(127 x / top) of a group's queries.  The quotient q0 = 127 x / top comes from
+// the hardware's reciprocal and one correction, whose relative error is below 2^-22.
+// That rounds as the exact quotient does: 127 x / top is 127 a / (b 2^e) with bf16
+// significands a, b < 256, so it lies on a tie or at least 1 / (2 b 2^e) from it, 2^-16
+// of itself; and where it is a tie it is a float, to which the correction comes exactly.
+// (Outside [2^-100, 2^100] products may leave the range of floats: true division.)
+struct Coder {
+  float top, inv;
+  bool fast;
+  __device__ __forceinline__ explicit Coder(float t)
+      : top(t), inv(__builtin_amdgcn_rcpf(t)), fast(t > 7.9e-31f && t < 1.2e30f) {}
+  __device__ __forceinline__ int code(float x) const {
+    const float y = x * 127.f;
+    float q;
+    if (fast) {
+      q = y * inv;
+      q = __builtin_fmaf(__builtin_fmaf(-q, top, y), inv, q);
+    } else {
+      q = top > 0.f ? y / top : 0.f;
     }
-    out[w] = (int)packed;
+    return (int)rintf(q);
   }
-  return out;
-}
+  // 16 channels
+  __device__ __forceinline__ i32x4 codes(u32x4 lo, u32x4 hi) const {
+    i32x4 out;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t packed = 0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t x = w < 2 ? lo[2 * w + j] : hi[2 * (w - 2) + j];
+        packed |= (uint32_t)(code(bf16_float(x & 0xffffu)) & 0xff) << (16 * j) |
+                  (uint32_t)(code(__uint_as_float(x & 0xffff0000u)) & 0xff) << (16 * j + 8);
+      }
+      out[w] = (int)packed;
+    }
+    return out;
+  }
+};
 
 __device__ __forceinline__ float abs_max8(u32x4 w) {
   float m = 0.f;
@@ -281,6 +345,7 @@ __device__ __forceinline__ int max16(const i32x16& c, int m) {
 }
 
 constexpr int kSelThreads = 256;
+using BlockTopK = TopK<kSelThreads, kMaxCandBlocks>;
 
 // ------------------------------------------------ prefill: a list per query block
 //
@@ -299,11 +364,11 @@ struct SelTiles {
 };
 
 template <int D>
-__global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArgs a) {
   using ST = SelTiles<D>;
   extern __shared__ __attribute__((aligned(16))) uint8_t sel_smem[];
-  TopK<kSelThreads>& topk = *(TopK<kSelThreads>*)sel_smem;
-  uint8_t* const rows_lds = sel_smem + (sizeof(TopK<kSelThreads>) + 15) / 16 * 16;
+  BlockTopK& topk = *(BlockTopK*)sel_smem;
+  uint8_t* const rows_lds = sel_smem + (sizeof(BlockTopK) + 15) / 16 * 16;
   int* const best = (int*)(rows_lds + ST::kCodeBytes);
   __shared__ float red[kSelThreads / 64];
 
@@ -347,23 +412,41 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
   const int n_rows = n_tok * G;  // row r: token r / G, head g * G + r % G (contiguous in q)
   const uint16_t* const q0 = a.q + ((base + r0) * a.Hq + (int64_t)g * G) * D;
   auto row_at = [&](int r) { return q0 + ((int64_t)(r / G) * a.Hq + r % G) * D; };
+  // The first pass's rows stay in registers from the maximum to their codes.  (Rows past
+  // the last repeat it, which changes no maximum.)
+  constexpr int kItems = ST::kRowTiles * 32 * (D / 16) / kSelThreads;  // 16 channels each
+  u32x4 held[kItems][2];
   float top = 0.f;
-  for (int c = tid; c < n_rows * (D / 8); c += kSelThreads)
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const int c = u * kSelThreads + tid;
+    const u32x4* p = (const u32x4*)(row_at(min(c / (D / 16), n_rows - 1)) + c % (D / 16) * 16);
+    held[u][0] = p[0];
+    held[u][1] = p[1];
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) top = fmaxf(top, fmaxf(abs_max8(held[u][0]), abs_max8(held[u][1])));
+  for (int c = ST::kRowTiles * 32 * (D / 8) + tid; c < n_rows * (D / 8); c += kSelThreads)
     top = fmaxf(top, abs_max8(*(const u32x4*)(row_at(c / (D / 8)) + c % (D / 8) * 8)));
   top = wave_max(top);
   if (lane == 0) red[wave] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const Coder coder(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
 
   const int64_t blk0 = base / kPage + b;
   for (int p0 = 0; p0 < n_rows; p0 += ST::kRowTiles * 32) {
-    if (p0) __syncthreads();
     const int rows = min(n_rows - p0, ST::kRowTiles * 32);
     const int tiles = (rows + 31) / 32;
-    // (rows past the last repeat it, which changes no maximum)
-    for (int c = tid; c < tiles * 32 * (D / 16); c += kSelThreads) {
-      const int r = c / (D / 16), w = c % (D / 16);
-      *(i32x4*)(rows_lds + r * ST::kRowBytes + w * 16) = quantise(row_at(p0 + min(r, rows - 1)) + w * 16, top);
+    if (p0) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int c = u * kSelThreads + tid, r = c / (D / 16), w = c % (D / 16);
+      if (p0) {
+        const u32x4* p = (const u32x4*)(row_at(p0 + min(r, rows - 1)) + w * 16);
+        held[u][0] = p[0];
+        held[u][1] = p[1];
+      }
+      if (r < tiles * 32) *(i32x4*)(rows_lds + r * ST::kRowBytes + w * 16) = coder.codes(held[u][0], held[u][1]);
     }
     __syncthreads();
     i32x4 qf[ST::kRowTiles][D / 32];
@@ -399,7 +482,15 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
     keys[i] = i < a.n_sink || i >= n - a.n_recent ? kForced : order_bits(score);
   }
   __syncthreads();
-  select_top<kSelThreads>(topk, keys, n, a.top_k, [&](int rank, int i) { list[rank] = i; });
+  select_top(
+      topk, n, a.top_k,
+      [&](auto f) {
+        for (int s = 0; s * kSelThreads < n; ++s) {
+          const int i = s * kSelThreads + tid;
+          f(s, i, i < n ? keys[i] : kAbsent);
+        }
+      },
+      [&](int rank, int i) { list[rank] = i; });
 }
 
 // ------------------------------------------------- decode: a list per query token
@@ -426,10 +517,13 @@ __device__ __forceinline__ bool token_of(const SelectArgs& a, int64_t item, Toke
   return true;
 }
 
+// The codes of the token's rows are made once per workgroup, through LDS, while the
+// first pages' codes are on their way.
 template <int D>
 __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-  const int wave = threadIdx.x >> 6;
+  constexpr int kPer = kScoreTiles / (kSelThreads / 64);  // tiles of a wave
+  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * SelTiles<D>::kRowBytes];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31, wave = tid >> 6;
   const int G = a.Hq / a.Hkv;
   const int64_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
@@ -439,28 +533,45 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
   const int t0 = blockIdx.y * (kScoreTiles * 32);
   if (t0 >= n || n <= a.top_k) return;  // (all are chosen without scores)
   const uint16_t* const q0 = a.q + (tk.t * a.Hq + (int64_t)g * G) * D;
-  float top = 0.f;
-  for (int c = lane; c < G * (D / 8); c += 64) top = fmaxf(top, abs_max8(*(const u32x4*)(q0 + c * 8)));
-  top = wave_max(top);
   const int32_t* const row = a.table + (int64_t)tk.s * a.M;
   uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
-  constexpr int kPer = kScoreTiles / (kSelThreads / 64);  // tiles of a wave
+  int page[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) page[i] = row[min(t0 + (i * (kSelThreads / 64) + wave) * 32 + col, n - 1)];
+  float top = 0.f;
+  for (int c = lane; c < G * (D / 8); c += 64) top = fmaxf(top, abs_max8(*(const u32x4*)(q0 + c * 8)));
+  float scale[kPer];
+  i32x4 kf[kPer][D / 32];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int64_t e = (unsigned)page[i] < (unsigned)a.P ? page[i] : 0;
+    const int8_t* cp = a.codes + (e * a.Hkv + g) * D + half * 16;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) kf[i][kk] = *(const i32x4*)(cp + kk * 32);
+    scale[i] = a.scales[e * a.Hkv + g];
+  }
+  const Coder coder(wave_max(top));
   int m[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) m[i] = INT32_MIN;
   for (int u = 0; u < G; u += 32) {  // (more than one turn for more than 32 heads only)
-    const uint16_t* qr = q0 + (int64_t)min(u + col, G - 1) * D + half * 16;
+    if (u) __syncthreads();
+    // (rows past the last repeat it, which changes no maximum)
+    for (int c = tid; c < 32 * (D / 16); c += kSelThreads) {
+      const u32x4* p = (const u32x4*)(q0 + min(u + c / (D / 16), G - 1) * D + c % (D / 16) * 16);
+      *(i32x4*)(rows_lds + c / (D / 16) * SelTiles<D>::kRowBytes + c % (D / 16) * 16) = coder.codes(p[0], p[1]);
+    }
+    __syncthreads();
     i32x4 qf[D / 32];
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) qf[kk] = quantise(qr + kk * 32, top);
+    for (int kk = 0; kk < D / 32; ++kk)
+      qf[kk] = *(const i32x4*)(rows_lds + col * SelTiles<D>::kRowBytes + kk * 32 + half * 16);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int j = min(t0 + (i * (kSelThreads / 64) + wave) * 32 + col, n - 1);
-      int e = row[j];
-      e = (unsigned)e < (unsigned)a.P ? e : 0;
-      const int8_t* cp = a.codes + ((int64_t)e * a.Hkv + g) * D + half * 16;
       i32x16 acc = i32x16{};
 #pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) acc = mfma_i8(qf[kk], *(const i32x4*)(cp + kk * 32), acc);
-      m[i] = max16(acc, u ? m[i] : INT32_MIN);
+      for (int kk = 0; kk < D / 32; ++kk) acc = mfma_i8(qf[kk], kf[i][kk], acc);
+      m[i] = max16(acc, m[i]);
     }
   }
 #pragma unroll
@@ -469,26 +580,49 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
     const int j = t0 + (i * (kSelThreads / 64) + wave) * 32 + col;
     if (half == 0 && j < n) {
       // (a page that the table does not name comes last: nothing of it is attended to)
-      const int e = row[j];
-      uint32_t key = 0u;
-      if ((unsigned)e < (unsigned)a.P) key = order_bits((float)m[i] * a.scales[(int64_t)e * a.Hkv + g]);
+      const uint32_t key = (unsigned)page[i] < (unsigned)a.P ? order_bits((float)m[i] * scale[i]) : kAbsent;
       keys[j] = j < a.n_sink || j >= n - a.n_recent ? kForced : key;
     }
   }
 }
 
 constexpr int kPickThreads = 1024;
+constexpr int kPickHeld = 16;  // keys per thread held in registers
 __global__ __launch_bounds__(kPickThreads) void pick_pages_kernel(SelectArgs a) {
-  __shared__ TopK<kPickThreads> topk;
+  __shared__ TopK<kPickThreads, kMaxCandPages> topk;
+  const int tid = threadIdx.x;
   const int64_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
   Token tk;
   if (!token_of(a, item, &tk)) return;
   const int n = min(max(tk.pos, 0) / kPage, a.max_blocks);
   int32_t* const list = a.pages + (tk.t * a.Hkv + g) * a.top_k;
-  for (int i = min(n, a.top_k) + threadIdx.x; i < a.top_k; i += kPickThreads) list[i] = -1;
-  const uint32_t* keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
-  select_top<kPickThreads>(topk, keys, n, a.top_k, [&](int rank, int i) { list[rank] = i; });
+  for (int i = min(n, a.top_k) + tid; i < a.top_k; i += kPickThreads) list[i] = -1;
+  const uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
+  auto emit = [&](int rank, int i) { list[rank] = i; };
+  if (n <= kPickThreads * kPickHeld && n > a.top_k) {
+    uint32_t x[kPickHeld];
+#pragma unroll
+    for (int s = 0; s < kPickHeld; ++s) x[s] = s * kPickThreads + tid < n ? keys[s * kPickThreads + tid] : kAbsent;
+    select_top(
+        topk, n, a.top_k,
+        [&](auto f) {
+#pragma unroll
+          for (int s = 0; s < kPickHeld; ++s)
+            if (s * kPickThreads < n) f(s, s * kPickThreads + tid, x[s]);
+        },
+        emit);
+  } else {
+    select_top(
+        topk, n, a.top_k,
+        [&](auto f) {
+          for (int s = 0; s * kPickThreads < n; ++s) {
+            const int i = s * kPickThreads + tid;
+            f(s, i, i < n ? keys[i] : kAbsent);
+          }
+        },
+        emit);
+  }
 }
 
 }  // namespace
@@ -505,7 +639,7 @@ hipError_t launch_summary(const SummaryArgs& a, hipStream_t s) {
 
 hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.nqb * a.B * a.Hkv));
-  const size_t head = (sizeof(TopK<kSelThreads>) + 15) / 16 * 16;
+  const size_t head = (sizeof(BlockTopK) + 15) / 16 * 16;
   if (a.d == 128)
     hipLaunchKernelGGL(select_blocks_kernel<128>, grid, dim3(kSelThreads),
                        head + SelTiles<128>::kCodeBytes + (size_t)a.max_blocks * 4, s, a);

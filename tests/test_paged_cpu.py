@@ -115,7 +115,12 @@ def test_the_arguments_above_are_good(lib, fn):
     """(so that each refusal is that of the one argument that was changed)"""
     if torch.cuda.is_available():
         pytest.skip("the pointers are made up: nothing may be launched")
-    assert getattr(lib, fn)(*ARGS[fn].values()) in (HIP, UNSUP)
+    import threading
+    got = []  # (in a thread of its own: the last HIP error is kept per thread)
+    t = threading.Thread(target=lambda: got.append(getattr(lib, fn)(*ARGS[fn].values())))
+    t.start()
+    t.join()
+    assert got[0] in (HIP, UNSUP)
 
 
 def test_pages_and_workspaces_are_refused_when_small(lib):
