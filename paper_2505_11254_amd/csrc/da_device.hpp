@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <math.h>
+
 #include <hip/hip_runtime.h>
 
 namespace da {
@@ -33,6 +35,40 @@ __device__ __forceinline__ void wave_lds_exchange() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Sums and maxima over a wavefront by DPP moves, which cost a few clocks each where an
+// exchange through LDS takes about a hundred.  An inclusive scan: shifts by 1, 2, 4 and 8
+// inside rows of 16 lanes, then lane 15 of each row to the next one and lane 31 to the
+// upper half; lanes without a source take the identity.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_move(int identity, int x) {
+  return __builtin_amdgcn_update_dpp(identity, x, CTRL, ROWS, 0xf, false);
+}
+template <typename Op>
+__device__ __forceinline__ int wave_scan(int x, int identity, Op op) {
+  x = op(x, dpp_move<0x111, 0xf>(identity, x));
+  x = op(x, dpp_move<0x112, 0xf>(identity, x));
+  x = op(x, dpp_move<0x114, 0xf>(identity, x));
+  x = op(x, dpp_move<0x118, 0xf>(identity, x));
+  x = op(x, dpp_move<0x142, 0xa>(identity, x));
+  x = op(x, dpp_move<0x143, 0xc>(identity, x));
+  return x;
+}
+__device__ __forceinline__ int wave_scan_add(int x) {
+  return wave_scan(x, 0, [](int a, int b) { return a + b; });
+}
+// (the whole wavefront's, in every lane)
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, int identity, Op op) {
+  return __builtin_amdgcn_readlane(wave_scan(x, identity, op), 63);
+}
+__device__ __forceinline__ int wave_add(int x) { return __builtin_amdgcn_readlane(wave_scan_add(x), 63); }
+// of floats, none of them NaN
+__device__ __forceinline__ float wave_fmax(float x) {
+  return __int_as_float(wave_reduce(__float_as_int(x), __float_as_int(-INFINITY), [](int a, int b) {
+    return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
+  }));
 }
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));

@@ -99,14 +99,13 @@ struct PagedArgs {
   float scale_log2;
   int n_rowgroups;       // workgroups per (sequence or token, kv head, split)
   int n_split;           // key splits of the launch
-  int min_pages;         // least pages of a split
   float* part_o;         // [B][N][Hq][n_split][d]
   float* part_ml;        // [B][N][Hq][n_split][2]
 };
 // How a launch is cut (da_paged_api.cpp).
 struct PagedPlan {
   int row_tiles;         // tiles of 32 rows per workgroup: 1, 2, 4 or 8
-  int n_rowgroups, n_split, min_pages;
+  int n_rowgroups, n_split;
   size_t bytes;          // workspace
 };
 hipError_t launch_paged_attn(const PagedArgs& a, int row_tiles, hipStream_t s);

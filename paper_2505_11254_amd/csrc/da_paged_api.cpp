@@ -42,15 +42,33 @@ da_status check_rows(int B, int N, int Hq, int Hkv, int d) {
 da_status launched(hipError_t e) { return e == hipSuccess ? DA_OK : fail_hip(e); }
 
 // How the attention over pages is cut: rows into tiles of 32, up to row_tiles of
-// them per workgroup, and the key axis into n_split parts of at least min_pages.
-// Workgroups hold most of a CU's LDS, so that about one runs per CU; the key axis is
-// split until there are kTarget of them, which evens out sequences of different
-// lengths, as long as a part is worth its partial result: 4 pages feed each of four
-// key streams twice, and a row's partial (d + 2 floats) is small against the keys of
-// rows / 16 pages.
-constexpr int kTarget = 1024;
+// them per workgroup, and the key axis into n_split parts.  A workgroup alone takes
+// kPageUs per page; kSlots of them run at once (by LDS and registers).  Splitting fills
+// idle CUs, and where they are full it evens out sequences of different lengths, but
+// every workgroup has a start (kStartUs that little covers), every row of every split
+// a partial result that is written and read again, and the merge is a launch.  The
+// number of splits is the one whose estimate is least.  Measured (us, 32 heads on 8, d
+// 128 unless said): 64 single tokens, up to 8192 keys, 1 split 261, 5 245, 8 254; up to
+// 1000 keys 34, 45, 100; one token, 16 pages 14.3, 8 splits 10.9; 5 pages 9.5, 2 splits
+// 11.5; 7 tokens, 60000 keys, 1 split 428, 16 45, 32 46, 128 61; 4 trees of 64 drafts,
+// 40000 keys 962, 8 169, 16 178, 32 192; 24 of 40 drafts, 20 heads on 4, d 64, 700
+// keys 14.6, 2 splits 22.0.
 constexpr int kMaxPartPages = 1024;  // page ids a workgroup holds
-da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
+constexpr double kStartUs = 1.5, kMergeUs = 4., kHbmBytesPerUs = 5.5e6, kPartBytesPerUs = 4e6;
+
+double split_us(double s, double wgs, double groups, double pages, double rows, int d, double page_us, int slots) {
+  const double part = pages * page_us / s;  // of one workgroup
+  const double rounds = wgs * s / slots;
+  const double hbm = groups * pages * kPage * d * 4 / kHbmBytesPerUs;
+  const double work = rounds > 1. ? (rounds + 1.) * part : part;
+  double t = work > hbm ? work + 0.5 * hbm : hbm + 0.5 * work;
+  t += kStartUs * (rounds > 1. ? rounds : 1.);
+  if (s > 1.) t += kMergeUs + s * rows * (d + 2) * 8 / kPartBytesPerUs;  // each written and read
+  return t;
+}
+
+// `limit`: bytes of workspace at hand (0 splits where there is none).
+da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, size_t limit, PagedPlan* p) {
   const int G = Hq / Hkv;
   const int64_t rows = n_list ? G : (int64_t)N * G;
   p->row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
@@ -58,16 +76,35 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   const int64_t groups = (n_list ? (int64_t)B * N : B) * Hkv;
   if (n_list) pages = n_list + 1;
   const int64_t wgs = groups * p->n_rowgroups;
-  int64_t least = rows / 16 > 4 ? rows / 16 : 4;
-  if (least > kMaxPartPages) least = kMaxPartPages;
-  int64_t split = (kTarget + wgs - 1) / wgs;
-  if (split > (pages + least - 1) / least) split = (pages + least - 1) / least;
+  const int c = p->row_tiles == 1 ? 0 : p->row_tiles == 2 ? 1 : p->row_tiles == 4 ? 2 : 3;
+  static const double page_us[2][4] = {{0.46, 1.0, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
+  static const int slots[2][4] = {{256, 256, 512, 256}, {512, 512, 768, 768}};
   const int64_t need = (pages + kMaxPartPages - 1) / kMaxPartPages;
-  if (split < need) split = need;
-  p->min_pages = (int)least;
+  const size_t part = (size_t)B * N * Hq * (size_t)(d + 2) * 4;  // bytes per split
+  const int64_t most = (int64_t)(limit / part);                  // (1 split takes none)
+  if (need > 1 && most < need) return DA_ERR_WORKSPACE;
+  int64_t split = need;
+  double best = 1e300;
+  // candidates: 1, 2, 3, 4, 6, 8, 12, ... and what fills the slots once, two pages each at least
+  auto consider = [&](int64_t s) {
+    if (s < need || (s > 1 && (s > most || s > (pages + 1) / 2) && s > need)) return;
+    const double t = split_us((double)s, (double)wgs, (double)groups, (double)pages, (double)B * N * Hq, d,
+                              page_us[d == 64][c], slots[d == 64][c]);
+    if (t < best) {
+      best = t;
+      split = s;
+    }
+  };
+  consider(1);
+  consider(need);
+  for (int64_t s = 2; s <= 1024; s *= 2) {
+    consider(s);
+    consider(s + s / 2);
+  }
+  consider(slots[d == 64][c] / wgs);
   if ((groups * split + 7) / 8 * 8 * p->n_rowgroups > INT32_MAX) return DA_ERR_SHAPE;
   p->n_split = (int)split;
-  p->bytes = split > 1 ? (size_t)B * N * Hq * (size_t)split * (d + 2) * 4 : 0;
+  p->bytes = split > 1 ? part * (size_t)split : 0;
   return DA_OK;
 }
 
@@ -94,18 +131,14 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   const int64_t room = (int64_t)a.M * kPage;
   if (a.max_len > room) a.max_len = (int)room;
   PagedPlan p;
-  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, &p);
+  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, workspace ? workspace_bytes : 0, &p);
   if (st != DA_OK) return st;
-  if (p.bytes) {
-    if (!workspace || workspace_bytes < p.bytes) return DA_ERR_WORKSPACE;
-    if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
-  }
+  if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
   a.scale_log2 = 1.4426950408889634f / (a.d == 128 ? 11.313708498984761f : 8.f);
   a.n_rowgroups = p.n_rowgroups;
   a.n_split = p.n_split;
-  a.min_pages = p.min_pages;
   a.part_o = (float*)workspace;
   a.part_ml = a.part_o + (size_t)a.B * a.N * a.Hq * p.n_split * a.d;
   return launched(launch_paged_attn(a, p.row_tiles, (hipStream_t)stream));
@@ -357,7 +390,7 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
 size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len, int n_list) {
   PagedPlan p;
   if (check_rows(B, max_seqlen, Hq, Hkv, d) != DA_OK || max_len < 1 || n_list < 0) return 0;
-  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, &p) != DA_OK) return 0;
+  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, SIZE_MAX, &p) != DA_OK) return 0;
   return p.bytes;
 }
 

@@ -32,14 +32,13 @@ template <int D, int RT>
 struct Shape {
   static constexpr int NW = RT > 4 ? RT : 4;
   static constexpr int KS = NW / RT;
-  // Keys per unit: half a page where several streams share LDS, a whole page where
-  // all waves take the same one.
-  static constexpr int UNIT = KS == 1 ? 64 : 32;
+  // Keys per unit: half a page where four streams share LDS, else a whole page.
+  static constexpr int UNIT = KS == 4 ? 32 : 64;
   static constexpr int UPP = kPage / UNIT;  // units per page
   static constexpr int NB = UNIT / 32;      // 32-key blocks of scores
   static constexpr int unitElems = 2 * UNIT * D;  // keys, then values
   // ring of each stream: 128 KB together at d = 128 where several stream, 64 KB for one
-  static constexpr int DEPTH = KS == 2 ? 4 : 2;
+  static constexpr int DEPTH = 2;
   static constexpr int ringElems = KS * DEPTH * unitElems;
   static constexpr int regions = UNIT * D * 2 / 1024;  // 1 KB DMA regions per tile
   static constexpr int RPW = regions / RT;             // of a wave
@@ -72,7 +71,7 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, int b, int m, int i)
   const int pages = (x.L + kPage - 1) / kPage;
   // with lists a row reads the list's pages and the page of its own position
   x.n = a.lists ? (x.first + i >= 0 ? a.n_list + 1 : 0) : pages;
-  x.per = max(a.min_pages, (x.n + a.n_split - 1) / a.n_split);
+  x.per = max(1, (x.n + a.n_split - 1) / a.n_split);
   return x;
 }
 __device__ __forceinline__ int splits_of(const Span& x) { return (x.n + x.per - 1) / x.per; }

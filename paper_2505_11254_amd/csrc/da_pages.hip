@@ -104,11 +104,7 @@ __global__ __launch_bounds__(kThreads) void free_kernel(Table t, const int32_t* 
 template <int NT>
 __device__ __forceinline__ int block_scan(int x, int* lds, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  x = wave_scan_add(x);
   __syncthreads();
   if (lane == 63) lds[wave] = x;
   __syncthreads();
@@ -134,8 +130,8 @@ constexpr int kPlanThreads = 1024;
 constexpr int kRefsPerThread = 16;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32_t* __restrict__ slots,
                                                            const int32_t* __restrict__ new_lens, int n, int32_t* __restrict__ result) {
-  __shared__ int named[kMaxRequests];  // the slots of the requests
-  __shared__ int part[kMaxRequests];   // the page a request would write into, or -1
+  __shared__ __attribute__((aligned(16))) int named[kMaxRequests];  // the slots of the requests
+  __shared__ __attribute__((aligned(16))) int part[kMaxRequests];   // the page a request would write into, or -1
   __shared__ int cum[kMaxRequests];    // pages that the requests up to this one ask for
   __shared__ int entry[kMaxRequests];  // the entries it holds
   __shared__ int copied[kMaxRequests];  // 1: the last of them is copied, before new ones follow
@@ -151,7 +147,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   bool valid = (unsigned)s < (unsigned)t.S && want >= 0 && want <= t.M * kPage;
   if (valid) old = min(max(t.lens[s], 0), t.M * kPage);
   __syncthreads();
-  for (int j = 0; j < n; ++j) valid &= !(j < i && named[j] == s);
+  const int n4 = (n + 3) / 4 * 4;
+  for (int j = 0; j < n4; j += 4) {  // (names past n are -1)
+    const int4 x = *(const int4*)(named + j);
+    valid &= !((x.x == s && j < i) || (x.y == s && j + 1 < i) || (x.z == s && j + 2 < i) || (x.w == s && j + 3 < i));
+  }
   if (i < n && !valid) *r = int4{-1, -1, -1, 0};
 
   // ---- shrinking
@@ -181,31 +181,30 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   part[i] = pg;
   int rank = 0;
   if (__syncthreads_or(holders > 1)) {
-    for (int j = 0; j < n; ++j) rank += j < i && part[j] == pg;
+    for (int j = 0; j < n4; j += 4) {
+      const int4 x = *(const int4*)(part + j);
+      rank += (x.x == pg && j < i) + (x.y == pg && j + 1 < i) + (x.z == pg && j + 2 < i) + (x.w == pg && j + 3 < i);
+    }
   }
   const bool copy = pg >= 0 && holders - rank > 1;
   const int ask = grow ? (copy ? 1 : 0) + pages_of(want) - pages_of(old) : 0;
   // (sums are held at the pool's size: one more page than that is refused anyway)
-  int total;
-  int upto = ask;
+  int total, upto;
   {
-    // a sum of n requests of up to M pages each may pass 31 bits: saturate lane by lane
+    // a sum of n requests of up to M pages each may pass 31 bits: each is held at the
+    // pool's size + 1, in 64-bit sums across the waves (64 of them fit 32 bits inside one
+    // where the pool is below 2^25 pages, beyond which a page's bytes pass all memory)
     const int lane = i & 63, wave = i >> 6;
-    const int cap = t.P + 1;
-    upto = min(upto, cap);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(upto, d);
-      if (lane >= d) upto = min((int64_t)upto + y, (int64_t)cap);
-    }
-    if (lane == 63) scan[wave] = upto;
+    const int cap = min(t.P, (1 << 25) - 2) + 1;
+    const int x = wave_scan_add(min(ask, cap));
+    if (lane == 63) scan[wave] = x;
     __syncthreads();
     int64_t before = 0, all = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) {
       before += w < wave ? scan[w] : 0;
       all += scan[w];
     }
-    upto = (int)min(before + upto, (int64_t)cap);
+    upto = (int)min(before + x, (int64_t)cap);
     total = (int)min(all, (int64_t)cap);
     __syncthreads();
   }
@@ -256,8 +255,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   // the pages handed out: those asked for by the requests that are served
   int granted;
   {
-    int x = served ? upto : 0;
-    for (int d = 32; d; d /= 2) x = max(x, __shfl_xor(x, d));
+    const int x = wave_reduce(served ? upto : 0, 0, [](int p, int q) { return max(p, q); });
     __syncthreads();
     if ((i & 63) == 0) scan[i >> 6] = x;
     __syncthreads();
@@ -323,24 +321,28 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Table t, Pages p, cons
   const int64_t base = cu ? cu[b] : (int64_t)b * N;
   const int m = min(cu ? cu[b + 1] - cu[b] : N, N);
   const int s = slots ? slots[b] : b;
-  if ((unsigned)s >= (unsigned)t.S || base < 0 || base + m > T) return;
+  if ((unsigned)s >= (unsigned)t.S || m <= 0 || base < 0 || base + m > T) return;
   const int per_head = p.d / 8;
   const int row = p.Hkv * per_head;  // chunks per token
   const unsigned chunks = (unsigned)m * row;  // (the host has checked that N tokens' fit)
+  if (part * kAppendChunks >= chunks) return;
   const int pos0 = t.lens[s] - m;
+  // (in phases, so that the loads of a thread's chunks are under way together)
+  int at[kAppendPer], e[kAppendPer];
+  u32x4 x[kAppendPer];
 #pragma unroll
   for (int j = 0; j < kAppendPer; ++j) {
     const unsigned c = part * kAppendChunks + j * kThreads + threadIdx.x;
-    if (c >= chunks) break;
-    const int i = c / (unsigned)row, w = c % (unsigned)row;
+    const int i = min(c, chunks - 1) / (unsigned)row, w = min(c, chunks - 1) % (unsigned)row;
     const int pos = pos0 + i;
-    if (pos < 0 || pos >= t.M * kPage) continue;
-    const int e = t.table[(int64_t)s * t.M + pos / kPage];
-    if (!page_ok(e, t.P)) continue;
-    const u32x4 x = *(const u32x4*)(src + (base + i) * (int64_t)p.Hkv * p.d + w * 8);
-    const int h = w / per_head, q = w % per_head;
-    *(u32x4*)(dst + (((int64_t)e * p.Hkv + h) * kPage + pos % kPage) * p.d + q * 8) = x;
+    const bool inside = c < chunks && pos >= 0 && pos < t.M * kPage;
+    e[j] = inside ? t.table[(int64_t)s * t.M + pos / kPage] : -1;
+    x[j] = *(const u32x4*)(src + (base + i) * (int64_t)p.Hkv * p.d + w * 8);
+    at[j] = (w / per_head * kPage + pos % kPage) * p.d + w % per_head * 8;
   }
+#pragma unroll
+  for (int j = 0; j < kAppendPer; ++j)
+    if (page_ok(e[j], t.P)) *(u32x4*)(dst + (int64_t)e[j] * p.Hkv * kPage * p.d + at[j]) = x[j];
 }
 
 // Compacting, first launch, one request per workgroup: checks the kept places
@@ -420,24 +422,28 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, con
   const int rows = kThreads / per;     // rows per step of the workgroup
   const int j_in = threadIdx.x / per, c = threadIdx.x % per;
   constexpr int kMax = kMoveRows / 16;  // (d = 128: 16 rows per step, d = 64: 32)
+  const int steps = kMoveRows / rows;
   for (int j0 = r.y; j0 < r.x; j0 += kMoveRows) {
     u32x4 x[kMax];
+    int from[kMax], e[kMax], to[kMax];
+    // (in phases, so that the loads of a thread's rows are under way together)
 #pragma unroll
     for (int u = 0; u < kMax; ++u) {
-      const int j = j0 + u * rows + j_in;
-      if (u * rows >= kMoveRows || j >= r.x) continue;
-      const int pos = st + kp[j];
-      const int e = row[pos / kPage];
-      x[u] = page_ok(e, t.P) ? *(const u32x4*)(base + e * page + (pos % kPage) * p.d + c * 8) : u32x4{};
+      const int j = min(j0 + u * rows + j_in, r.x - 1);
+      from[u] = st + kp[j];
+      to[u] = row[(st + j) / kPage];
     }
+#pragma unroll
+    for (int u = 0; u < kMax; ++u) e[u] = row[from[u] / kPage];
+#pragma unroll
+    for (int u = 0; u < kMax; ++u)
+      if (u < steps)
+        x[u] = page_ok(e[u], t.P) ? *(const u32x4*)(base + e[u] * page + (from[u] % kPage) * p.d + c * 8) : u32x4{};
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMax; ++u) {
       const int j = j0 + u * rows + j_in;
-      if (u * rows >= kMoveRows || j >= r.x) continue;
-      const int pos = st + j;
-      const int e = row[pos / kPage];
-      *(u32x4*)(base + e * page + (pos % kPage) * p.d + c * 8) = x[u];
+      if (u < steps && j < r.x) *(u32x4*)(base + to[u] * page + ((st + j) % kPage) * p.d + c * 8) = x[u];
     }
     __syncthreads();
   }

@@ -159,13 +159,10 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
       members += in;
       forced += x == kForced;
     });
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      mn = min(mn, (uint32_t)__shfl_xor((int)mn, d));
-      mx = max(mx, (uint32_t)__shfl_xor((int)mx, d));
-      members += __shfl_xor(members, d);
-      forced += __shfl_xor(forced, d);
-    }
+    mn = (uint32_t)wave_reduce((int)mn, -1, [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
+    mx = (uint32_t)wave_reduce((int)mx, 0, [](int x, int y) { return (int)max((uint32_t)x, (uint32_t)y); });
+    members = wave_add(members);
+    forced = wave_add(forced);
     if (lane == 0) {
       t.ends[0][wave] = mn;
       t.ends[1][wave] = mx;
@@ -202,12 +199,7 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     __syncthreads();
     // thread tid holds the steps kBins-1 - 2 tid and the one below, the highest first
     const int c0 = t.hist[TK::kBins - 1 - 2 * tid], c1 = t.hist[TK::kBins - 2 - 2 * tid];
-    int upto = c0 + c1;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
-    }
+    int upto = wave_scan_add(c0 + c1);
     if (lane == 63) t.scan[2][wave] = upto;
     __syncthreads();
     for (int w = 0; w < wave; ++w) upto += t.scan[2][w];
@@ -245,12 +237,7 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
   int before[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    int x = sum[q];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
+    const int x = wave_scan_add(sum[q]);
     if (lane == 63) t.scan[q][wave] = x;
     before[q] = x - sum[q];
   }
@@ -329,12 +316,6 @@ __device__ __forceinline__ float abs_max8(u32x4 w) {
   for (int q = 0; q < 4; ++q)
     m = fmaxf(m, fmaxf(fabsf(bf16_float(w[q] & 0xffffu)), fabsf(__uint_as_float(w[q] & 0xffff0000u))));
   return m;
-}
-
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
 }
 
 // The largest of a lane's 16 products and m.
@@ -428,7 +409,7 @@ __global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArg
   for (int u = 0; u < kItems; ++u) top = fmaxf(top, fmaxf(abs_max8(held[u][0]), abs_max8(held[u][1])));
   for (int c = ST::kRowTiles * 32 * (D / 8) + tid; c < n_rows * (D / 8); c += kSelThreads)
     top = fmaxf(top, abs_max8(*(const u32x4*)(row_at(c / (D / 8)) + c % (D / 8) * 8)));
-  top = wave_max(top);
+  top = wave_fmax(top);
   if (lane == 0) red[wave] = top;
   __syncthreads();
   const Coder coder(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
@@ -550,7 +531,7 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
     for (int kk = 0; kk < D / 32; ++kk) kf[i][kk] = *(const i32x4*)(cp + kk * 32);
     scale[i] = a.scales[e * a.Hkv + g];
   }
-  const Coder coder(wave_max(top));
+  const Coder coder(wave_fmax(top));
   int m[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) m[i] = INT32_MIN;
@@ -586,10 +567,13 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
   }
 }
 
-constexpr int kPickThreads = 1024;
+// Workgroups of 256 threads take up to 4096 candidates, whose keys they hold in
+// registers, 1024 up to 16384 likewise, and more from memory: barriers of four waves
+// cost less than those of sixteen.
 constexpr int kPickHeld = 16;  // keys per thread held in registers
-__global__ __launch_bounds__(kPickThreads) void pick_pages_kernel(SelectArgs a) {
-  __shared__ TopK<kPickThreads, kMaxCandPages> topk;
+template <int NT, bool HELD>
+__global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
+  __shared__ TopK<NT, HELD ? NT * kPickHeld : kMaxCandPages> topk;
   const int tid = threadIdx.x;
   const int64_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
@@ -597,27 +581,29 @@ __global__ __launch_bounds__(kPickThreads) void pick_pages_kernel(SelectArgs a) 
   if (!token_of(a, item, &tk)) return;
   const int n = min(max(tk.pos, 0) / kPage, a.max_blocks);
   int32_t* const list = a.pages + (tk.t * a.Hkv + g) * a.top_k;
-  for (int i = min(n, a.top_k) + tid; i < a.top_k; i += kPickThreads) list[i] = -1;
+  for (int i = min(n, a.top_k) + tid; i < a.top_k; i += NT) list[i] = -1;
   const uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   auto emit = [&](int rank, int i) { list[rank] = i; };
-  if (n <= kPickThreads * kPickHeld && n > a.top_k) {
+  if constexpr (HELD) {
     uint32_t x[kPickHeld];
+    if (n > a.top_k) {
 #pragma unroll
-    for (int s = 0; s < kPickHeld; ++s) x[s] = s * kPickThreads + tid < n ? keys[s * kPickThreads + tid] : kAbsent;
+      for (int s = 0; s < kPickHeld; ++s) x[s] = s * NT + tid < n ? keys[s * NT + tid] : kAbsent;
+    }
     select_top(
         topk, n, a.top_k,
         [&](auto f) {
 #pragma unroll
           for (int s = 0; s < kPickHeld; ++s)
-            if (s * kPickThreads < n) f(s, s * kPickThreads + tid, x[s]);
+            if (s * NT < n) f(s, s * NT + tid, x[s]);
         },
         emit);
   } else {
     select_top(
         topk, n, a.top_k,
         [&](auto f) {
-          for (int s = 0; s * kPickThreads < n; ++s) {
-            const int i = s * kPickThreads + tid;
+          for (int s = 0; s * NT < n; ++s) {
+            const int i = s * NT + tid;
             f(s, i, i < n ? keys[i] : kAbsent);
           }
         },
@@ -658,7 +644,13 @@ hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s) {
     else
       hipLaunchKernelGGL(score_pages_kernel<64>, grid, dim3(kSelThreads), 0, s, a);
   }
-  hipLaunchKernelGGL(pick_pages_kernel, dim3((unsigned)items), dim3(kPickThreads), 0, s, a);
+  const dim3 grid((unsigned)items);
+  if (a.max_blocks <= 256 * kPickHeld)
+    hipLaunchKernelGGL((pick_pages_kernel<256, true>), grid, dim3(256), 0, s, a);
+  else if (a.max_blocks <= 1024 * kPickHeld)
+    hipLaunchKernelGGL((pick_pages_kernel<1024, true>), grid, dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL((pick_pages_kernel<1024, false>), grid, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
