@@ -8,6 +8,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "da_internal.hpp"
 #include "delta_attn.h"
 
 namespace da {
@@ -96,18 +97,19 @@ struct PagedArgs {
   const int32_t* lists;  // [T][Hkv][n_list] page positions, or nullptr: every page
   int B, N, Hq, Hkv, d, S, M, P;
   int max_len, mask_words, n_list;
+  int G;                 // Hq / Hkv
+  FastDiv fd_G, fd_Hkv, fd_Hq, fd_N;
   float scale_log2;
-  int n_rowgroups;       // workgroups per (sequence or token, kv head, split)
-  int n_split;           // key splits of the launch
-  float* part_o;         // [B][N][Hq][n_split][d]
-  float* part_ml;        // [B][N][Hq][n_split][2]
+  // How the work is shared (da_paged_api.cpp): n_wgs workgroups of row_tiles tiles of 32
+  // rows, at least min_units pages each; or, with `whole`, segments (a kv head's rows of
+  // a sequence, a workgroup's worth of them) as they are, min_units of them each.
+  // Workgroups begin at segments where that costs at most align_pages pages each.
+  int row_tiles, n_wgs, min_units, whole, align_pages;
+  // Workspace
+  int32_t* units;        // [B + 2] pages before each sequence's, the share, whether aligned
+  float* part_o;         // [n_wgs][2][row_tiles * 32][d] partial results of cut segments
+  float* part_ml;        // [n_wgs][2][row_tiles * 32][2]
 };
-// How a launch is cut (da_paged_api.cpp).
-struct PagedPlan {
-  int row_tiles;         // tiles of 32 rows per workgroup: 1, 2, 4 or 8
-  int n_rowgroups, n_split;
-  size_t bytes;          // workspace
-};
-hipError_t launch_paged_attn(const PagedArgs& a, int row_tiles, hipStream_t s);
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s);
 
 }  // namespace da

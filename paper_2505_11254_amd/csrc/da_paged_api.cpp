@@ -41,74 +41,61 @@ da_status check_rows(int B, int N, int Hq, int Hkv, int d) {
 
 da_status launched(hipError_t e) { return e == hipSuccess ? DA_OK : fail_hip(e); }
 
-// How the attention over pages is cut: rows into tiles of 32, up to row_tiles of
-// them per workgroup, and the key axis into n_split parts.  A workgroup alone takes
-// kPageUs per page; kSlots of them run at once (by LDS and registers).  Splitting fills
-// idle CUs, and where they are full it evens out sequences of different lengths, but
-// every workgroup has a start (kStartUs that little covers), every row of every split
-// a partial result that is written and read again, and the merge is a launch.  The
-// number of splits is the one whose estimate is least.  Measured (us, 32 heads on 8, d
-// 128 unless said): 64 single tokens, up to 8192 keys, 1 split 261, 5 245, 8 254; up to
-// 1000 keys 34, 45, 100; one token, 16 pages 14.3, 8 splits 10.9; 5 pages 9.5, 2 splits
-// 11.5; 7 tokens, 60000 keys, 1 split 428, 16 45, 32 46, 128 61; 4 trees of 64 drafts,
-// 40000 keys 962, 8 169, 16 178, 32 192; 24 of 40 drafts, 20 heads on 4, d 64, 700
-// keys 14.6, 2 splits 22.0.
-constexpr int kMaxPartPages = 1024;  // page ids a workgroup holds
-constexpr double kStartUs = 1.5, kMergeUs = 4., kHbmBytesPerUs = 5.5e6, kPartBytesPerUs = 4e6;
+int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 
-double split_us(double s, double wgs, double groups, double pages, double rows, int d, double page_us, int slots) {
-  const double part = pages * page_us / s;  // of one workgroup
-  const double rounds = wgs * s / slots;
-  const double hbm = groups * pages * kPage * d * 4 / kHbmBytesPerUs;
-  const double work = rounds > 1. ? (rounds + 1.) * part : part;
-  double t = work > hbm ? work + 0.5 * hbm : hbm + 0.5 * work;
-  t += kStartUs * (rounds > 1. ? rounds : 1.);
-  if (s > 1.) t += kMergeUs + s * rows * (d + 2) * 8 / kPartBytesPerUs;  // each written and read
-  return t;
-}
-
-// `limit`: bytes of workspace at hand (0 splits where there is none).
-da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, size_t limit, PagedPlan* p) {
+// How the attention over pages is shared: rows in tiles of 32, up to row_tiles of them
+// per workgroup, and as many workgroups as run at once (kSlots: by LDS and registers; at
+// d = 64 more would fit, but make more partial results than they gain), each with an
+// even share of all pages.  A workgroup alone takes kPageUs per page.
+//  - Segments are left whole where their even shares would gain less than the cuts cost:
+//    kCutUs for a second start in a workgroup, two tiles of partial results written and
+//    read, and the merge's launch.  Whole against shared (us; 32 heads on 8, d 128 unless
+//    said): one token, 300 keys 9.8, 15.4; 1000 keys 14.7, 11.2; 64 sequences up to
+//    1000 keys 36, 42, up to 8192 keys 257, 240; 30 trees of 64 up to 1500 keys 61, 74, 9
+//    of them up to 5000 keys 151, 62; 24 of 40 drafts, 20 heads on 4, d 64, up to 700
+//    keys 16, 20.
+//  - Workgroups begin at segments (and some stay idle) where that costs each at most
+//    kAlignPages pages, less than a second start and its partial results: one sequence of
+//    9000 keys, 14 drafts 26.5 -> 21.8 us; six of them 40.4 -> 37.3; 16 of 24 drafts, 6000
+//    keys 60.5 -> 58.7; eight of 2000 keys, 8 heads on 2, d 64, one token 13.0 -> 10.6.
+constexpr int kAlignPages = 8;
+struct PagedPlan {
+  int row_tiles, n_wgs, min_units, whole, align_pages;
+  size_t units_bytes, part_rows, bytes;
+};
+da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
   const int G = Hq / Hkv;
   const int64_t rows = n_list ? G : (int64_t)N * G;
-  p->row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
-  p->n_rowgroups = (int)((rows + 32 * p->row_tiles - 1) / (32 * p->row_tiles));
-  const int64_t groups = (n_list ? (int64_t)B * N : B) * Hkv;
+  const int rt = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
+  const int c = rt == 1 ? 0 : rt == 2 ? 1 : rt == 4 ? 2 : 3;
+  static const int kSlots[2][4] = {{256, 256, 512, 256}, {256, 256, 512, 512}};
+  static const double kPageUs[2][4] = {{0.46, 0.9, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
+  static const double kCutUs[4] = {4., 6., 8., 25.};
+  const int64_t segs = (n_list ? (int64_t)B * N : B) * Hkv * ((rows + 32 * rt - 1) / (32 * rt));
   if (n_list) pages = n_list + 1;
-  const int64_t wgs = groups * p->n_rowgroups;
-  const int c = p->row_tiles == 1 ? 0 : p->row_tiles == 2 ? 1 : p->row_tiles == 4 ? 2 : 3;
-  static const double page_us[2][4] = {{0.46, 1.0, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
-  static const int slots[2][4] = {{256, 256, 512, 256}, {512, 512, 768, 768}};
-  const int64_t need = (pages + kMaxPartPages - 1) / kMaxPartPages;
-  const size_t part = (size_t)B * N * Hq * (size_t)(d + 2) * 4;  // bytes per split
-  const int64_t most = (int64_t)(limit / part);                  // (1 split takes none)
-  if (need > 1 && most < need) return DA_ERR_WORKSPACE;
-  int64_t split = need;
-  double best = 1e300;
-  // candidates: 1, 2, 3, 4, 6, 8, 12, ... and what fills the slots once, two pages each at least
-  auto consider = [&](int64_t s) {
-    if (s < need || (s > 1 && (s > most || s > (pages + 1) / 2) && s > need)) return;
-    const double t = split_us((double)s, (double)wgs, (double)groups, (double)pages, (double)B * N * Hq, d,
-                              page_us[d == 64][c], slots[d == 64][c]);
-    if (t < best) {
-      best = t;
-      split = s;
-    }
-  };
-  consider(1);
-  consider(need);
-  for (int64_t s = 2; s <= 1024; s *= 2) {
-    consider(s);
-    consider(s + s / 2);
+  if (pages < 1) pages = 1;
+  if ((double)segs * (double)pages > (double)INT32_MAX) return DA_ERR_SHAPE;
+  const int64_t slots = kSlots[d == 64][c];
+  const double page_us = kPageUs[d == 64][c], seg_us = (double)pages * page_us;
+  // (lengths below the longest are taken to make four fifths of the work)
+  const double rounds = (double)segs / (double)slots;
+  p->row_tiles = rt;
+  p->whole = (seg_us < 12. && rounds >= 0.25) ||
+             seg_us * (double)((segs + slots - 1) / slots) < 0.8 * seg_us * rounds + kCutUs[c];
+  if (p->whole) {
+    p->min_units = 1;
+    p->n_wgs = (int)segs;
+  } else {
+    p->min_units = 2 * rt;
+    const int64_t most = (segs * pages + p->min_units - 1) / p->min_units;
+    p->n_wgs = (int)(most < slots ? most : slots);
   }
-  consider(slots[d == 64][c] / wgs);
-  if ((groups * split + 7) / 8 * 8 * p->n_rowgroups > INT32_MAX) return DA_ERR_SHAPE;
-  p->n_split = (int)split;
-  p->bytes = split > 1 ? part * (size_t)split : 0;
+  p->align_pages = kAlignPages;
+  p->units_bytes = ((size_t)B + 2 + 63) / 64 * 256;
+  p->part_rows = p->whole || p->n_wgs == 1 ? 0 : (size_t)p->n_wgs * 2 * rt * 32;
+  p->bytes = p->units_bytes + p->part_rows * (size_t)(d + 2) * 4;
   return DA_OK;
 }
-
-int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 
 // Entries of the lists of one (sequence, kv head): min(top_k, qb * R) each.
 int64_t list_total(int max_seqlen, int top_k, int block_q) {
@@ -131,17 +118,27 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   const int64_t room = (int64_t)a.M * kPage;
   if (a.max_len > room) a.max_len = (int)room;
   PagedPlan p;
-  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, workspace ? workspace_bytes : 0, &p);
+  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, &p);
   if (st != DA_OK) return st;
+  if (!workspace || workspace_bytes < p.bytes) return DA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
   a.scale_log2 = 1.4426950408889634f / (a.d == 128 ? 11.313708498984761f : 8.f);
-  a.n_rowgroups = p.n_rowgroups;
-  a.n_split = p.n_split;
-  a.part_o = (float*)workspace;
-  a.part_ml = a.part_o + (size_t)a.B * a.N * a.Hq * p.n_split * a.d;
-  return launched(launch_paged_attn(a, p.row_tiles, (hipStream_t)stream));
+  a.G = a.Hq / a.Hkv;
+  a.fd_G = make_fastdiv(a.G);
+  a.fd_Hkv = make_fastdiv(a.Hkv);
+  a.fd_Hq = make_fastdiv(a.Hq);
+  a.fd_N = make_fastdiv(a.N);
+  a.row_tiles = p.row_tiles;
+  a.n_wgs = p.n_wgs;
+  a.min_units = p.min_units;
+  a.whole = p.whole;
+  a.align_pages = p.align_pages;
+  a.units = (int32_t*)workspace;
+  a.part_o = (float*)((char*)workspace + p.units_bytes);
+  a.part_ml = a.part_o + p.part_rows * a.d;
+  return launched(launch_paged_attn(a, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -390,7 +387,7 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
 size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len, int n_list) {
   PagedPlan p;
   if (check_rows(B, max_seqlen, Hq, Hkv, d) != DA_OK || max_len < 1 || n_list < 0) return 0;
-  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, SIZE_MAX, &p) != DA_OK) return 0;
+  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, &p) != DA_OK) return 0;
   return p.bytes;
 }
 

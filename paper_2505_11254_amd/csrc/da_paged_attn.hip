@@ -15,8 +15,10 @@
 // as LDS holds.  Each of its four waves takes units of its own (4 key streams, no
 // barrier in the loop), and the waves' partial results meet at the end.  With more
 // rows, tiles of 32 rows share a unit: 2 tiles x 2 streams, 4 x 1, or 8 x 1.
-// The key axis is split over workgroups; partial results are merged by a second
-// launch.
+// The pages of all rows' keys, sequence by sequence and head by head, are one line of
+// work that the workgroups share evenly, as many of them as run at once: each takes a
+// stretch of it, whatever sequences that touches.  Rows whose keys several workgroups
+// have are merged by a second launch.
 #include "da_device.hpp"
 #include "da_paged.hpp"
 
@@ -25,7 +27,7 @@
 namespace da {
 namespace {
 
-constexpr int kMaxSplitPages = 1024;  // page ids of a split, held in LDS
+constexpr int kIdPages = 1024;  // page ids that a workgroup holds in LDS at a time
 
 // RT tiles of 32 rows and KS key streams per workgroup of NW waves.
 template <int D, int RT>
@@ -42,7 +44,7 @@ struct Shape {
   static constexpr int ringElems = KS * DEPTH * unitElems;
   static constexpr int regions = UNIT * D * 2 / 1024;  // 1 KB DMA regions per tile
   static constexpr int RPW = regions / RT;             // of a wave
-  static constexpr int ldsBytes = ringElems * 2 + kMaxSplitPages * 4;
+  static constexpr int ldsBytes = ringElems * 2 + kIdPages * 4 + 256;
   // waves per SIMD that LDS has room for
   static constexpr int WAVES = ldsBytes > 81920 ? 1 : 2;
   __device__ static constexpr int kswz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
@@ -56,28 +58,39 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
 }
 
-// The keys of one row group: pages of the sequence and how they are split.
-struct Span {
-  int L;      // keys of the sequence
-  int first;  // the position of the first new token
-  int n;      // pages (list entries and the own page, where there are lists)
-  int per;    // pages per split
+// One sequence: its new tokens, its keys, and its share of the work.
+struct SeqWork {
+  int64_t base;  // first row of q
+  int m;         // new tokens
+  int s;         // slot
+  int L;         // keys
+  int np;        // pages that each of its segments reads, at least 1
+  int n_rg;      // row groups per kv head (and token, with lists)
+  int segs;      // segments: (token with lists,) kv head, row group
 };
-__device__ __forceinline__ Span span_of(const PagedArgs& a, int b, int m, int i) {
-  Span x;
-  const int s = a.slots ? a.slots[b] : b;
-  x.L = (unsigned)s < (unsigned)a.S ? min(max(a.lens[s], 0), min(a.max_len, a.M * kPage)) : 0;
-  x.first = x.L - m;
-  const int pages = (x.L + kPage - 1) / kPage;
-  // with lists a row reads the list's pages and the page of its own position
-  x.n = a.lists ? (x.first + i >= 0 ? a.n_list + 1 : 0) : pages;
-  x.per = max(1, (x.n + a.n_split - 1) / a.n_split);
+template <bool LISTS>
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int b, int group_rows) {
+  SeqWork x;
+  x.base = a.cu ? a.cu[b] : (int64_t)b * a.N;
+  x.m = max(0, min(a.cu ? a.cu[b + 1] - a.cu[b] : a.N, a.N));
+  x.s = a.slots ? a.slots[b] : b;
+  x.L = (unsigned)x.s < (unsigned)a.S ? min(max(a.lens[x.s], 0), min(a.max_len, a.M * kPage)) : 0;
+  x.np = LISTS ? a.n_list + 1 : max(1, (x.L + kPage - 1) / kPage);
+  x.n_rg = (unsigned)((LISTS ? a.G : x.m * a.G) + group_rows - 1) / (unsigned)group_rows;
+  x.segs = (LISTS ? x.m : 1) * a.Hkv * x.n_rg;
   return x;
 }
-__device__ __forceinline__ int splits_of(const Span& x) { return (x.n + x.per - 1) / x.per; }
+// Units of work that count for a sequence: pages of its segments, or whole segments.
+__device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
+  return a.whole ? x.segs : x.segs * x.np;
+}
+// Units per workgroup, of `total`.
+__device__ __forceinline__ int share_of(const PagedArgs& a, int total) {
+  return max(a.min_units, (total + a.n_wgs - 1) / a.n_wgs);
+}
 
 template <int D, int RT, bool LISTS>
-__global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) void paged_attn_kernel(PagedArgs a, uint32_t n_items) {
+__global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) void paged_attn_kernel(PagedArgs a) {
   using SH = Shape<D, RT>;
   constexpr int NW = SH::NW, KS = SH::KS, DEPTH = SH::DEPTH, RPW = SH::RPW, MB = D / 32;
   constexpr int UNIT = SH::UNIT, UPP = SH::UPP, NB = SH::NB;
@@ -89,54 +102,148 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
   const int rt = wave % RT, ks = wave / RT;
+  const int G = a.G;
 
-  // Row groups of the same keys run side by side on one XCD (block i goes to XCD
-  // i % 8).
-  const uint32_t y = blockIdx.x / 8;
-  const uint32_t rg = y % (uint32_t)a.n_rowgroups;
-  uint32_t item = (y / (uint32_t)a.n_rowgroups) * 8 + blockIdx.x % 8;
-  if (item >= n_items) return;
-  const int split = item % (uint32_t)a.n_split;
-  item /= (uint32_t)a.n_split;
-  const int g = item % (uint32_t)a.Hkv;
-  item /= (uint32_t)a.Hkv;
-  const int b = LISTS ? item / (uint32_t)a.N : item;
-  const int tok = LISTS ? item % (uint32_t)a.N : 0;  // the token of a list
-  const int64_t base = a.cu ? a.cu[b] : (int64_t)b * a.N;
-  const int m = min(a.cu ? a.cu[b + 1] - a.cu[b] : a.N, a.N);
-  if (tok >= m) return;
-  const int G = a.Hq / a.Hkv;
+  // ---- this workgroup's share: units [x0, x1) of all sequences' in a row.  Neighbours
+  // in that order run on one XCD (block i goes to XCD i % 8): row groups of the same keys
+  // meet in its L2.
+  const int w = gridDim.x % 8 == 0 ? (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8) : (int)blockIdx.x;
+  // Up to 64 sequences each wave holds in its lanes, one each, and looks up there;
+  // more are counted by the whole workgroup and loaded one by one.
+  const bool few = a.B <= 64;
+  auto from_lane = [](const SeqWork& x, int j) {
+    SeqWork y;
+    y.base = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x.base, j) |
+             (int64_t)__builtin_amdgcn_readlane((int)(x.base >> 32), j) << 32;
+    y.m = __builtin_amdgcn_readlane(x.m, j);
+    y.s = __builtin_amdgcn_readlane(x.s, j);
+    y.L = __builtin_amdgcn_readlane(x.L, j);
+    y.np = __builtin_amdgcn_readlane(x.np, j);
+    y.n_rg = __builtin_amdgcn_readlane(x.n_rg, j);
+    y.segs = __builtin_amdgcn_readlane(x.segs, j);
+    return y;
+  };
+  SeqWork held{};
+  int b, off, left;
+  bool aligned = false;  // segments begin with workgroups
+  if (few) {
+    if (lane < a.B) held = seq_work<LISTS>(a, lane, RT * 32);
+    const int mine = lane < a.B ? units_of(a, held) : 0;
+    int upto = wave_scan_add(mine), units = mine;
+    int total = __builtin_amdgcn_readlane(upto, 63);
+    int share = share_of(a, total);
+    if (!a.whole) {
+      // Where segments are few against workgroups, whole workgroups go to each: a
+      // second segment would cost a workgroup another start, more than the pages that
+      // the even share saves.
+      const int segs = wave_add(lane < a.B ? held.segs : 0);
+      if (segs < a.n_wgs && (double)total * segs < (double)a.align_pages * a.n_wgs * (a.n_wgs - segs)) {
+        aligned = true;
+        share = max(a.min_units, (total + a.n_wgs - segs - 1) / (a.n_wgs - segs));
+        units = lane < a.B ? held.segs * ((held.np + share - 1) / share * share) : 0;
+        upto = wave_scan_add(units);
+        total = __builtin_amdgcn_readlane(upto, 63);
+      }
+    }
+    const int before = upto - units;
+    const int64_t x0 = (int64_t)w * share;
+    if (w == 0 && tid < 64) {  // (for the merge)
+      if (lane < a.B) a.units[lane] = before;
+      if (lane == 0) {
+        a.units[a.B] = share;
+        a.units[a.B + 1] = aligned;
+      }
+    }
+    if (x0 >= total) return;
+    left = min(share, total - (int)x0);
+    b = __builtin_ctzll(__ballot(before <= x0 && x0 < upto));
+    off = (int)x0 - __builtin_amdgcn_readlane(before, b);
+  } else {
+    int* const red = ids + kIdPages;  // [NW] sums, then what is found
+    auto block_scan = [&](int x, int* total) {
+      x = wave_scan_add(x);
+      __syncthreads();
+      if (lane == 63) red[wave] = x;
+      __syncthreads();
+      int before = 0, all = 0;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        before += v < wave ? red[v] : 0;
+        all += red[v];
+      }
+      *total = all;
+      return x + before;
+    };
+    auto units_at = [&](int j) { return j < a.B ? units_of(a, seq_work<LISTS>(a, j, RT * 32)) : 0; };
+    int mine = units_at(tid), sum, total;
+    int upto = block_scan(mine, &sum);
+    total = sum;
+    for (int b0 = kThreads; b0 < a.B; b0 += kThreads) {
+      int more;
+      block_scan(units_at(b0 + tid), &more);
+      total += more;
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int share = share_of(a, total);
+    const int64_t x0 = (int64_t)w * share;
+    if (w == 0 && tid == 0) {
+      a.units[a.B] = share;
+      a.units[a.B + 1] = 0;
+    }
+    if (x0 >= total) return;
+    left = min(share, total - (int)x0);
+    for (int b0 = 0, carry = 0; b0 < a.B; b0 += kThreads) {
+      if (b0) {
+        mine = units_at(b0 + tid);
+        upto = block_scan(mine, &sum);
+      }
+      const int64_t before = (int64_t)carry + upto - mine;
+      if (w == 0 && b0 + tid < a.B) a.units[b0 + tid] = (int)before;
+      if (before <= x0 && x0 < before + mine) {
+        red[NW] = b0 + tid;
+        red[NW + 1] = (int)(x0 - before);
+      }
+      carry += sum;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(red[NW]);
+    off = __builtin_amdgcn_readfirstlane(red[NW + 1]);
+  }
+  auto seq_at = [&](int j) {
+    return few ? from_lane(held, j) : from_lane(seq_work<LISTS>(a, j, RT * 32), 0);
+  };
+  SeqWork sq = seq_at(b);
+  int seg = off, p0 = 0;
+  if (!a.whole) {
+    const int np = aligned ? (sq.np + left - 1) / left * left : sq.np;  // (`left` is the share there)
+    seg = (unsigned)off / (unsigned)np;
+    p0 = off - seg * np;
+  }
+
+  // ---- segment after segment
+  while (true) {
+  const int head = sq.n_rg == 1 ? seg : (unsigned)seg / (unsigned)sq.n_rg;
+  const int rg = seg - head * sq.n_rg;
+  const int tok = LISTS ? (int)fdiv(head, a.fd_Hkv) : 0;  // the token of a list
+  const int g = head - tok * a.Hkv;
+  const int p1 = a.whole ? sq.np : min(sq.np, p0 + left);
+  const bool direct = p0 == 0 && p1 == sq.np;  // no other workgroup has keys of these rows
+  const int64_t base = sq.base;
+  const int m = sq.m;
   const int n_rows = LISTS ? G : m * G;
   const int row0 = rg * (RT * 32);
-  if (row0 >= n_rows) return;
-  const Span sp = span_of(a, b, m, tok);
-  const int n_eff = splits_of(sp);
-  // (a sequence without keys: the first split writes its rows)
-  const int p0 = __builtin_amdgcn_readfirstlane(split * sp.per);
-  const int p1 = __builtin_amdgcn_readfirstlane(min(p0 + sp.per, sp.n));
-  if (p0 >= p1 && split > 0) return;
-  const int n_pages = max(p1 - p0, 0);
-  const int first = __builtin_amdgcn_readfirstlane(sp.first);
-
-  // ---- page ids of the split (-1: no such page, its keys are not seen)
-  const int s = a.slots ? a.slots[b] : b;
-  const int own = LISTS ? (first + tok) / kPage : 0;
-  for (int j = tid; j < n_pages; j += kThreads) {
-    int at = p0 + j;
-    if (LISTS) {
-      at = at < a.n_list ? a.lists[((base + tok) * a.Hkv + g) * a.n_list + at] : own;
-      if (at < 0 || at > own || (at == own && p0 + j < a.n_list)) at = -1;
-    }
-    const int e = at >= 0 ? a.table[(int64_t)s * a.M + at] : -1;
-    ids[j] = (unsigned)e < (unsigned)a.P ? e : -1;
-  }
+  const int first = sq.L - m;  // the position of the first new token
+  // (with lists a row whose own position is missing reads nothing)
+  const int own = LISTS ? max(first + tok, 0) / kPage : 0;
+  // keys: up to the last that some row sees
+  const int last_key = LISTS ? first + tok : sq.L - 1;
 
   // ---- this lane's row
   const int r = row0 + rt * 32 + col;
   const int rc = min(r, n_rows - 1);
-  const int i_tok = LISTS ? tok : rc / G;
+  const int i_tok = LISTS ? tok : (int)fdiv(rc, a.fd_G);
   const int64_t t = base + i_tok;
-  const int h = g * G + (LISTS ? rc : rc % G);
+  const int h = g * G + (LISTS ? rc : rc - i_tok * G);
   const int pos = first + i_tok;
   bf16x8 qf[D / 16];
   {
@@ -144,20 +251,45 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + kk * 16);
   }
+
+  // ---- state of the rows
+  f32x16 o[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) o[mb] = f32x16{};
+  // Online softmax against a lagging reference, as in the prefill kernels: `ref` in
+  // base-2 units of the logits, -ref / c in every register of nref, from which the score
+  // accumulators start, so that c times them is logit - ref.
+  const float c2 = a.scale_log2, inv_c2 = 1.f / a.scale_log2;
+  float ref = 0.f, l = 0.f;
+  bool has_ref = false;
+  f32x16 nref = f32x16{};
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+
+  // ---- the segment's pages, as many at a time as there is room for ids
+  const int p_end = last_key < 0 ? p0 : p1;
+  for (int q0 = p0; q0 < p_end; q0 += kIdPages) {
+  const int q1 = min(q0 + kIdPages, p_end), n_pages = q1 - q0;
+  if (q0 > p0) __syncthreads();  // (the ids before are read)
+  for (int j = tid; j < n_pages; j += kThreads) {
+    int at = q0 + j;
+    if (LISTS) {
+      at = at < a.n_list ? a.lists[((base + tok) * a.Hkv + g) * a.n_list + at] : own;
+      if (at < 0 || at > own || (at == own && q0 + j < a.n_list)) at = -1;
+    }
+    const int e = at >= 0 ? a.table[(int64_t)sq.s * a.M + at] : -1;
+    ids[j] = (unsigned)e < (unsigned)a.P ? e : -1;  // (-1: no such page, its keys are not seen)
+  }
   // the queries have landed: the loop's products must not wait for them behind the
   // transfers issued there
   wait_vm<0>();
   __syncthreads();
 
-  // ---- units of this wave's stream: ks, ks + KS, ... of the split's
-  // the last key that some row of the sequence may see, and the units that hold keys up
-  // to there
-  const int last_key = __builtin_amdgcn_readfirstlane(LISTS ? first + tok : sp.L - 1);
-  // (with lists the last page is the own one, where the split has it)
-  const bool ends = p1 == sp.n;
-  const int tail_pos = LISTS ? own * kPage : (p1 - 1) * kPage;  // position of the last page
-  const int n_units = __builtin_amdgcn_readfirstlane(
-      n_pages == 0 ? 0 : (n_pages - 1) * UPP + (ends ? min(UPP, (last_key - tail_pos) / UNIT + 1) : UPP));
+  // ---- units of this wave's stream: ks, ks + KS, ... of these pages'
+  // (with lists the last page of all is the own one)
+  const bool ends = q1 == sq.np;
+  const int tail_pos = LISTS ? own * kPage : (q1 - 1) * kPage;  // position of the last page
+  const int n_units = (n_pages - 1) * UPP + (ends ? min(UPP, (last_key - tail_pos) / UNIT + 1) : UPP);
   const int tail_keys = ends ? last_key + 1 - tail_pos - (n_units - 1) % UPP * UNIT : UNIT;  // of the last unit
   const int n_it = (n_units + KS - 1) / KS;
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)smem;
@@ -176,7 +308,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   }
   auto page_of = [&](int it) -> int {  // -1: nothing to read
     const int u = it * KS + ks;
-    const int e = ids[min(u, max(n_units - 1, 0)) / UPP];
+    const int e = ids[min(u, n_units - 1) / UPP];
     return __builtin_amdgcn_readfirstlane(u < n_units ? e : -1);
   };
   // Every call issues 2 * RPW transfers, so that waits can count them; a unit
@@ -211,19 +343,6 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
     vread[mb] = (4 * half + tr_k) * D + (((4 * mb + 2 * tr_g1 + (tr_m >> 1)) ^ vsw) * 8) + (tr_m & 1) * 4;
-
-  f32x16 o[MB];
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb) o[mb] = f32x16{};
-  // Online softmax against a lagging reference, as in the prefill kernels: `ref` in
-  // base-2 units of the logits, -ref / c in every register of nref, from which the score
-  // accumulators start, so that c times them is logit - ref.
-  const float c2 = a.scale_log2, inv_c2 = 1.f / a.scale_log2;
-  float ref = 0.f, l = 0.f;
-  bool has_ref = false;
-  f32x16 nref = f32x16{};
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
 
   // Which of 32 keys from position k0 on this lane's row sees, bit by bit.
   auto visible = [&](int k0) -> uint32_t {
@@ -266,7 +385,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     }
     // mask the units that some row does not see whole
-    const int at = p0 + u / UPP;
+    const int at = q0 + u / UPP;
     const int k0 = (LISTS ? own : at) * kPage + u % UPP * UNIT;
     if (LISTS ? at >= a.n_list : k0 + UNIT > first) {
 #pragma unroll
@@ -389,6 +508,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     if (now >= 0) compute(it);
   }
   wait_vm<0>();
+  }  // (pages)
   __syncthreads();  // every transfer has landed and every read is done: the ring is free
   // A row that has seen nothing has the reference kNone, whose share of any sum is 0.
   constexpr float kNone = -1e30f;
@@ -435,9 +555,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     const auto pr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(pr[0]) + __uint_as_float(pr[1]);
   }
-  if (r >= n_rows) return;
   const int64_t orow = t * a.Hq + h;
-  if (n_eff <= 1) {
+  if (direct && r < n_rows) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -450,8 +569,10 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       }
     }
     if (a.lse && ks == 0 && half == 0) a.lse[orow] = l > 0.f ? (ref + __log2f(l)) * 0.6931471805599453f : -INFINITY;
-  } else {
-    const int64_t prow = (((int64_t)b * a.N + i_tok) * a.Hq + h) * a.n_split + split;
+  } else if (r < n_rows) {
+    // A workgroup cuts at most the first and the last of its segments: place 1 holds one
+    // that begins with its rows' first page, place 0 one that does not.
+    const int64_t prow = (int64_t)(2 * w + (p0 == 0 ? 1 : 0)) * (RT * 32) + rt * 32 + col;
     float* const po = a.part_o + prow * D;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -463,61 +584,92 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     }
     if (ks == 0 && half == 0) *(f32x2*)(a.part_ml + prow * 2) = f32x2{ref, l};
   }
+
+  // ---- on to the next segment
+  left -= a.whole ? 1 : p1 - p0;
+  if (left <= 0 || aligned) break;
+  p0 = 0;
+  if (++seg == sq.segs) {
+    seg = 0;
+    do {
+      if (++b >= a.B) return;  // (not reached: `left` counts the units that follow)
+      sq = seq_at(b);
+    } while (sq.segs == 0);
+  }
+  __syncthreads();  // (the ring is read)
+  }  // (segments)
 }
 
-// Merge of the splits' partial results, one workgroup per row: every wave finds the
-// largest reference with a split per lane, then groups of D/4 lanes take splits in
-// turn, four loads in flight each, and meet in LDS.
+// Merge of the partial results of rows whose keys several workgroups had.  Groups of
+// D/4 lanes, kRowGroups of them per row: one where rows are many, or all of a
+// workgroup's, which take workgroups' parts in turn and meet in LDS.  Four loads are
+// in flight per group.
 constexpr int kMergeThreads = 256;
-template <int D>
+constexpr int kManyRows = 2048;  // from here on a group of lanes per row
+template <int D, bool LISTS, bool MANY>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a) {
-  constexpr int kLanes = D / 4, kGroups = kMergeThreads / kLanes, kFlight = 4;
-  __shared__ f32x4 xo[kGroups][kLanes];
-  __shared__ float xl[kGroups];
-  const int tid = threadIdx.x, grp = tid / kLanes, c = tid % kLanes;
-  const int h = blockIdx.x % (unsigned)a.Hq;
-  const unsigned item = blockIdx.x / (unsigned)a.Hq;
-  const int b = item / (unsigned)a.N, i = item % (unsigned)a.N;
-  const int64_t base = a.cu ? a.cu[b] : (int64_t)b * a.N;
-  const int m = min(a.cu ? a.cu[b + 1] - a.cu[b] : a.N, a.N);
-  if (i >= m) return;
-  const Span sp = span_of(a, b, m, i);
-  const int n = splits_of(sp);
-  if (n <= 1) return;  // written by its one split
-  const int64_t orow = (base + i) * a.Hq + h;
-  const int64_t prow = (int64_t)blockIdx.x * a.n_split;
-  const float* po = a.part_o + prow * D + c * 4;
-  const f32x2* ml = (const f32x2*)a.part_ml + prow;
+  constexpr int kLanes = D / 4, kAll = kMergeThreads / kLanes;
+  constexpr int kRows = MANY ? kAll : 1, kRowGroups = kAll / kRows, kFlight = 4;
+  __shared__ f32x4 xo[kRowGroups][kLanes];
+  __shared__ float xl[kRowGroups];
+  const int tid = threadIdx.x, grp = MANY ? 0 : tid / kLanes, c = tid % kLanes;
+  const unsigned row = blockIdx.x * kRows + (MANY ? tid / kLanes : 0);
+  const unsigned item = fdiv(row, a.fd_Hq);
+  const int h = row - item * a.Hq;
+  const int b = fdiv(item, a.fd_N), i = item - b * a.N;
+  if (b >= a.B) return;  // (past the last row; whole groups only, and no barrier where kRows > 1)
+  const unsigned group_rows = a.row_tiles * 32;
+  const SeqWork sq = seq_work<LISTS>(a, b, group_rows);
+  if (i >= sq.m) return;
+  const int g = fdiv(h, a.fd_G);
+  const unsigned in_head = (LISTS ? 0 : i * a.G) + h - g * a.G;  // row of the (token and) kv head
+  const int seg = ((LISTS ? i * a.Hkv : 0) + g) * sq.n_rg + in_head / group_rows;
+  const unsigned share = a.units[a.B];
+  const int np = a.units[a.B + 1] ? (sq.np + share - 1) / share * share : sq.np;
+  const unsigned u0 = a.units[b] + seg * np;
+  const int w0 = u0 / share, n = (int)((u0 + sq.np - 1) / share) - w0 + 1;
+  if (n <= 1) return;  // written by the one workgroup that has all its keys
+  const int64_t orow = (sq.base + i) * a.Hq + h;
+  // part 0 lies in place 1 of workgroup w0, part j in place 0 of workgroup w0 + j
+  auto place = [&](int j) { return (int64_t)(2 * (w0 + j) + (j == 0 ? 1 : 0)) * group_rows + in_head % group_rows; };
+  const f32x2* ml = (const f32x2*)a.part_ml;
   float top = -1e30f;
-  for (int s = tid & 63; s < n; s += 64) top = fmaxf(top, ml[s][0]);
+  if (MANY) {
+    for (int j = c; j < n; j += kLanes) top = fmaxf(top, ml[place(j)][0]);
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    for (int d = 1; d < kLanes; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  } else {
+    for (int j = tid & 63; j < n; j += 64) top = fmaxf(top, ml[place(j)][0]);
+    top = wave_fmax(top);
+  }
   f32x4 acc = f32x4{};
   float l = 0.f;
-  for (int s0 = grp; s0 < n; s0 += kGroups * kFlight) {
+  for (int j0 = grp; j0 < n; j0 += kRowGroups * kFlight) {
     f32x2 x[kFlight];
     f32x4 y[kFlight];
 #pragma unroll
-    for (int u = 0; u < kFlight; ++u) {  // (past the last split: that one again, unused)
-      const int s = min(s0 + u * kGroups, n - 1);
-      x[u] = ml[s];
-      y[u] = *(const f32x4*)(po + (int64_t)s * D);
+    for (int u = 0; u < kFlight; ++u) {  // (past the last part: that one again, unused)
+      const int64_t at = place(min(j0 + u * kRowGroups, n - 1));
+      x[u] = ml[at];
+      y[u] = *(const f32x4*)(a.part_o + at * D + c * 4);
     }
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) {
-      const float f = s0 + u * kGroups < n ? fast_exp2(x[u][0] - top) : 0.f;
+      const float f = j0 + u * kRowGroups < n ? fast_exp2(x[u][0] - top) : 0.f;
       l += f * x[u][1];
       acc += f * y[u];
     }
   }
-  xo[grp][c] = acc;
-  if (c == 0) xl[grp] = l;
-  __syncthreads();
-  if (grp) return;
+  if (!MANY) {
+    xo[grp][c] = acc;
+    if (c == 0) xl[grp] = l;
+    __syncthreads();
+    if (grp) return;
 #pragma unroll
-  for (int w = 1; w < kGroups; ++w) {
-    acc += xo[w][c];
-    l += xl[w];
+    for (int w = 1; w < kRowGroups; ++w) {
+      acc += xo[w][c];
+      l += xl[w];
+    }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -527,15 +679,13 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a)
 
 }  // namespace
 
-hipError_t launch_paged_attn(const PagedArgs& a, int row_tiles, hipStream_t s) {
-  const int64_t groups = a.lists ? (int64_t)a.B * a.N : a.B;
-  const uint32_t items = (uint32_t)(groups * a.Hkv * a.n_split);
-  const dim3 grid((items + 7) / 8 * 8 * (uint32_t)a.n_rowgroups);
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_wgs);
 #define DA_PAGED(DD, RT, LS)                                                                       \
   hipLaunchKernelGGL((paged_attn_kernel<DD, RT, LS>), grid, dim3(64 * Shape<DD, RT>::NW),          \
-                     (Shape<DD, RT>::ldsBytes), s, a, items)
+                     (Shape<DD, RT>::ldsBytes), s, a)
 #define DA_PAGED_RT(DD, LS)                                                                        \
-  switch (row_tiles) {                                                                             \
+  switch (a.row_tiles) {                                                                           \
     case 1: DA_PAGED(DD, 1, LS); break;                                                            \
     case 2: DA_PAGED(DD, 2, LS); break;                                                            \
     default: DA_PAGED(DD, 4, LS); break;                                                           \
@@ -547,7 +697,7 @@ hipError_t launch_paged_attn(const PagedArgs& a, int row_tiles, hipStream_t s) {
       DA_PAGED_RT(64, true)
     }
   } else if (a.d == 128) {
-    if (row_tiles == 8)
+    if (a.row_tiles == 8)
       DA_PAGED(128, 8, false);
     else
       DA_PAGED_RT(128, false)
@@ -556,13 +706,31 @@ hipError_t launch_paged_attn(const PagedArgs& a, int row_tiles, hipStream_t s) {
   }
 #undef DA_PAGED_RT
 #undef DA_PAGED
-  if (a.n_split > 1) {
-    const dim3 g((unsigned)((int64_t)a.B * a.N * a.Hq));
-    if (a.d == 128)
-      hipLaunchKernelGGL(paged_merge_kernel<128>, g, dim3(kMergeThreads), 0, s, a);
-    else
-      hipLaunchKernelGGL(paged_merge_kernel<64>, g, dim3(kMergeThreads), 0, s, a);
+  if (a.whole || a.n_wgs == 1) return hipGetLastError();
+  const int64_t rows = (int64_t)a.B * a.N * a.Hq;
+  const bool many = rows >= kManyRows;
+  const int per = many ? kMergeThreads / (a.d / 4) : 1;
+  const dim3 g((unsigned)((rows + per - 1) / per));
+#define DA_MERGE(DD, LS, MANY)                                                                     \
+  hipLaunchKernelGGL((paged_merge_kernel<DD, LS, MANY>), g, dim3(kMergeThreads), 0, s, a)
+#define DA_MERGE_LS(DD, LS)                                                                        \
+  if (many)                                                                                        \
+    DA_MERGE(DD, LS, true);                                                                        \
+  else                                                                                             \
+    DA_MERGE(DD, LS, false)
+  if (a.lists) {
+    if (a.d == 128) {
+      DA_MERGE_LS(128, true);
+    } else {
+      DA_MERGE_LS(64, true);
+    }
+  } else if (a.d == 128) {
+    DA_MERGE_LS(128, false);
+  } else {
+    DA_MERGE_LS(64, false);
   }
+#undef DA_MERGE_LS
+#undef DA_MERGE
   return hipGetLastError();
 }
 

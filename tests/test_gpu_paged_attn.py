@@ -170,6 +170,42 @@ def test_long_context_in_many_splits(n_split_len):
     c.check(again, None, lambda b, i, g: torch.ones(lens[b], dtype=torch.bool))
 
 
+@pytest.mark.parametrize("B,Hkv", [(300, 2), (700, 1)])
+def test_many_short_sequences(B, Hkv):
+    """More sequences than a wavefront or a workgroup holds, empty ones among them."""
+    from paper_2505_11254_amd import binding
+    r = random.Random(B)
+    lens = [r.choice([0, 1, 63, 64, 200, 300]) for _ in range(B)]
+    lens[7] = 40 * 64
+    c = Case(lens, [1 if n else 0 for n in lens], 4 * Hkv, Hkv, 64, seed=B)
+    q, k, v, table, L = c.gpu()
+    out = binding.tree_attn_paged(q, k, v, table, L, **c.kw())
+    c.check(out, None, lambda b, i, g: torch.ones(lens[b], dtype=torch.bool))
+    # with a longer bound the work is shared differently
+    long = torch.cat([table, torch.full_like(table, -1)[:, :1].expand(-1, 3000)], 1).contiguous()
+    again = binding.tree_attn_paged(q, k, v, long, L, **c.kw())
+    c.check(again, None, lambda b, i, g: torch.ones(lens[b], dtype=torch.bool))
+
+
+def test_shares_of_more_pages_than_ids_are_held():
+    """Forty sequences of 100,000 tokens that repeat the same few pages: every workgroup has almost
+    2000 pages."""
+    from paper_2505_11254_amd import binding
+    g = torch.Generator().manual_seed(1)
+    P, n, Hkv, d = 60, 100_003, 8, 64
+    k, v = (torch.randn((P, Hkv, PAGE, d), generator=g).to(torch.bfloat16) for _ in range(2))
+    table = torch.randint(0, P, (40, pages_of(n)), generator=g).to(torch.int32)
+    L = torch.full((40,), n, dtype=torch.int32)
+    q = torch.randn((40, 8, d), generator=g).to(torch.bfloat16)
+    out = binding.tree_attn_paged(q.cuda(), k.cuda(), v.cuda(), table.cuda(), L.cuda(), B=40).cpu()
+    for b in (0, 17, 39):
+        c = Case([1], [1], 8, Hkv, d, seed=0)
+        c.q, c.lens = q[b:b + 1], [n]
+        t = table[b].long()
+        c.keys = lambda _, h: tuple(x[t, h].reshape(-1, d)[:n] for x in (k, v))
+        c.check(out[b:b + 1], None, lambda _, i, h: torch.ones(n, dtype=torch.bool))
+
+
 def test_logits_far_apart_and_equal():
     """One key far above the rest, all keys alike, and logits that rise along the axis."""
     from paper_2505_11254_amd import binding

@@ -124,31 +124,26 @@ def test_the_arguments_above_are_good(lib, fn):
 
 
 def test_workspaces_that_are_too_small(lib):
-    """Up to 65536 keys any workspace does; past that each 65536 need a split of their own."""
-    part = 2 * 3 * 8 * (128 + 2) * 4
-    a = dict(ARGS["tree_attn_paged"], M=5000, max_len=5000 * 64)  # 4.9 times 65536 keys
-    for size, ok in ((5 * part, True), (5 * part - 1, False), (0, False)):
-        a["size"] = size
-        if not ok or not torch.cuda.is_available():  # (made-up pointers: nothing may be launched)
-            assert (lib.tree_attn_paged(*a.values()) == WORKSPACE) != ok
-    a["ws"], a["size"] = None, 1 << 40
-    assert lib.tree_attn_paged(*a.values()) == WORKSPACE
+    for fn, need in (("tree_attn_paged", binding.paged_workspace_bytes(2, 3, 8, 2, 128, 512)),
+                     ("selected_attn_paged", binding.paged_workspace_bytes(2, 3, 8, 2, 128, 1, 4))):
+        a = dict(ARGS[fn], size=need - 1)
+        assert need > 0 and getattr(lib, fn)(*a.values()) == WORKSPACE
+        a["size"], a["ws"] = need, None
+        assert getattr(lib, fn)(*a.values()) == WORKSPACE
 
 
 @pytest.mark.parametrize("B,N,Hq,Hkv,d", [(1, 1, 32, 8, 128), (64, 1, 32, 8, 128), (3, 64, 64, 8, 128), (1, 1, 8, 1, 64),
-                                          (500, 7, 28, 4, 128)])
-def test_workspaces_hold_whole_splits(lib, B, N, Hq, Hkv, d):
-    part = B * N * Hq * (d + 2) * 4
-    for n in (1, 64, 100, 1000, 10 ** 4, 10 ** 5, 10 ** 6, 10 ** 7):
-        size = binding.paged_workspace_bytes(B, N, Hq, Hkv, d, n)
-        assert size % part == 0 and size // part != 1
-        assert size // part >= (n // 65536 if n > 65536 else 0)
-        assert size // part <= max(2, n // 64)  # a page each at least
+                                          (500, 7, 28, 4, 128), (20000, 1, 8, 2, 64)])
+def test_workspaces_of_any_length_are_bounded(lib, B, N, Hq, Hkv, d):
+    """At most two tiles of partial results for each workgroup that runs at once, and a count per sequence."""
+    most = 768 * 2 * 256 * (d + 2) * 4 + 4 * B + 512
+    for n in (1, 64, 100, 1000, 10 ** 4, 10 ** 5, 10 ** 6):
+        assert 0 < binding.paged_workspace_bytes(B, N, Hq, Hkv, d, n) <= most
     for k in (1, 8, 64, 500):
-        assert binding.paged_workspace_bytes(B, N, Hq, Hkv, d, 1, k) % part == 0
-    assert binding.paged_workspace_bytes(B, N, Hq, Hkv, d, 64) == 0
+        assert 0 < binding.paged_workspace_bytes(B, N, Hq, Hkv, d, 1, k) <= most
     assert binding.paged_workspace_bytes(0, N, Hq, Hkv, d, 64) == 0
     assert binding.paged_workspace_bytes(B, N, Hq, Hkv, 80, 64) == 0
+    assert binding.paged_workspace_bytes(50000, 1, 64, 64, 64, 1 << 30) == 0  # more pages than are counted
 
 
 def test_list_entries(lib):
