@@ -24,6 +24,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace da {
 namespace {
 
@@ -306,23 +308,24 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     dma_kc[i] = (pc ^ SH::kswz(dma_row[i])) * 16;
     dma_vc[i] = (pc ^ SH::vswz(dma_row[i])) * 16;
   }
-  auto page_of = [&](int it) -> int {  // -1: nothing to read
+  auto page_of = [&](int it) -> int {  // -1: nothing to read (a vector register until dma)
     const int u = it * KS + ks;
     const int e = ids[min(u, n_units - 1) / UPP];
-    return __builtin_amdgcn_readfirstlane(u < n_units ? e : -1);
+    return u < n_units ? e : -1;
   };
   // Every call issues 2 * RPW transfers, so that waits can count them; a unit
   // without keys reads page 0.  Rows past the last key read that key: what lies
   // behind it in the page may be anything, and a weight of zero times it could be
   // NaN.
-  auto dma = [&](int it, int e) {
+  auto dma = [&](int it, int stage, int page) -> int {
+    const int e = __builtin_amdgcn_readfirstlane(page);
     const int u = it * KS + ks;
     const int keys = e < 0 ? 1 : u == n_units - 1 ? tail_keys : UNIT;
     const uint64_t off = (uint64_t)max(e, 0) * page_bytes + (uint64_t)(u % UPP * UNIT * D * 2);
     const uint64_t ka = k0_addr + off, va = v0_addr + off;
     i32x4 kr = {(int)(uint32_t)ka, (int)((uint32_t)(ka >> 32) & 0xffffu), UNIT * D * 2, 0x00020000};
     i32x4 vr = {(int)(uint32_t)va, (int)((uint32_t)(va >> 32) & 0xffffu), UNIT * D * 2, 0x00020000};
-    uint32_t dst = ring + (uint32_t)((it % DEPTH) * SH::unitElems) * 2;
+    uint32_t dst = ring + (uint32_t)(stage * SH::unitElems) * 2;
     settle_sgprs(kr, vr, dst);
 #pragma unroll
     for (int i = 0; i < RPW; ++i) {
@@ -331,18 +334,21 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       dma16(kr, dst + region, row + dma_kc[i]);
       dma16(vr, dst + UNIT * D * 2 + region, row + dma_vc[i]);
     }
+    return e;
   };
 
-  // ---- LDS offsets of the operands (elements inside a unit)
+  // ---- LDS offsets of the operands (elements inside the stream's ring; the stage is a
+  // constant of the loop's unrolled halves)
+  const int ring0 = ks * DEPTH * SH::unitElems;
   int kread[D / 16];
 #pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) kread[kk] = col * D + (((2 * kk + half) ^ SH::kswz(col)) * 8);
+  for (int kk = 0; kk < D / 16; ++kk) kread[kk] = ring0 + col * D + (((2 * kk + half) ^ SH::kswz(col)) * 8);
   const int tr_g1 = (lane >> 4) & 1, tr_k = (lane >> 2) & 3, tr_m = lane & 3;
   const int vsw = SH::vswz(4 * half + tr_k);
   int vread[MB];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
-    vread[mb] = (4 * half + tr_k) * D + (((4 * mb + 2 * tr_g1 + (tr_m >> 1)) ^ vsw) * 8) + (tr_m & 1) * 4;
+    vread[mb] = ring0 + (4 * half + tr_k) * D + (((4 * mb + 2 * tr_g1 + (tr_m >> 1)) ^ vsw) * 8) + (tr_m & 1) * 4;
 
   // Which of 32 keys from position k0 on this lane's row sees, bit by bit.
   auto visible = [&](int k0) -> uint32_t {
@@ -362,28 +368,27 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     return (uint32_t)(sh ? (lo >> sh) | (hi << (64 - sh)) : lo);
   };
 
-  auto compute = [&](int it) {
+  auto compute = [&](int it, auto stage) {
     const int u = it * KS + ks;
-    const uint16_t* ku = smem + (ks * DEPTH + it % DEPTH) * SH::unitElems;
+    const uint16_t* ku = smem + decltype(stage)::value * SH::unitElems;
     const uint16_t* vu = ku + UNIT * D;
     f32x16 sc[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) sc[nb] = nref;
+    // K reads kAhead MFMAs ahead of their use, an order that the scheduling barriers hold
+    // (left to itself the compiler pairs each MFMA with its own read and a wait)
+    constexpr int kAhead = 4, kProducts = NB * D / 16;
+    auto kfrag = [&](int i) { return *(const bf16x8*)(ku + kread[i / NB] + (i % NB) * 32 * D); };
+    bf16x8 kf[kAhead];
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
+    for (int i = 0; i < kAhead; ++i) kf[i] = kfrag(i);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        sc[nb] = mfma32(*(const bf16x8*)(ku + kread[kk] + nb * 32 * D), qf[kk], sc[nb]);
-    if (NB == 2) {
-      // K reads four MFMAs ahead of their use
-      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-      for (int i = 0; i < D / 8 - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    for (int i = 0; i < kProducts; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      sc[i % NB] = mfma32(kf[i % kAhead], qf[i / NB], sc[i % NB]);
+      if (i + kAhead < kProducts) kf[i % kAhead] = kfrag(i + kAhead);
     }
+    __builtin_amdgcn_sched_barrier(0);
     // mask the units that some row does not see whole
     const int at = q0 + u / UPP;
     const int k0 = (LISTS ? own : at) * kPage + u % UPP * UNIT;
@@ -457,55 +462,51 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       tsum = weights();
     }
     l += tsum;
+    // V^T reads (two per MFMA) likewise
+    constexpr int kSums = 2 * NB * MB;
+    auto vfrag = [&](int i) {
+      const uint16_t* p = vu + vread[i % MB] + (16 * (i / MB)) * D;
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(p), lds_read_tr(p + 8 * D), 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    bf16x8 vf[kAhead];
 #pragma unroll
-    for (int f = 0; f < 2 * NB; ++f)
+    for (int i = 0; i < kAhead; ++i) vf[i] = vfrag(i);
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        const i16x4 lo = lds_read_tr(vu + vread[mb] + (16 * f) * D);
-        const i16x4 hi = lds_read_tr(vu + vread[mb] + (16 * f + 8) * D);
-        const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[mb] = mfma32(__builtin_bit_cast(bf16x8, both), pf[f], o[mb]);
-      }
-    if (NB == 2) {
-      // V^T reads (two per MFMA) four MFMAs ahead of their use
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-      for (int i = 0; i < D / 8 - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    for (int i = 0; i < kSums; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      o[i % MB] = mfma32(vf[i % kAhead], pf[i / MB], o[i % MB]);
+      if (i + kAhead < kSums) vf[i % kAhead] = vfrag(i + kAhead);
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   // ---- the loop.  Streams of one wave need no barrier: a stage is filled again when
   // the wave's own reads of it are done.  Waves that share a unit publish its parts
   // with one barrier per unit, which also says that the unit before it is read.  Page
   // ids are read one unit ahead of the transfers that need them.
-  int e[DEPTH];  // ids of the units in flight, the next to compute first
-#pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) {
-    e[d] = page_of(d);
-    dma(d, e[d]);
-  }
-  e[DEPTH - 1] = page_of(DEPTH - 1);
-  for (int it = 0; it < n_it; ++it) {
+  static_assert(DEPTH == 2, "the loop is unrolled by stage");
+  int now = dma(0, 0, page_of(0)), next = page_of(1);
+  auto step = [&](int it, auto stage) {
+    constexpr int kOther = 1 - decltype(stage)::value;
+    int after;
     if (RT == 1) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the reads of the stage that fills next
       asm volatile("" ::: "memory");
-      dma(it + DEPTH - 1, e[DEPTH - 1]);
-      wait_vm<(DEPTH - 1) * 2 * RPW>();
+      after = dma(it + 1, kOther, next);
+      wait_vm<2 * RPW>();
       asm volatile("" ::: "memory");
     } else {
-      wait_vm<(DEPTH - 2) * 2 * RPW>();
+      wait_vm<0>();
       __syncthreads();
-      dma(it + DEPTH - 1, e[DEPTH - 1]);
+      after = dma(it + 1, kOther, next);
     }
-    const int now = e[0];
-#pragma unroll
-    for (int d = 0; d < DEPTH - 1; ++d) e[d] = e[d + 1];
-    e[DEPTH - 1] = page_of(it + DEPTH);
-    if (now >= 0) compute(it);
+    next = page_of(it + 2);
+    if (now >= 0) compute(it, stage);
+    now = after;
+  };
+  for (int it = 0; it < n_it; it += 2) {
+    step(it, std::integral_constant<int, 0>{});
+    if (it + 1 < n_it) step(it + 1, std::integral_constant<int, 1>{});
   }
   wait_vm<0>();
   }  // (pages)
