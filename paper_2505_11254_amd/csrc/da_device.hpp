@@ -71,6 +71,24 @@ __device__ __forceinline__ float wave_fmax(float x) {
   }));
 }
 
+// of doubles that are not negative
+__device__ __forceinline__ double wave_dmax(double x) {
+  auto step = [&](auto move) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint64_t v = (uint64_t)(uint32_t)move((int)(uint32_t)u) | (uint64_t)(uint32_t)move((int)(u >> 32)) << 32;
+    x = fmax(x, __builtin_bit_cast(double, v));
+  };
+  step([](int a) { return dpp_move<0x111, 0xf>(0, a); });
+  step([](int a) { return dpp_move<0x112, 0xf>(0, a); });
+  step([](int a) { return dpp_move<0x114, 0xf>(0, a); });
+  step([](int a) { return dpp_move<0x118, 0xf>(0, a); });
+  step([](int a) { return dpp_move<0x142, 0xa>(0, a); });
+  step([](int a) { return dpp_move<0x143, 0xc>(0, a); });
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63) |
+                                        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32);
+}
+
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 

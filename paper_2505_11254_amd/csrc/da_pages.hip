@@ -138,6 +138,30 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   __shared__ int scan[kPlanThreads / 64];
   const int i = threadIdx.x;
   int4* const r = (int4*)result + i;
+  // Free pages: a bit each for sixteen counts per thread and step.  The first step's are
+  // loaded ahead (again after shrinking), all that a pool of 16384 pages needs.
+  constexpr int kStep = kPlanThreads * kRefsPerThread;
+  // (Plain loads: whether a count is 0 changes by atomics only where slots shrink, and the
+  // L1 cache holds no count from before that but the first step's, which an atomic
+  // load then fetches again.)
+  auto load = [&](int64_t base) -> unsigned {
+    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    unsigned bits = 0;
+    const int64_t p0 = base + i * kRefsPerThread;
+    if (p0 + kRefsPerThread <= t.P) {
+#pragma unroll
+      for (int j = 0; j < kRefsPerThread; j += 4) {
+        const i32x4u x = *(const i32x4u*)(t.refs + p0 + j);
+        bits |= (unsigned)(x[0] == 0) << j | (unsigned)(x[1] == 0) << (j + 1) | (unsigned)(x[2] == 0) << (j + 2) |
+                (unsigned)(x[3] == 0) << (j + 3);
+      }
+    } else {
+      for (int j = 0; j < kRefsPerThread; ++j)
+        if (p0 + j < t.P && t.refs[p0 + j] == 0) bits |= 1u << j;
+    }
+    return bits;
+  };
+  unsigned bits0 = load(0);
   int s = -1, old = 0, want = -1, pg = -1, holders = 0;
   if (i < n) {
     s = slots[i];
@@ -147,8 +171,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   bool valid = (unsigned)s < (unsigned)t.S && want >= 0 && want <= t.M * kPage;
   if (valid) old = min(max(t.lens[s], 0), t.M * kPage);
   __syncthreads();
-  const int n4 = (n + 3) / 4 * 4;
-  for (int j = 0; j < n4; j += 4) {  // (names past n are -1)
+  // (a wave compares with the requests before its own last; names past n are -1)
+  const int n4 = (i & ~63) < n ? min((n + 3) / 4 * 4, (i & ~63) + 64) : 0;
+  for (int j = 0; j < n4; j += 4) {
     const int4 x = *(const int4*)(named + j);
     valid &= !((x.x == s && j < i) || (x.y == s && j + 1 < i) || (x.z == s && j + 2 < i) || (x.w == s && j + 3 < i));
   }
@@ -156,7 +181,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
 
   // ---- shrinking
   const bool shrink = valid && want < old;
-  if (__syncthreads_or(shrink)) {
+  const bool shrunk = __syncthreads_or(shrink);
+  if (shrunk) {
     constexpr int kOwn = 4;  // pages that a thread gives back itself
     const int c0 = pages_of(want), c1 = pages_of(old);
     if (shrink) t.lens[s] = want;
@@ -212,31 +238,17 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
   entry[i] = pages_of(old);
   copied[i] = copy;
 
-  // free pages, sixteen counts per thread and step
-  constexpr int kStep = kPlanThreads * kRefsPerThread;
-  // (plain loads: no count that is 0 or becomes 0 above can be in the L1 cache yet, and
-  // below none becomes 0)
-  auto load = [&](int64_t base) -> unsigned {
-    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
-    unsigned bits = 0;
-    const int64_t p0 = base + i * kRefsPerThread;
-    if (p0 + kRefsPerThread <= t.P) {
-#pragma unroll
-      for (int j = 0; j < kRefsPerThread; j += 4) {
-        const i32x4u x = *(const i32x4u*)(t.refs + p0 + j);
-        bits |= (unsigned)(x[0] == 0) << j | (unsigned)(x[1] == 0) << (j + 1) | (unsigned)(x[2] == 0) << (j + 2) |
-                (unsigned)(x[3] == 0) << (j + 3);
-      }
-    } else {
-      for (int j = 0; j < kRefsPerThread; ++j)
-        if (p0 + j < t.P && t.refs[p0 + j] == 0) bits |= 1u << j;
-    }
-    return bits;
-  };
   int avail = 0;
+  if (shrunk) {
+    bits0 = 0;
+    for (int j = 0; j < kRefsPerThread; ++j) {
+      const int p = i * kRefsPerThread + j;
+      if (p < t.P && load_count(t.refs + p) == 0) bits0 |= 1u << j;
+    }
+  }
   for (int64_t base = 0; base < t.P && avail < total; base += kStep) {
     int all;
-    block_scan<kPlanThreads>(__popc(load(base)), scan, &all);
+    block_scan<kPlanThreads>(__popc(base ? load(base) : bits0), scan, &all);
     avail += all;
   }
   // Served in order until one does not fit; that one and every later one that
@@ -263,7 +275,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
     for (int w = 0; w < kPlanThreads / 64; ++w) granted = max(granted, scan[w]);
   }
   for (int64_t base = 0; base < t.P && seen < granted; base += kStep) {
-    const unsigned bits = load(base);
+    const unsigned bits = base ? load(base) : bits0;
     int all;
     int k = seen + block_scan<kPlanThreads>(__popc(bits), scan, &all) - __popc(bits);
     for (unsigned b = bits; b && k < granted; b &= b - 1, ++k) {
@@ -286,23 +298,25 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32
 }
 
 // Second launch: the rows of the copied pages, a workgroup per (request, layer, keys
-// or values, kv head).
+// or values, `heads` kv heads).
 __global__ __launch_bounds__(kThreads) void copy_kernel(Pages p, int P, const int32_t* __restrict__ result,
-                                                       int n) {
+                                                       int n, int heads) {
   unsigned b = blockIdx.x;
   const int i = b % (unsigned)n;
-  b /= (unsigned)n;
   const int4 r = ((const int4*)result)[i];
   if (r.y < 0 || r.z < 0) return;
-  const int h = b % (unsigned)p.Hkv;
-  b /= (unsigned)p.Hkv;
+  b /= (unsigned)n;
+  const int groups = p.Hkv / heads, h0 = b % (unsigned)groups * heads;
+  b /= (unsigned)groups;
   uint16_t* const base = (b & 1) ? p.v : p.k;
   const int64_t layer = b >> 1;
   const int64_t head = (int64_t)kPage * p.d;
-  const u32x4* const from = (const u32x4*)(base + ((layer * P + r.y) * p.Hkv + h) * head);
-  u32x4* const to = (u32x4*)(base + ((layer * P + r.z) * p.Hkv + h) * head);
   const int chunks = r.w * (p.d / 8);
-  for (int c = threadIdx.x; c < chunks; c += kThreads) to[c] = from[c];
+  for (int h = h0; h < h0 + heads; ++h) {
+    const u32x4* const from = (const u32x4*)(base + ((layer * P + r.y) * p.Hkv + h) * head);
+    u32x4* const to = (u32x4*)(base + ((layer * P + r.z) * p.Hkv + h) * head);
+    for (int c = threadIdx.x; c < chunks; c += kThreads) to[c] = from[c];
+  }
 }
 
 // New tokens become the last ones of their sequences: each thread moves 16 bytes
@@ -395,11 +409,12 @@ __global__ __launch_bounds__(kThreads) void compact_check_kernel(
   }
 }
 
-// Second launch: a workgroup per (request, layer, keys or values, kv head) moves
-// its rows up, 64 at a time.  Kept places ascend, so a row never moves down and a
-// batch's rows are all read before any of them, or of a later batch's sources, can
-// be written over.
-constexpr int kMoveRows = 64;
+// Second launch: a workgroup per (request, layer, keys or values, HB kv heads) moves
+// its rows up, kSteps steps at a time, each of the rows that the workgroup holds.
+// Kept places ascend, so a row never moves down and a batch's rows are all read before
+// any of them, or of a later batch's sources, can be written over.
+constexpr int kMoveSteps = 8;
+template <int HB>
 __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, const int32_t* __restrict__ slots,
                                                           const int32_t* __restrict__ start,
                                                           const int32_t* __restrict__ keep,
@@ -409,41 +424,45 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, con
   const int i = b % (unsigned)n;
   b /= (unsigned)n;
   const int4 r = ((const int4*)result)[i];
+  const int st = start[i], slot = slots[i];
+  const int32_t* const kp = keep + cu_keep[i];
   if (r.x < 0) return;  // refused
-  const int h = b % (unsigned)p.Hkv;
-  b /= (unsigned)p.Hkv;
+  const int32_t* const row = t.table + (int64_t)slot * t.M;
+  const int per = p.d / 8;                // 16-byte chunks per row
+  const int rows = kThreads / per / HB;   // rows per step of the workgroup
+  const int j_in = threadIdx.x / (per * HB), c = threadIdx.x % per;
+  const int groups = p.Hkv / HB, h = b % (unsigned)groups * HB + threadIdx.x / per % HB;
+  b /= (unsigned)groups;
   const int64_t layer = b >> 1;
-  uint16_t* const base = ((b & 1) ? p.v : p.k) + (layer * t.P * p.Hkv + h) * (int64_t)kPage * p.d;
+  uint16_t* const base = ((b & 1) ? p.v : p.k) + (layer * t.P * p.Hkv + h) * (int64_t)kPage * p.d + c * 8;
   const int64_t page = (int64_t)p.Hkv * kPage * p.d;
-  const int32_t* row = t.table + (int64_t)slots[i] * t.M;
-  const int st = start[i];
-  const int32_t* kp = keep + cu_keep[i];
-  const int per = p.d / 8;             // 16-byte chunks per row
-  const int rows = kThreads / per;     // rows per step of the workgroup
-  const int j_in = threadIdx.x / per, c = threadIdx.x % per;
-  constexpr int kMax = kMoveRows / 16;  // (d = 128: 16 rows per step, d = 64: 32)
-  const int steps = kMoveRows / rows;
-  for (int j0 = r.y; j0 < r.x; j0 += kMoveRows) {
-    u32x4 x[kMax];
-    int from[kMax], e[kMax], to[kMax];
-    // (in phases, so that the loads of a thread's rows are under way together)
+  for (int j0 = r.y; j0 < r.x; j0 += kMoveSteps * rows) {
+    u32x4 x[kMoveSteps];
+    int from[kMoveSteps], e[kMoveSteps], to[kMoveSteps];
+    // (in phases, so that the loads of a thread's rows are under way together; whole steps
+    // past the last row are left out)
 #pragma unroll
-    for (int u = 0; u < kMax; ++u) {
+    for (int u = 0; u < kMoveSteps; ++u) {
+      if (j0 + u * rows >= r.x) break;
       const int j = min(j0 + u * rows + j_in, r.x - 1);
       from[u] = st + kp[j];
       to[u] = row[(st + j) / kPage];
     }
 #pragma unroll
-    for (int u = 0; u < kMax; ++u) e[u] = row[from[u] / kPage];
+    for (int u = 0; u < kMoveSteps; ++u) {
+      if (j0 + u * rows >= r.x) break;
+      e[u] = row[from[u] / kPage];
+    }
 #pragma unroll
-    for (int u = 0; u < kMax; ++u)
-      if (u < steps)
-        x[u] = page_ok(e[u], t.P) ? *(const u32x4*)(base + e[u] * page + (from[u] % kPage) * p.d + c * 8) : u32x4{};
+    for (int u = 0; u < kMoveSteps; ++u) {
+      if (j0 + u * rows >= r.x) break;
+      x[u] = page_ok(e[u], t.P) ? *(const u32x4*)(base + e[u] * page + (from[u] % kPage) * p.d) : u32x4{};
+    }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kMax; ++u) {
+    for (int u = 0; u < kMoveSteps; ++u) {
       const int j = j0 + u * rows + j_in;
-      if (u < steps && j < r.x) *(u32x4*)(base + to[u] * page + ((st + j) % kPage) * p.d + c * 8) = x[u];
+      if (j < r.x) *(u32x4*)(base + to[u] * page + ((st + j) % kPage) * p.d) = x[u];
     }
     __syncthreads();
   }
@@ -453,9 +472,16 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Table t, Pages p, con
   if (c0 >= c1) return;
   __shared__ int left;
   __syncthreads();
-  if (threadIdx.x == 0) left = p.layers * 2 * p.Hkv - 1 - atomicAdd(result + 4 * i + 3, 1);
+  if (threadIdx.x == 0) left = p.layers * 2 * groups - 1 - atomicAdd(result + 4 * i + 3, 1);
   __syncthreads();
-  if (left == 0) give_back(t, slots[i], c0, c1);
+  if (left == 0) give_back(t, slot, c0, c1);
+}
+
+// Kv heads that a workgroup takes: one where that makes few workgroups, up to four where
+// it makes more than a few per CU, most of which would come and go without work.
+int heads_together(int n, const Pages& p) {
+  const int64_t wgs = (int64_t)n * p.layers * 2 * p.Hkv;
+  return wgs > 4096 && p.Hkv % 4 == 0 ? 4 : wgs > 2048 && p.Hkv % 2 == 0 ? 2 : 1;
 }
 
 }  // namespace
@@ -473,8 +499,9 @@ hipError_t launch_pages_resize(const Table& t, const Pages& p, const int32_t* sl
     return hipGetLastError();
   }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, t, slots, new_lens, n, result);
-  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, p, t.P,
-                     result, n);
+  const int heads = heads_together(n, p);
+  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(n * p.layers * 2 * (p.Hkv / heads))), dim3(kThreads), 0, s, p,
+                     t.P, result, n, heads);
   return hipGetLastError();
 }
 
@@ -493,8 +520,18 @@ hipError_t launch_pages_compact(const Table& t, const Pages& p, const int32_t* s
                                 const int32_t* cu_keep, int n, int32_t* result, hipStream_t s) {
   hipLaunchKernelGGL(compact_check_kernel, dim3(n), dim3(kThreads), 0, s, t, slots, start, keep, n_keep,
                      cu_keep, result);
-  hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(n * p.layers * 2 * p.Hkv)), dim3(kThreads), 0, s, t, p,
-                     slots, start, keep, cu_keep, n, result);
+  const int heads = heads_together(n, p);
+  const dim3 grid((unsigned)(n * p.layers * 2 * (p.Hkv / heads)));
+#define DA_COMPACT(HB)                                                                             \
+  hipLaunchKernelGGL(compact_kernel<HB>, grid, dim3(kThreads), 0, s, t, p, slots, start, keep,     \
+                     cu_keep, n, result)
+  if (heads == 4)
+    DA_COMPACT(4);
+  else if (heads == 2)
+    DA_COMPACT(2);
+  else
+    DA_COMPACT(1);
+#undef DA_COMPACT
   return hipGetLastError();
 }
 

@@ -22,6 +22,8 @@
 #include "da_device.hpp"
 #include "da_paged.hpp"
 
+#include <type_traits>
+
 namespace da {
 namespace {
 
@@ -40,17 +42,19 @@ __device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
 // ---------------------------------------------------------------- summaries
 //
 // A wavefront per (block, kv head): D/8 lanes read a key's row, 16 bytes each, so
-// that 512/D keys arrive per load; the lanes of one channel chunk are then added
-// up by exchanges.  Bound by HBM: every key is read once, 1/64 of that written.
+// that 512/D keys arrive per load.  The lanes that hold the same eight channels then
+// halve the sums they keep as they add them up, and each finishes one or two channels.
+// Every key is read once, 1/64 of that written; the conversions and sums in 64 bits
+// take about as long as the loads.
 template <int D>
 __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kSteps = kPage / kRows;
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int h = (int)(item % a.Hkv);
-  const int64_t x = item / a.Hkv;
-  int j = (int)(x % a.nblk);
-  const int b = (int)(x / a.nblk);
+  const uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const uint32_t x = item / (uint32_t)a.Hkv;
+  const int h = (int)(item - x * (uint32_t)a.Hkv);
+  const int b = (int)(x / (uint32_t)a.nblk);
+  int j = (int)(x - (uint32_t)b * (uint32_t)a.nblk);
   if (b >= a.B) return;
   int64_t block;  // where the summary goes
   const uint16_t* k;
@@ -87,25 +91,33 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
       sum[2 * q] += (double)bf16_float(w[i][q] & 0xffffu);
       sum[2 * q + 1] += (double)__uint_as_float(w[i][q] & 0xffff0000u);
     }
-  double top = 0.;
+  // Lanes a power of two apart exchange the halves that the other keeps: those with the
+  // bit set keep the upper one.
+  int q0 = 0;
+  auto halve = [&](auto width, int d) {
+    constexpr int kKept = decltype(width)::value;
+    const bool up = lane & d;
+    q0 += up ? kKept : 0;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-#pragma unroll
-    for (int d = kLanes; d < 64; d *= 2) sum[q] += __shfl_xor(sum[q], d);
-    top = fmax(top, fabs(sum[q]));
-  }
-#pragma unroll
-  for (int d = 1; d < kLanes; d *= 2) top = fmax(top, __shfl_xor(top, d));
-  if (r == 0) {
-    uint32_t out[2] = {};
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int code = top > 0. ? (int)rint(sum[q] * 127. / top) : 0;
-      out[q / 4] |= (uint32_t)(code & 0xff) << (8 * (q % 4));
+    for (int q = 0; q < kKept; ++q) {
+      const double other = __shfl_xor(up ? sum[q] : sum[q + kKept], d);
+      sum[q] = (up ? sum[q + kKept] : sum[q]) + other;
     }
-    *(uint2*)(a.codes + (block * a.Hkv + h) * D + c * 8) = uint2{out[0], out[1]};
-    if (c == 0) a.scales[block * a.Hkv + h] = (float)(top / (127. * kPage));
-  }
+  };
+  halve(std::integral_constant<int, 4>{}, 32);
+  halve(std::integral_constant<int, 2>{}, 16);
+  if (kLanes == 8) halve(std::integral_constant<int, 1>{}, 8);
+  constexpr int kMine = 8 * kLanes / 64;  // channels that this lane finishes, from q0 on
+  double top = fabs(sum[0]);
+  if (kMine == 2) top = fmax(top, fabs(sum[1]));
+  top = wave_dmax(top);
+  auto code = [&](double x) { return (uint32_t)((top > 0. ? (int)rint(x * 127. / top) : 0) & 0xff); };
+  uint8_t* const out = (uint8_t*)a.codes + (block * a.Hkv + h) * D + c * 8 + q0;
+  if (kMine == 2)
+    *(uint16_t*)out = (uint16_t)(code(sum[0]) | code(sum[1]) << 8);
+  else
+    *out = (uint8_t)code(sum[0]);
+  if (lane == 0) a.scales[block * a.Hkv + h] = (float)(top / (127. * kPage));
 }
 
 // ------------------------------------------------------------------- top_k
@@ -114,8 +126,9 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
 // values that holds the smallest chosen one: its keys' least and greatest value, a
 // histogram of kBins equal steps between them (in LDS, by atomics; steps of a range
 // that fits the keys spread them, where their leading bits alone would pile them up on
-// few counters), and the step that the count from above ends in.  32-bit keys need
-// at most three rounds of 2048 steps, scores two or three.  Then one pass ranks the chosen ones in
+// few counters), and the step that the count from above ends in, until that step holds
+// one value or just as many keys as are chosen.  32-bit keys need at most three
+// rounds of 2048 steps, scores two as a rule.  Then one pass ranks the chosen ones in
 // ascending order: stripes of NT keys, each wave's counts in a table, a prefix sum
 // over (stripe, wave).  Thread tid owns keys tid, tid + NT, ...; each(f) calls
 // f(stripe, index, key) for those of all stripes, index >= n where there is none.
@@ -126,14 +139,15 @@ constexpr uint32_t kAbsent = 0u;           // chosen last
 template <int NT, int MAX>
 struct TopK {
   static constexpr int kWaves = NT / 64;
-  static constexpr int kBins = 2 * NT;
+  static constexpr int kBins = 2048;
+  static constexpr int kPer = kBins / NT;  // of a thread
   static constexpr int kMaxStripes = (MAX + NT - 1) / NT;
   int hist[kBins];
   int table[2][kMaxStripes * kWaves];
   int scan[3][kWaves];
   uint32_t ends[2][kWaves];
   uint32_t bin;
-  int need;
+  int need, all;
 };
 
 template <int NT, int MAX, typename Each, typename Emit>
@@ -169,7 +183,8 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
       t.scan[0][wave] = members;
       t.scan[1][wave] = forced;
     }
-    t.hist[tid] = t.hist[NT + tid] = 0;
+#pragma unroll
+    for (int j = 0; j < TK::kPer; ++j) t.hist[j * NT + tid] = 0;
     __syncthreads();
     members = forced = 0;
 #pragma unroll
@@ -197,21 +212,34 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
       if (i < n && x >= lo && x <= hi) atomicAdd(&t.hist[(x - mn) >> sh], 1);
     });
     __syncthreads();
-    // thread tid holds the steps kBins-1 - 2 tid and the one below, the highest first
-    const int c0 = t.hist[TK::kBins - 1 - 2 * tid], c1 = t.hist[TK::kBins - 2 - 2 * tid];
-    int upto = wave_scan_add(c0 + c1);
+    // thread tid holds kPer steps, the highest of all threads' first
+    int c[TK::kPer], sum = 0;
+#pragma unroll
+    for (int j = 0; j < TK::kPer; ++j) sum += c[j] = t.hist[TK::kBins - 1 - TK::kPer * tid - j];
+    int upto = wave_scan_add(sum);
     if (lane == 63) t.scan[2][wave] = upto;
     __syncthreads();
     for (int w = 0; w < wave; ++w) upto += t.scan[2][w];
-    const int before = upto - c0 - c1;
+    int before = upto - sum;
     if (before < need && upto >= need) {
-      const bool second = before + c0 < need;
-      t.bin = TK::kBins - 1 - 2 * tid - (second ? 1 : 0);
-      t.need = need - before - (second ? c0 : 0);
+#pragma unroll
+      for (int j = 0; j < TK::kPer; ++j) {
+        if (before < need && before + c[j] >= need) {
+          t.bin = TK::kBins - 1 - TK::kPer * tid - j;
+          t.need = need - before;
+          t.all = before + c[j] == need;
+        }
+        before += c[j];
+      }
     }
     __syncthreads();
     need = t.need;
     lo = mn + (t.bin << sh);
+    if (t.all) {  // every key of the step is chosen
+      --lo;
+      need = 0;
+      break;
+    }
     if (sh == 0) break;
     hi = lo + min(mx - lo, (1u << sh) - 1u);
   }
@@ -281,10 +309,11 @@ struct Coder {
   bool fast;
   __device__ __forceinline__ explicit Coder(float t)
       : top(t), inv(__builtin_amdgcn_rcpf(t)), fast(t > 7.9e-31f && t < 1.2e30f) {}
+  template <bool FAST>
   __device__ __forceinline__ int code(float x) const {
     const float y = x * 127.f;
     float q;
-    if (fast) {
+    if (FAST) {
       q = y * inv;
       q = __builtin_fmaf(__builtin_fmaf(-q, top, y), inv, q);
     } else {
@@ -292,8 +321,8 @@ struct Coder {
     }
     return (int)rintf(q);
   }
-  // 16 channels
-  __device__ __forceinline__ i32x4 codes(u32x4 lo, u32x4 hi) const {
+  template <bool FAST>
+  __device__ __forceinline__ i32x4 codes16(u32x4 lo, u32x4 hi) const {
     i32x4 out;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -301,12 +330,16 @@ struct Coder {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t x = w < 2 ? lo[2 * w + j] : hi[2 * (w - 2) + j];
-        packed |= (uint32_t)(code(bf16_float(x & 0xffffu)) & 0xff) << (16 * j) |
-                  (uint32_t)(code(__uint_as_float(x & 0xffff0000u)) & 0xff) << (16 * j + 8);
+        packed |= (uint32_t)(code<FAST>(bf16_float(x & 0xffffu)) & 0xff) << (16 * j) |
+                  (uint32_t)(code<FAST>(__uint_as_float(x & 0xffff0000u)) & 0xff) << (16 * j + 8);
       }
       out[w] = (int)packed;
     }
     return out;
+  }
+  // 16 channels
+  __device__ __forceinline__ i32x4 codes(u32x4 lo, u32x4 hi) const {
+    return fast ? codes16<true>(lo, hi) : codes16<false>(lo, hi);
   }
 };
 
