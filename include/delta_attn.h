@@ -464,9 +464,9 @@ da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, in
  * A row that sees no token is 0.  Keys and values of all L tokens must be finite.
  * max_len: no slot is longer; tokens past it are ignored.  lse (fp32 [T, Hq], may be
  * NULL): log of the sum of exp(q.k / sqrt d), -inf for a row that sees nothing.
- * workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, 0) bytes.  At
- * most 2^31 - 1 pages are read in all, counted per kv head and workgroup's worth of rows
- * (64 to 256 of them), with every length max_len: else DA_ERR_SHAPE.
+ * workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, 0) bytes (may
+ * be 0).  At most 2^31 - 1 pages may be read in all, counted per kv head and workgroup's
+ * worth of rows (32 to 256), with every length max_len: else DA_ERR_SHAPE.
  */
 da_status tree_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out,
                           float* lse, const int32_t* table, const int32_t* lens, int S, int M,
@@ -541,8 +541,8 @@ da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_
                               int max_seqlen, int Hq, int Hkv, int d, const int32_t* pages,
                               int top_k, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace of tree_attn_paged (top_k 0) and selected_attn_paged (max_len 1); 0 if the sizes
- * are invalid.  Its contents on entry do not matter. */
+/* Workspace of tree_attn_paged (top_k 0) and selected_attn_paged (max_len 1); 0 if none is
+ * needed or the sizes are invalid.  Its contents on entry do not matter. */
 size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len,
                                 int top_k);
 

@@ -437,6 +437,8 @@ def check_inputs(*, max_seqlen, B=None, cu_seqlens=None, Hkv=None, block_q=None,
 
 PAGE_TOKENS = 64
 
+_entries = {}  # the library's entry points that have been called
+
 
 class _On:
     """The device of a call and its stream: sets the device where another is current, and takes
@@ -452,11 +454,16 @@ class _On:
         self.other = dev.index != torch._C._cuda_getDevice()
 
     def call(self, name, *args):
+        fn = _entries.get(name)
+        if fn is None:
+            fn = _entries[name] = getattr(load_library(), name)
         if self.other:
             with torch.cuda.device(self.dev):
-                _call(name, *args, self.raw)
+                rc = fn(*args, self.raw)
         else:
-            _call(name, *args, self.raw)
+            rc = fn(*args, self.raw)
+        if rc != 0:
+            raise DeltaAttnError(name, rc, load_library().da_last_hip_error())
 
     def empty(self, shape, dtype):
         if self.stream is None:

@@ -71,6 +71,8 @@ struct SelectArgs {
   const int32_t* slots;
   int B, N, Hq, Hkv, d, S, M, P;
   int top_k, n_sink, n_recent;
+  int G;                 // Hq / Hkv
+  FastDiv fd_G;
   int block_q, nqb;      // prefill
   int32_t* block_ptr;
   int32_t* block_idx;
@@ -105,7 +107,7 @@ struct PagedArgs {
   // a sequence, a workgroup's worth of them) as they are, min_units of them each.
   // Workgroups begin at segments where that costs at most align_pages pages each.
   int row_tiles, n_wgs, min_units, whole, align_pages;
-  // Workspace
+  // Workspace (nullptr where no rows are cut)
   int32_t* units;        // [B + 2] pages before each sequence's, the share, whether aligned
   float* part_o;         // [n_wgs][2][row_tiles * 32][d] partial results of cut segments
   float* part_ml;        // [n_wgs][2][row_tiles * 32][2]

@@ -91,8 +91,8 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
     p->n_wgs = (int)(most < slots ? most : slots);
   }
   p->align_pages = kAlignPages;
-  p->units_bytes = ((size_t)B + 2 + 63) / 64 * 256;
   p->part_rows = p->whole || p->n_wgs == 1 ? 0 : (size_t)p->n_wgs * 2 * rt * 32;
+  p->units_bytes = p->part_rows ? ((size_t)B + 2 + 63) / 64 * 256 : 0;  // (the merge's alone)
   p->bytes = p->units_bytes + p->part_rows * (size_t)(d + 2) * 4;
   return DA_OK;
 }
@@ -120,7 +120,7 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   PagedPlan p;
   st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, &p);
   if (st != DA_OK) return st;
-  if (!workspace || workspace_bytes < p.bytes) return DA_ERR_WORKSPACE;
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return DA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
@@ -135,7 +135,7 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   a.min_units = p.min_units;
   a.whole = p.whole;
   a.align_pages = p.align_pages;
-  a.units = (int32_t*)workspace;
+  a.units = p.bytes ? (int32_t*)workspace : nullptr;
   a.part_o = (float*)((char*)workspace + p.units_bytes);
   a.part_ml = a.part_o + p.part_rows * a.d;
   return launched(launch_paged_attn(a, (hipStream_t)stream));
@@ -319,6 +319,8 @@ da_status da_select_blocks(const void* q, const void* codes, const float* scales
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.d = d;
+  a.G = Hq / Hkv;
+  a.fd_G = make_fastdiv(a.G);
   a.top_k = top_k;
   a.n_sink = n_sink;
   a.n_recent = n_recent;
@@ -375,6 +377,8 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
   a.S = S;
   a.M = M;
   a.P = P;
+  a.G = Hq / Hkv;
+  a.fd_G = make_fastdiv(a.G);
   a.top_k = top_k;
   a.n_sink = n_sink;
   a.n_recent = n_recent;

@@ -149,7 +149,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     }
     const int before = upto - units;
     const int64_t x0 = (int64_t)w * share;
-    if (w == 0 && tid < 64) {  // (for the merge)
+    if (w == 0 && tid < 64 && a.units) {  // (for the merge)
       if (lane < a.B) a.units[lane] = before;
       if (lane == 0) {
         a.units[a.B] = share;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     total = __builtin_amdgcn_readfirstlane(total);
     const int share = share_of(a, total);
     const int64_t x0 = (int64_t)w * share;
-    if (w == 0 && tid == 0) {
+    if (w == 0 && tid == 0 && a.units) {
       a.units[a.B] = share;
       a.units[a.B + 1] = 0;
     }
@@ -200,7 +200,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
         upto = block_scan(mine, &sum);
       }
       const int64_t before = (int64_t)carry + upto - mine;
-      if (w == 0 && b0 + tid < a.B) a.units[b0 + tid] = (int)before;
+      if (w == 0 && b0 + tid < a.B && a.units) a.units[b0 + tid] = (int)before;
       if (before <= x0 && x0 < before + mine) {
         red[NW] = b0 + tid;
         red[NW + 1] = (int)(x0 - before);
@@ -707,7 +707,7 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   }
 #undef DA_PAGED_RT
 #undef DA_PAGED
-  if (a.whole || a.n_wgs == 1) return hipGetLastError();
+  if (!a.units) return hipGetLastError();  // no rows are cut
   const int64_t rows = (int64_t)a.B * a.N * a.Hq;
   const bool many = rows >= kManyRows;
   const int per = many ? kMergeThreads / (a.d / 4) : 1;

@@ -136,6 +136,15 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
 constexpr uint32_t kForced = 0xffffffffu;  // always chosen (never more than top_k are)
 constexpr uint32_t kAbsent = 0u;           // chosen last
 
+// A score as a whole number that orders as it does (+0 and -0 alike).
+__device__ __forceinline__ uint32_t order_bits(float x) {
+  const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float order_float(uint32_t x) {
+  return __uint_as_float(x & 0x80000000u ? x ^ 0x80000000u : ~x);
+}
+
 template <int NT, int MAX>
 struct TopK {
   static constexpr int kWaves = NT / 64;
@@ -159,15 +168,22 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     for (int i = tid; i < n; i += NT) emit(i, i);
     return;
   }
-  // members: keys in [lo, hi]; `need` of them are chosen, and every key above
+  // members: keys in [lo, hi]; `need` of them are chosen, and every key above.  The first
+  // round's steps are equal ones of the scores themselves, where their range allows
+  // (`lin`), later ones of the keys, whose spacing is by octaves.
   uint32_t lo = 1, hi = kForced - 1;
+  float f0 = 0.f, per_step = 0.f;
+  bool lin = false;
+  auto lin_step = [&](uint32_t x) { return (uint32_t)((order_float(x) - f0) * per_step); };
   int need = top_k;
-  for (bool first = true;; first = false) {
+  uint32_t bin = 0;
+  bool all = false;
+  for (int round = 0;; ++round) {
     uint32_t mn = ~0u, mx = 0;
     int forced = 0, members = 0;
     each([&](int, int i, uint32_t x) {
       if (i >= n) return;
-      const bool in = x >= lo && x <= hi;
+      const bool in = x >= lo && x <= hi && (!lin || lin_step(x) == bin);
       mn = in ? min(mn, x) : mn;
       mx = in ? max(mx, x) : mx;
       members += in;
@@ -175,8 +191,10 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     });
     mn = (uint32_t)wave_reduce((int)mn, -1, [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
     mx = (uint32_t)wave_reduce((int)mx, 0, [](int x, int y) { return (int)max((uint32_t)x, (uint32_t)y); });
-    members = wave_add(members);
-    forced = wave_add(forced);
+    if (round == 0) {
+      members = wave_add(members);
+      forced = wave_add(forced);
+    }
     if (lane == 0) {
       t.ends[0][wave] = mn;
       t.ends[1][wave] = mx;
@@ -194,7 +212,7 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
       members += t.scan[0][w];
       forced += t.scan[1][w];
     }
-    if (first) {
+    if (round == 0) {
       if (forced >= need) {  // (scores past the range of floats count as forced: the first of them)
         lo = kForced;
         break;
@@ -206,10 +224,25 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
         break;
       }
     }
-    const int bits = 32 - __clz((int)(mx - mn));  // 0 for a single value
-    const int sh = max(0, bits - (31 - __clz(TK::kBins)));
+    lo = mn;
+    hi = mx;
+    if (all) {  // every key of the last round's step is chosen
+      --lo;
+      need = 0;
+      break;
+    }
+    int sh = 0;
+    if (round == 0) {
+      f0 = order_float(mn);
+      const float range = order_float(mx) - f0;  // (steps 0 .. kBins - 1: the product may round up)
+      lin = range > 1e-30f && range < 1e30f;
+      per_step = lin ? (float)(TK::kBins - 1) * 0.9999f / range : 0.f;
+    } else {
+      lin = false;
+    }
+    if (!lin) sh = max(0, 32 - __clz((int)(mx - mn)) - (31 - __clz(TK::kBins)));  // (0 for a single value)
     each([&](int, int i, uint32_t x) {
-      if (i < n && x >= lo && x <= hi) atomicAdd(&t.hist[(x - mn) >> sh], 1);
+      if (i < n && x >= lo && x <= hi) atomicAdd(&t.hist[lin ? lin_step(x) : (x - mn) >> sh], 1);
     });
     __syncthreads();
     // thread tid holds kPer steps, the highest of all threads' first
@@ -234,8 +267,11 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     }
     __syncthreads();
     need = t.need;
-    lo = mn + (t.bin << sh);
-    if (t.all) {  // every key of the step is chosen
+    bin = t.bin;
+    all = t.all;
+    if (lin) continue;  // the step's keys: those whose score falls into it
+    lo = mn + (bin << sh);
+    if (all) {
       --lo;
       need = 0;
       break;
@@ -292,63 +328,101 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
   });
 }
 
-// A score as a whole number that orders as it does (+0 and -0 alike).
-__device__ __forceinline__ uint32_t order_bits(float x) {
-  const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+// The same by one wavefront for at most 64 RK keys, which it holds in registers (key s *
+// 64 + lane in x[s], 0 past the last): the smallest chosen key bit by bit, counting the
+// keys that are as large by ballots, without LDS or barriers.  Ends early where just
+// top_k keys are as large.
+template <int RK, typename Emit>
+__device__ __forceinline__ void select_wave(const uint32_t (&x)[RK], int n, int top_k, Emit emit) {
+  const int lane = threadIdx.x & 63;
+  auto count = [&](auto holds) {
+    int c = 0;
+#pragma unroll
+    for (int s = 0; s < RK; ++s) {
+      if (s * 64 >= n) break;
+      c += __popcll(__ballot(holds(s)));
+    }
+    return c;
+  };
+  uint32_t least = 0;
+  int above = 0;  // keys above it that are chosen
+  bool exact = n <= top_k;
+  for (int bit = 31; bit >= 0 && !exact; --bit) {
+    const uint32_t t = least | 1u << bit;
+    const int c = count([&](int s) { return x[s] >= t; });
+    if (c >= top_k) least = t;
+    exact = c == top_k;
+  }
+  if (!exact) above = count([&](int s) { return x[s] > least; });
+  const int need = exact ? 0 : top_k - above;  // of those equal to it, the first
+  int before = 0, same_before = 0;
+  const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+  for (int s = 0; s < RK; ++s) {
+    if (s * 64 >= n) break;
+    const bool in = s * 64 + lane < n;
+    const bool up = in && (exact ? x[s] >= least : x[s] > least), same = in && !exact && x[s] == least;
+    const uint64_t ups = __ballot(up), sames = __ballot(same);
+    const int ns = same_before + __popcll(sames & lower);
+    if (up || (same && ns < need)) emit(before + __popcll(ups & lower) + min(ns, need), s * 64 + lane);
+    before += __popcll(ups);
+    same_before += __popcll(sames);
+  }
 }
+constexpr int kWaveKeys = 16;  // per lane
 
-// Codes round(127 x / top) of a group's queries.  The quotient q0 = 127 x / top comes from
-// the hardware's reciprocal and one correction, whose relative error is below 2^-22.
-// That rounds as the exact quotient does: 127 x / top is 127 a / (b 2^e) with bf16
-// significands a, b < 256, so it lies on a tie or at least 1 / (2 b 2^e) from it, 2^-16
-// of itself; and where it is a tie it is a float, to which the correction comes exactly.
-// (Outside [2^-100, 2^100] products may leave the range of floats: true division.)
+// Codes round(127 x / top) of a group's queries, top its largest magnitude, ties to even.
+// With bf16 significands a and b of x and top, 128 to 255, the quotient is 127 a / (b 2^e).
+//  - It is a tie n + 1/2 where 254 a = (2n + 1) b 2^e.  127 is prime, so either 2n + 1 =
+//    127 and a = b, x = +-top / 2, whose code is +-64, or 127 divides b, which is 254.
+//  - Else it lies at least 1 / (2 b 2^e) from a tie, 2^-16 of itself.
+// So unless b is 254, round(k x) with k above 127 / top by a 2^-19th of it is the code: too
+// little to cross a tie, enough to round 63.5 to 64.  That takes one fma, onto 1.5 * 2^23, where
+// floats are whole numbers: the low byte of the sum is the code.
+//  - With b = 254, or top outside [2^-100, 2^100], where k or k x may not be normal: true
+//    division.
 struct Coder {
-  float top, inv;
+  float top, k;
   bool fast;
   __device__ __forceinline__ explicit Coder(float t)
-      : top(t), inv(__builtin_amdgcn_rcpf(t)), fast(t > 7.9e-31f && t < 1.2e30f) {}
+      : top(t),
+        k(127.f * __builtin_amdgcn_rcpf(t) * (1.f + 0x1p-19f)),
+        fast(t > 0x1p-100f && t < 0x1p100f && (__float_as_uint(t) & 0x7f0000u) != 0x7e0000u) {}
   template <bool FAST>
-  __device__ __forceinline__ int code(float x) const {
-    const float y = x * 127.f;
-    float q;
-    if (FAST) {
-      q = y * inv;
-      q = __builtin_fmaf(__builtin_fmaf(-q, top, y), inv, q);
-    } else {
-      q = top > 0.f ? y / top : 0.f;
-    }
-    return (int)rintf(q);
+  __device__ __forceinline__ uint32_t code(uint32_t bits) const {  // (the low byte)
+    const float x = __uint_as_float(bits);
+    if (FAST) return __float_as_uint(__builtin_fmaf(x, k, 12582912.f));
+    // (scaled by a power of two, so that 127 x neither overflows nor loses bits)
+    const float s = top > 1.f ? 0x1p-64f : 0x1p64f;
+    return (uint32_t)(int)rintf(top > 0.f ? x * s * 127.f / (top * s) : 0.f);
   }
   template <bool FAST>
-  __device__ __forceinline__ i32x4 codes16(u32x4 lo, u32x4 hi) const {
-    i32x4 out;
+  __device__ __forceinline__ uint2 codes8(u32x4 x) const {
+    uint32_t out[2];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      uint32_t packed = 0;
+    for (int w = 0; w < 2; ++w) {
+      uint32_t pair[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t x = w < 2 ? lo[2 * w + j] : hi[2 * (w - 2) + j];
-        packed |= (uint32_t)(code<FAST>(bf16_float(x & 0xffffu)) & 0xff) << (16 * j) |
-                  (uint32_t)(code<FAST>(__uint_as_float(x & 0xffff0000u)) & 0xff) << (16 * j + 8);
-      }
-      out[w] = (int)packed;
+      for (int j = 0; j < 2; ++j)
+        pair[j] = __builtin_amdgcn_perm(code<FAST>(x[2 * w + j] & 0xffff0000u), code<FAST>(x[2 * w + j] << 16), 0x0c0c0400u);
+      out[w] = __builtin_amdgcn_perm(pair[1], pair[0], 0x05040100u);
     }
-    return out;
+    return uint2{out[0], out[1]};
   }
-  // 16 channels
-  __device__ __forceinline__ i32x4 codes(u32x4 lo, u32x4 hi) const {
-    return fast ? codes16<true>(lo, hi) : codes16<false>(lo, hi);
-  }
+  // 8 channels
+  __device__ __forceinline__ uint2 codes(u32x4 x) const { return fast ? codes8<true>(x) : codes8<false>(x); }
 };
 
-__device__ __forceinline__ float abs_max8(u32x4 w) {
-  float m = 0.f;
+// The larger magnitudes of two times two bf16 values (whose bits, without the sign, order as
+// they do), and the largest of a wavefront's.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 max_bits(u16x2 m, u32x4 w) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    m = fmaxf(m, fmaxf(fabsf(bf16_float(w[q] & 0xffffu)), fabsf(__uint_as_float(w[q] & 0xffff0000u))));
+  for (int q = 0; q < 4; ++q) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[q] & 0x7fff7fffu));
   return m;
+}
+__device__ __forceinline__ float wave_top(u16x2 m) {
+  return __uint_as_float((uint32_t)wave_reduce(max((int)m[0], (int)m[1]), 0, [](int x, int y) { return max(x, y); }) << 16);
 }
 
 // The largest of a lane's 16 products and m.
@@ -360,40 +434,44 @@ __device__ __forceinline__ int max16(const i32x16& c, int m) {
 
 constexpr int kSelThreads = 256;
 using BlockTopK = TopK<kSelThreads, kMaxCandBlocks>;
+constexpr int kScoreThreads = 256;
 
 // ------------------------------------------------ prefill: a list per query block
 //
 // One workgroup per (sequence, kv head, query block), the late blocks first, which
-// have the most candidates.  The block's rows (block_q rows of G heads) pass
-// through LDS as codes, kRowTiles tiles of 32 at a time, and from there into
-// registers: each wave holds all of them and takes every fourth tile of 32
-// blocks, so a block's codes are read once per workgroup and pass.  Scores stay in
-// LDS.  Bound by the matrix unit where rows are many (256 rows: 32 MFMAs per 4 KB of
-// codes).
+// have the most candidates.  Each of its four waves holds kTiles tiles of 32 of the
+// block's rows (block_q rows of G heads) as codes in registers and takes every tile of 32
+// blocks; the waves' maxima meet in LDS.  Rows are loaded whole, neighbouring lanes
+// neighbouring chunks, and their codes pass through the wave's part of LDS into the
+// operand's layout.  (Loaded straight into that layout, each instruction took 16 bytes
+// of each of 64 lines, which the L1 cache did not keep for the next one: 52 us with
+// 16384 tokens, 32 heads on 8.)  More rows take further passes.  Bound by the queries, which are read once, and by the
+// selection; of the products there are 8 MFMAs per wave and 32 blocks.
 template <int D>
 struct SelTiles {
-  static constexpr int kRowTiles = 1024 / D;       // row tiles per pass (128 registers)
-  static constexpr int kRowBytes = D + 16;         // LDS row of codes, padded against conflicts
-  static constexpr int kCodeBytes = kRowTiles * 32 * kRowBytes;
+  static constexpr int kTiles = 256 / D;     // row tiles of a wave (32 registers of codes)
+  static constexpr int kRows = kTiles * 32;  // rows of a wave per pass
+  static constexpr int kRowBytes = D + 16;   // of codes in LDS, padded against bank conflicts
+  static constexpr int kBytes = kSelThreads / 64 * kRows * kRowBytes;
 };
 
 template <int D>
-__global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArgs a) {
   using ST = SelTiles<D>;
+  constexpr int kWaves = kSelThreads / 64;
   extern __shared__ __attribute__((aligned(16))) uint8_t sel_smem[];
   BlockTopK& topk = *(BlockTopK*)sel_smem;
   uint8_t* const rows_lds = sel_smem + (sizeof(BlockTopK) + 15) / 16 * 16;
-  int* const best = (int*)(rows_lds + ST::kCodeBytes);
-  __shared__ float red[kSelThreads / 64];
+  int* const best = (int*)(rows_lds + ST::kBytes);
+  __shared__ float red[kWaves];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int half = lane >> 5, col = lane & 31;
-  const int G = a.Hq / a.Hkv;
-  int64_t x = blockIdx.x;
-  const int g = (int)(x % a.Hkv);
-  x /= a.Hkv;
-  const int b = (int)(x % a.B);
-  const int qb = a.nqb - 1 - (int)(x / a.B);
+  const int G = a.G;
+  const uint32_t x = blockIdx.x / (uint32_t)a.Hkv;
+  const int g = (int)(blockIdx.x - x * (uint32_t)a.Hkv);
+  const int b = (int)(x % (uint32_t)a.B);
+  const int qb = a.nqb - 1 - (int)(x / (uint32_t)a.B);
   const int64_t base = a.cu ? a.cu[b] : (int64_t)b * a.N;
   const int L = min(a.cu ? a.cu[b + 1] - a.cu[b] : a.N, a.N);
   const int R = a.block_q / kPage;
@@ -401,7 +479,7 @@ __global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArg
 
   // list sizes are known ahead: min(top_k, qb * R) each
   auto before = [&](int qb_) -> int64_t {  // entries of the lists before qb_
-    const int64_t m = min((int64_t)qb_, (int64_t)a.top_k / R + 1);  // lists with j * R <= top_k
+    const int64_t m = min(qb_, a.top_k / R + 1);  // lists with j * R <= top_k
     return m * (m - 1) / 2 * R + (qb_ - m) * a.top_k;
   };
   const int64_t list0 = ((int64_t)b * a.Hkv + g) * a.total;
@@ -425,76 +503,101 @@ __global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArg
   const int r0 = qb * a.block_q, n_tok = min(a.block_q, L - r0);
   const int n_rows = n_tok * G;  // row r: token r / G, head g * G + r % G (contiguous in q)
   const uint16_t* const q0 = a.q + ((base + r0) * a.Hq + (int64_t)g * G) * D;
-  auto row_at = [&](int r) { return q0 + ((int64_t)(r / G) * a.Hq + r % G) * D; };
-  // The first pass's rows stay in registers from the maximum to their codes.  (Rows past
-  // the last repeat it, which changes no maximum.)
-  constexpr int kItems = ST::kRowTiles * 32 * (D / 16) / kSelThreads;  // 16 channels each
-  u32x4 held[kItems][2];
-  float top = 0.f;
+  // (byte offsets inside a query block fit 32 bits)
+  auto row_at = [&](int r) {
+    const uint32_t i = fdiv((uint32_t)r, a.fd_G);
+    return (const uint16_t*)((const char*)q0 + (i * (uint32_t)a.Hq + ((uint32_t)r - i * (uint32_t)G)) * (uint32_t)(2 * D));
+  };
+  // (Rows past the last repeat it, which changes no maximum.)
+  constexpr int kLanes = D / 8, kLoads = ST::kRows * kLanes / 64;
+  u32x4 held[kLoads];
+  auto load_row = [&](int p0, int u) {
+    const int r = p0 + wave * ST::kRows + u * (64 / kLanes) + lane / kLanes;
+    return *(const u32x4*)(row_at(min(r, n_rows - 1)) + lane % kLanes * 8);
+  };
+  auto load_rows = [&](int p0) {
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) {
-    const int c = u * kSelThreads + tid;
-    const u32x4* p = (const u32x4*)(row_at(min(c / (D / 16), n_rows - 1)) + c % (D / 16) * 16);
-    held[u][0] = p[0];
-    held[u][1] = p[1];
-  }
+    for (int u = 0; u < kLoads; ++u) held[u] = load_row(p0, u);
+  };
+  load_rows(0);
+  const int64_t blk0 = base / kPage + b;
+  const int8_t* const codes = a.codes + (blk0 * a.Hkv + g) * D + half * 16;
+  const int64_t stride = (int64_t)a.Hkv * D;
+  auto load_block = [&](i32x4* kf, int t0) {
+    const i32x4* p = (const i32x4*)(codes + min(t0 + col, n - 1) * stride);
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) top = fmaxf(top, fmaxf(abs_max8(held[u][0]), abs_max8(held[u][1])));
-  for (int c = ST::kRowTiles * 32 * (D / 8) + tid; c < n_rows * (D / 8); c += kSelThreads)
-    top = fmaxf(top, abs_max8(*(const u32x4*)(row_at(c / (D / 8)) + c % (D / 8) * 8)));
-  top = wave_fmax(top);
+    for (int kk = 0; kk < D / 32; ++kk) kf[kk] = p[2 * kk];
+  };
+  for (int i = tid; i < n; i += kSelThreads) best[i] = INT32_MIN;
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) most = max_bits(most, held[u]);
+  for (int c = kWaves * ST::kRows * (D / 8) + tid; c < n_rows * (D / 8); c += kSelThreads)
+    most = max_bits(most, *(const u32x4*)(row_at(c / (D / 8)) + c % (D / 8) * 8));
+  float top = wave_top(most);
   if (lane == 0) red[wave] = top;
   __syncthreads();
-  const Coder coder(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  top = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, red[w]);
+  const Coder coder(top);
 
-  const int64_t blk0 = base / kPage + b;
-  for (int p0 = 0; p0 < n_rows; p0 += ST::kRowTiles * 32) {
-    const int rows = min(n_rows - p0, ST::kRowTiles * 32);
-    const int tiles = (rows + 31) / 32;
-    if (p0) __syncthreads();
+  for (int p0 = 0; p0 < n_rows; p0 += kWaves * ST::kRows) {
+    if (p0) load_rows(p0);
+    if (p0 + wave * ST::kRows >= n_rows) break;  // (uniform over the wave; no barrier in the loop)
+    uint8_t* const mine = rows_lds + wave * (ST::kRows * ST::kRowBytes);
+    wave_lds_exchange();  // (the pass before has read its rows)
+    auto place = [&](int u) {
+      return (uint2*)(mine + (u * (64 / kLanes) + lane / kLanes) * ST::kRowBytes + lane % kLanes * 8);
+    };
+    if (coder.fast) {
 #pragma unroll
-    for (int u = 0; u < kItems; ++u) {
-      const int c = u * kSelThreads + tid, r = c / (D / 16), w = c % (D / 16);
-      if (p0) {
-        const u32x4* p = (const u32x4*)(row_at(p0 + min(r, rows - 1)) + w * 16);
-        held[u][0] = p[0];
-        held[u][1] = p[1];
-      }
-      if (r < tiles * 32) *(i32x4*)(rows_lds + r * ST::kRowBytes + w * 16) = coder.codes(held[u][0], held[u][1]);
+      for (int u = 0; u < kLoads; ++u) *place(u) = coder.codes8<true>(held[u]);
+    } else {  // (rare: rolled up, from memory again, so that it takes no registers of the other)
+#pragma unroll 1
+      for (int u = 0; u < kLoads; ++u) *place(u) = coder.codes8<false>(load_row(p0, u));
     }
-    __syncthreads();
-    i32x4 qf[ST::kRowTiles][D / 32];
+    i32x4 kf[D / 32], next[D / 32];
+    load_block(next, 0);
+    wave_lds_exchange();
+    i32x4 qf[ST::kTiles][D / 32];
 #pragma unroll
-    for (int t = 0; t < ST::kRowTiles; ++t)
+    for (int t = 0; t < ST::kTiles; ++t)
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk)
-        qf[t][kk] = *(const i32x4*)(rows_lds + (min(t, tiles - 1) * 32 + col) * ST::kRowBytes + kk * 32 + half * 16);
-    for (int t0 = wave * 32; t0 < n; t0 += kSelThreads / 64 * 32) {
-      const int j = min(t0 + col, n - 1);
-      const int8_t* cp = a.codes + ((blk0 + j) * a.Hkv + g) * D + half * 16;
-      i32x4 kf[D / 32];
+        qf[t][kk] = *(const i32x4*)(mine + (t * 32 + col) * ST::kRowBytes + kk * 32 + half * 16);
+    for (int t0 = 0; t0 < n; t0 += 32) {
 #pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) kf[kk] = *(const i32x4*)(cp + kk * 32);
+      for (int kk = 0; kk < D / 32; ++kk) kf[kk] = next[kk];
+      if (t0 + 32 < n) load_block(next, t0 + 32);
       int m = INT32_MIN;
 #pragma unroll
-      for (int t = 0; t < ST::kRowTiles; ++t) {
-        if (t < tiles) {
-          i32x16 acc = i32x16{};
+      for (int t = 0; t < ST::kTiles; ++t) {
+        i32x16 acc = i32x16{};
 #pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk) acc = mfma_i8(qf[t][kk], kf[kk], acc);
-          m = max16(acc, m);
-        }
+        for (int kk = 0; kk < D / 32; ++kk) acc = mfma_i8(qf[t][kk], kf[kk], acc);
+        m = max16(acc, m);
       }
       m = max(m, __shfl_xor(m, 32));
-      if (half == 0 && t0 + col < n) best[t0 + col] = p0 ? max(best[t0 + col], m) : m;
+      if (half == 0 && t0 + col < n) atomicMax(&best[t0 + col], m);
     }
   }
   __syncthreads();
-  uint32_t* const keys = (uint32_t*)best;
-  for (int i = tid; i < n; i += kSelThreads) {
+  auto emit = [&](int rank, int i) { list[rank] = i; };
+  auto key_of = [&](int i) {
     const float score = (float)best[i] * a.scales[(blk0 + i) * a.Hkv + g];
-    keys[i] = i < a.n_sink || i >= n - a.n_recent ? kForced : order_bits(score);
+    return i < a.n_sink || i >= n - a.n_recent ? kForced : order_bits(score);
+  };
+  if (n <= 64 * kWaveKeys) {
+    if (wave) return;
+    uint32_t x[kWaveKeys];
+#pragma unroll
+    for (int s = 0; s < kWaveKeys; ++s) x[s] = s * 64 + lane < n ? key_of(s * 64 + lane) : kAbsent;
+    select_wave(x, n, a.top_k, emit);
+    return;
   }
+  uint32_t* const keys = (uint32_t*)best;
+  for (int i = tid; i < n; i += kSelThreads) keys[i] = key_of(i);
   __syncthreads();
   select_top(
       topk, n, a.top_k,
@@ -504,7 +607,7 @@ __global__ __launch_bounds__(kSelThreads, 2) void select_blocks_kernel(SelectArg
           f(s, i, i < n ? keys[i] : kAbsent);
         }
       },
-      [&](int rank, int i) { list[rank] = i; });
+      emit);
 }
 
 // ------------------------------------------------- decode: a list per query token
@@ -519,9 +622,9 @@ struct Token {
   int b, s, pos;
   int64_t t;  // row of q
 };
-__device__ __forceinline__ bool token_of(const SelectArgs& a, int64_t item, Token* x) {
-  x->b = (int)(item / a.N);
-  const int i = (int)(item % a.N);
+__device__ __forceinline__ bool token_of(const SelectArgs& a, uint32_t item, Token* x) {
+  x->b = (int)(item / (uint32_t)a.N);
+  const int i = (int)(item - (uint32_t)x->b * (uint32_t)a.N);
   const int64_t base = a.cu ? a.cu[x->b] : (int64_t)x->b * a.N;
   const int m = min(a.cu ? a.cu[x->b + 1] - a.cu[x->b] : a.N, a.N);
   if (i >= m) return false;
@@ -534,12 +637,13 @@ __device__ __forceinline__ bool token_of(const SelectArgs& a, int64_t item, Toke
 // The codes of the token's rows are made once per workgroup, through LDS, while the
 // first pages' codes are on their way.
 template <int D>
-__global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) {
-  constexpr int kPer = kScoreTiles / (kSelThreads / 64);  // tiles of a wave
-  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * SelTiles<D>::kRowBytes];
+__global__ __launch_bounds__(kScoreThreads) void score_pages_kernel(SelectArgs a) {
+  constexpr int kPer = kScoreTiles / (kScoreThreads / 64);  // tiles of a wave
+  constexpr int kRowBytes = D + 16;  // padded against bank conflicts
+  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * kRowBytes];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31, wave = tid >> 6;
   const int G = a.Hq / a.Hkv;
-  const int64_t item = blockIdx.x / (unsigned)a.Hkv;
+  const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
   Token tk;
   if (!token_of(a, item, &tk)) return;
@@ -551,9 +655,9 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
   uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   int page[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) page[i] = row[min(t0 + (i * (kSelThreads / 64) + wave) * 32 + col, n - 1)];
-  float top = 0.f;
-  for (int c = lane; c < G * (D / 8); c += 64) top = fmaxf(top, abs_max8(*(const u32x4*)(q0 + c * 8)));
+  for (int i = 0; i < kPer; ++i) page[i] = row[min(t0 + (i * (kScoreThreads / 64) + wave) * 32 + col, n - 1)];
+  u16x2 most = {0, 0};
+  for (int c = lane; c < G * (D / 8); c += 64) most = max_bits(most, *(const u32x4*)(q0 + c * 8));
   float scale[kPer];
   i32x4 kf[kPer][D / 32];
 #pragma unroll
@@ -564,22 +668,21 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
     for (int kk = 0; kk < D / 32; ++kk) kf[i][kk] = *(const i32x4*)(cp + kk * 32);
     scale[i] = a.scales[e * a.Hkv + g];
   }
-  const Coder coder(wave_fmax(top));
+  const Coder coder(wave_top(most));
   int m[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) m[i] = INT32_MIN;
   for (int u = 0; u < G; u += 32) {  // (more than one turn for more than 32 heads only)
     if (u) __syncthreads();
     // (rows past the last repeat it, which changes no maximum)
-    for (int c = tid; c < 32 * (D / 16); c += kSelThreads) {
-      const u32x4* p = (const u32x4*)(q0 + min(u + c / (D / 16), G - 1) * D + c % (D / 16) * 16);
-      *(i32x4*)(rows_lds + c / (D / 16) * SelTiles<D>::kRowBytes + c % (D / 16) * 16) = coder.codes(p[0], p[1]);
-    }
+    for (int c = tid; c < 32 * (D / 8); c += kScoreThreads)
+      *(uint2*)(rows_lds + c / (D / 8) * kRowBytes + c % (D / 8) * 8) =
+          coder.codes(*(const u32x4*)(q0 + min(u + c / (D / 8), G - 1) * D + c % (D / 8) * 8));
     __syncthreads();
     i32x4 qf[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk)
-      qf[kk] = *(const i32x4*)(rows_lds + col * SelTiles<D>::kRowBytes + kk * 32 + half * 16);
+      qf[kk] = *(const i32x4*)(rows_lds + col * kRowBytes + kk * 32 + half * 16);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       i32x16 acc = i32x16{};
@@ -591,7 +694,7 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     m[i] = max(m[i], __shfl_xor(m[i], 32));
-    const int j = t0 + (i * (kSelThreads / 64) + wave) * 32 + col;
+    const int j = t0 + (i * (kScoreThreads / 64) + wave) * 32 + col;
     if (half == 0 && j < n) {
       // (a page that the table does not name comes last: nothing of it is attended to)
       const uint32_t key = (unsigned)page[i] < (unsigned)a.P ? order_bits((float)m[i] * scale[i]) : kAbsent;
@@ -600,15 +703,15 @@ __global__ __launch_bounds__(kSelThreads) void score_pages_kernel(SelectArgs a) 
   }
 }
 
-// Workgroups of 256 threads take up to 4096 candidates, whose keys they hold in
-// registers, 1024 up to 16384 likewise, and more from memory: barriers of four waves
-// cost less than those of sixteen.
+// One wavefront takes up to 1024 candidates.  Workgroups of 256 threads take up to 4096,
+// whose keys they hold in registers, 1024 up to 16384 likewise, and more from memory:
+// barriers of four waves cost less than those of sixteen.
 constexpr int kPickHeld = 16;  // keys per thread held in registers
 template <int NT, bool HELD>
 __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
-  __shared__ TopK<NT, HELD ? NT * kPickHeld : kMaxCandPages> topk;
+  __shared__ std::conditional_t<NT == 64, char, TopK<NT == 64 ? 256 : NT, HELD ? NT * kPickHeld : kMaxCandPages>> topk;
   const int tid = threadIdx.x;
-  const int64_t item = blockIdx.x / (unsigned)a.Hkv;
+  const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
   Token tk;
   if (!token_of(a, item, &tk)) return;
@@ -617,7 +720,12 @@ __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
   for (int i = min(n, a.top_k) + tid; i < a.top_k; i += NT) list[i] = -1;
   const uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   auto emit = [&](int rank, int i) { list[rank] = i; };
-  if constexpr (HELD) {
+  if constexpr (NT == 64) {
+    uint32_t x[kWaveKeys];
+#pragma unroll
+    for (int s = 0; s < kWaveKeys; ++s) x[s] = s * 64 + tid < n && n > a.top_k ? keys[s * 64 + tid] : kAbsent;
+    select_wave(x, n, a.top_k, emit);
+  } else if constexpr (HELD) {
     uint32_t x[kPickHeld];
     if (n > a.top_k) {
 #pragma unroll
@@ -661,10 +769,10 @@ hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t s) {
   const size_t head = (sizeof(BlockTopK) + 15) / 16 * 16;
   if (a.d == 128)
     hipLaunchKernelGGL(select_blocks_kernel<128>, grid, dim3(kSelThreads),
-                       head + SelTiles<128>::kCodeBytes + (size_t)a.max_blocks * 4, s, a);
+                       head + SelTiles<128>::kBytes + (size_t)a.max_blocks * 4, s, a);
   else
     hipLaunchKernelGGL(select_blocks_kernel<64>, grid, dim3(kSelThreads),
-                       head + SelTiles<64>::kCodeBytes + (size_t)a.max_blocks * 4, s, a);
+                       head + SelTiles<64>::kBytes + (size_t)a.max_blocks * 4, s, a);
   return hipGetLastError();
 }
 
@@ -673,12 +781,14 @@ hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s) {
   if (a.max_blocks > a.top_k) {
     const dim3 grid((unsigned)items, (unsigned)((a.max_blocks + kScoreTiles * 32 - 1) / (kScoreTiles * 32)));
     if (a.d == 128)
-      hipLaunchKernelGGL(score_pages_kernel<128>, grid, dim3(kSelThreads), 0, s, a);
+      hipLaunchKernelGGL(score_pages_kernel<128>, grid, dim3(kScoreThreads), 0, s, a);
     else
-      hipLaunchKernelGGL(score_pages_kernel<64>, grid, dim3(kSelThreads), 0, s, a);
+      hipLaunchKernelGGL(score_pages_kernel<64>, grid, dim3(kScoreThreads), 0, s, a);
   }
   const dim3 grid((unsigned)items);
-  if (a.max_blocks <= 256 * kPickHeld)
+  if (a.max_blocks <= 64 * kWaveKeys)
+    hipLaunchKernelGGL((pick_pages_kernel<64, true>), grid, dim3(64), 0, s, a);
+  else if (a.max_blocks <= 256 * kPickHeld)
     hipLaunchKernelGGL((pick_pages_kernel<256, true>), grid, dim3(256), 0, s, a);
   else if (a.max_blocks <= 1024 * kPickHeld)
     hipLaunchKernelGGL((pick_pages_kernel<1024, true>), grid, dim3(1024), 0, s, a);

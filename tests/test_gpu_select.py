@@ -152,6 +152,34 @@ def test_select_pages(Hq, Hkv, d, top_k, few):
                 assert got[c.cu[b] + i, g].tolist() == want + [-1] * (top_k - len(want)), (b, g, i)
 
 
+@pytest.mark.parametrize("bits", [0x3FFE, 0x3F80, 0x3FFF, 0x4055, 0x0100, 0x7F7E, 0x7F7F, 0x0002, 0x8000, 0xC07E])
+def test_query_codes_on_every_border(bits):
+    """Token t's row holds a largest value in channel 0 and in channel 1 the t-th of all bf16 magnitudes
+    from there down by ten octaves, with either sign: ties among them, many where the largest has the
+    significand 254.  Of its two pages the first scores c times the code of channel 0, the second 127
+    times that of channel 1, so the choice for c around the expected code tells it."""
+    from paper_2505_11254_amd import binding
+    top = torch.tensor([bits], dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    most = bits & 0x7FFF
+    rows = torch.arange(max(0, most - 1400), most + 1).to(torch.int16).view(torch.bfloat16)
+    T = len(rows)
+    rows = torch.where(torch.arange(T) % 2 == 0, rows, -rows)
+    q = torch.zeros((T, 1, 64), dtype=torch.bfloat16)
+    q[:, 0, 0], q[:, 0, 1] = top, rows
+    a = top.double().abs()
+    code = (torch.round(q[:, 0, :2].double() * 127 / a) if float(a) else q[:, 0, :2].double() * 0).long()
+    table = torch.arange(3 * T, dtype=torch.int32).view(T, 3)
+    L = torch.full((T,), 2 * PAGE + 1, dtype=torch.int32)
+    for off in (-1, 0, 1):
+        c = (code[:, 1] * code[:, 0].sign() + off).clamp(-127, 127)
+        pages = torch.zeros((T, 3, 1, 64), dtype=torch.int8)
+        pages[:, 0, 0, 0], pages[:, 1, 0, 1] = c.to(torch.int8), 127
+        got = binding.select_pages(q.cuda(), pages.view(3 * T, 1, 64).cuda(), torch.ones((3 * T, 1)).cuda(), table.cuda(),
+                                   L.cuda(), top_k=1, n_sink=0, n_recent=0, B=T).cpu()[:, 0, 0]
+        want = (c * code[:, 0] < 127 * code[:, 1]).long()  # (ties go to the first)
+        assert torch.equal(got.long(), want), off
+
+
 @pytest.mark.parametrize("n_pages,top_k", [(3000, 128), (20000, 64), (2049, 2048)])
 def test_select_pages_of_long_sequences(n_pages, top_k):
     """Far more candidates than one stripe of the selection, with codes drawn at random, so that no keys are

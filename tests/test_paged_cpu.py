@@ -124,12 +124,14 @@ def test_the_arguments_above_are_good(lib, fn):
 
 
 def test_workspaces_that_are_too_small(lib):
-    for fn, need in (("tree_attn_paged", binding.paged_workspace_bytes(2, 3, 8, 2, 128, 512)),
-                     ("selected_attn_paged", binding.paged_workspace_bytes(2, 3, 8, 2, 128, 1, 4))):
-        a = dict(ARGS[fn], size=need - 1)
+    for fn, more, need in (("tree_attn_paged", dict(M=5000, max_len=300000), binding.paged_workspace_bytes(2, 3, 8, 2, 128, 300000)),
+                           ("selected_attn_paged", dict(top_k=100), binding.paged_workspace_bytes(2, 3, 8, 2, 128, 1, 100))):
+        a = dict(ARGS[fn], **{**more, "size": need - 1})  # (keeps the order of the arguments)
         assert need > 0 and getattr(lib, fn)(*a.values()) == WORKSPACE
         a["size"], a["ws"] = need, None
         assert getattr(lib, fn)(*a.values()) == WORKSPACE
+    # few pages: no rows are cut, nothing is needed
+    assert binding.paged_workspace_bytes(2, 3, 8, 2, 128, 512) == binding.paged_workspace_bytes(2, 3, 8, 2, 128, 1, 4) == 0
 
 
 @pytest.mark.parametrize("B,N,Hq,Hkv,d", [(1, 1, 32, 8, 128), (64, 1, 32, 8, 128), (3, 64, 64, 8, 128), (1, 1, 8, 1, 64),
@@ -138,9 +140,9 @@ def test_workspaces_of_any_length_are_bounded(lib, B, N, Hq, Hkv, d):
     """At most two tiles of partial results for each workgroup that runs at once, and a count per sequence."""
     most = 768 * 2 * 256 * (d + 2) * 4 + 4 * B + 512
     for n in (1, 64, 100, 1000, 10 ** 4, 10 ** 5, 10 ** 6):
-        assert 0 < binding.paged_workspace_bytes(B, N, Hq, Hkv, d, n) <= most
+        assert 0 <= binding.paged_workspace_bytes(B, N, Hq, Hkv, d, n) <= most
     for k in (1, 8, 64, 500):
-        assert 0 < binding.paged_workspace_bytes(B, N, Hq, Hkv, d, 1, k) <= most
+        assert 0 <= binding.paged_workspace_bytes(B, N, Hq, Hkv, d, 1, k) <= most
     assert binding.paged_workspace_bytes(0, N, Hq, Hkv, d, 64) == 0
     assert binding.paged_workspace_bytes(B, N, Hq, Hkv, 80, 64) == 0
     assert binding.paged_workspace_bytes(50000, 1, 64, 64, 64, 1 << 30) == 0  # more pages than are counted
