@@ -127,10 +127,12 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
 // histogram of kBins equal steps between them (in LDS, by atomics; steps of a range
 // that fits the keys spread them, where their leading bits alone would pile them up on
 // few counters), and the step that the count from above ends in, until that step holds
-// one value or just as many keys as are chosen.  32-bit keys need at most three
-// rounds of 2048 steps, scores two as a rule.  Then one pass ranks the chosen ones in
-// ascending order: stripes of NT keys, each wave's counts in a table, a prefix sum
-// over (stripe, wave).  Thread tid owns keys tid, tid + NT, ...; each(f) calls
+// one value or just as many keys as are chosen.  The first round's steps are of the
+// scores themselves; where its step holds 64 keys or fewer, as a rule, one wave ranks
+// those and there is no second round (8000 keys: 19.0 us against 20.3, scores included).
+// Then one pass ranks the chosen ones in ascending order: stripes of NT keys, each wave's
+// counts in a table, a prefix sum over (stripe, wave).  Thread tid owns keys tid,
+// tid + NT, ...; each(f) calls
 // f(stripe, index, key) for those of all stripes, index >= n where there is none.
 // emit(rank, index) is called once per chosen key.
 constexpr uint32_t kForced = 0xffffffffu;  // always chosen (never more than top_k are)
@@ -156,7 +158,9 @@ struct TopK {
   int scan[3][kWaves];
   uint32_t ends[2][kWaves];
   uint32_t bin;
-  int need, all;
+  int need, all, held;       // of the step that was found, and how many keys it holds
+  uint32_t list[2][64], cut[2];  // its keys and their places; the last chosen one
+  int listed;
 };
 
 template <int NT, int MAX, typename Each, typename Emit>
@@ -177,7 +181,7 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
   auto lin_step = [&](uint32_t x) { return (uint32_t)((order_float(x) - f0) * per_step); };
   int need = top_k;
   uint32_t bin = 0;
-  bool all = false;
+  bool all = false, cut = false;  // cut: t.cut is the last chosen key
   for (int round = 0;; ++round) {
     uint32_t mn = ~0u, mx = 0;
     int forced = 0, members = 0;
@@ -261,6 +265,8 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
           t.bin = TK::kBins - 1 - TK::kPer * tid - j;
           t.need = need - before;
           t.all = before + c[j] == need;
+          t.held = c[j];
+          t.listed = 0;
         }
         before += c[j];
       }
@@ -269,6 +275,33 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     need = t.need;
     bin = t.bin;
     all = t.all;
+    if (lin && t.held <= 64) {
+      // One wave ranks the step's keys: the need-th of them is the last one chosen.
+      each([&](int, int i, uint32_t x) {
+        if (i < n && x >= lo && x <= hi && lin_step(x) == bin) {
+          const int at = atomicAdd(&t.listed, 1);
+          t.list[0][at] = x;
+          t.list[1][at] = i;
+        }
+      });
+      __syncthreads();
+      if (wave == 0) {
+        const int m = t.held;
+        const uint32_t key = lane < m ? t.list[0][lane] : 0u, at = lane < m ? t.list[1][lane] : ~0u;
+        int rank = 0;
+        for (int j = 0; j < m; ++j) {
+          const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key, j), i = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
+          rank += k > key || (k == key && i < at);
+        }
+        if (lane < m && rank == need - 1) {
+          t.cut[0] = key;
+          t.cut[1] = at;
+        }
+      }
+      __syncthreads();
+      cut = true;
+      break;
+    }
     if (lin) continue;  // the step's keys: those whose score falls into it
     lo = mn + (bin << sh);
     if (all) {
@@ -279,9 +312,18 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     if (sh == 0) break;
     hi = lo + min(mx - lo, (1u << sh) - 1u);
   }
-  // keys above lo are chosen, and the first `need` equal to it
+  // Keys above lo are chosen, and the first `need` equal to it (with `cut`, those up to
+  // place cut_at), in ascending order of their places.
+  uint32_t cut_at = 0;
+  if (cut) {
+    lo = t.cut[0];
+    cut_at = t.cut[1];
+    need = 0;
+  }
+  auto is_above = [&](int i, uint32_t x) { return i < n && (x > lo || (cut && x == lo && (uint32_t)i <= cut_at)); };
+  auto is_same = [&](int i, uint32_t x) { return !cut && i < n && x == lo; };
   each([&](int s, int i, uint32_t x) {
-    const uint64_t above = __ballot(i < n && x > lo), same = __ballot(i < n && x == lo);
+    const uint64_t above = __ballot(is_above(i, x)), same = __ballot(is_same(i, x));
     if (lane == 0) {
       t.table[0][s * W + wave] = __popcll(above);
       t.table[1][s * W + wave] = __popcll(same);
@@ -319,35 +361,53 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     }
   }
   __syncthreads();
+  const uint64_t lower = (1ull << lane) - 1;
   each([&](int s, int i, uint32_t x) {
-    const bool above = i < n && x > lo, same = i < n && x == lo;
-    const uint64_t lower = (1ull << lane) - 1;
-    const int na = t.table[0][s * W + wave] + __popcll(__ballot(above) & lower);
-    const int ns = t.table[1][s * W + wave] + __popcll(__ballot(same) & lower);
+    const bool above = is_above(i, x), same = is_same(i, x);
+    const uint64_t ups = __ballot(above), sames = __ballot(same);
+    if (!(ups | sames)) return;
+    const int na = t.table[0][s * W + wave] + __popcll(ups & lower);
+    const int ns = t.table[1][s * W + wave] + __popcll(sames & lower);
     if (above || (same && ns < need)) emit(na + min(ns, need), i);
   });
 }
 
 // The same by one wavefront for at most 64 RK keys, which it holds in registers (key s *
-// 64 + lane in x[s], 0 past the last): the smallest chosen key bit by bit, counting the
-// keys that are as large by ballots, without LDS or barriers.  Ends early where just
-// top_k keys are as large.
+// 64 + lane in x[s], kAbsent past the last): the smallest chosen key bit by bit below those
+// that all keys share, counting the keys that are as large by ballots, without LDS or
+// barriers.  Ends early where just top_k keys are as large.  (A histogram in LDS, or
+// guesses by interpolation, take a single wave longer: 780 keys 17.2 and 21.5 us against
+// 13.6, scores included.)
 template <int RK, typename Emit>
 __device__ __forceinline__ void select_wave(const uint32_t (&x)[RK], int n, int top_k, Emit emit) {
   const int lane = threadIdx.x & 63;
   auto count = [&](auto holds) {
     int c = 0;
 #pragma unroll
-    for (int s = 0; s < RK; ++s) {
-      if (s * 64 >= n) break;
-      c += __popcll(__ballot(holds(s)));
-    }
+    for (int s = 0; s < RK; ++s) c += __popcll(__ballot(holds(s)));  // (never true of absent keys below)
     return c;
   };
   uint32_t least = 0;
   int above = 0;  // keys above it that are chosen
   bool exact = n <= top_k;
-  for (int bit = 31; bit >= 0 && !exact; --bit) {
+  int bit = 31;
+  if (!exact) {
+    uint32_t mn = kForced, mx = kAbsent;  // of the keys that are neither forced nor absent
+#pragma unroll
+    for (int s = 0; s < RK; ++s) {
+      const bool in = x[s] != kForced && x[s] != kAbsent;
+      mn = in ? min(mn, x[s]) : mn;
+      mx = in ? max(mx, x[s]) : mx;
+    }
+    mn = (uint32_t)wave_reduce((int)mn, -1, [](int p, int q) { return (int)min((uint32_t)p, (uint32_t)q); });
+    mx = (uint32_t)wave_reduce((int)mx, 0, [](int p, int q) { return (int)max((uint32_t)p, (uint32_t)q); });
+    // the bits that all of them share are the key's, unless it is a forced or an absent one
+    if (count([&](int s) { return x[s] > mx; }) < top_k && count([&](int s) { return x[s] >= mn; }) >= top_k) {
+      bit = 31 - __clz((int)(mn ^ mx));  // (-1 for a single value)
+      least = bit < 0 ? mn : bit == 31 ? 0u : mn & ~((2u << bit) - 1u);
+    }
+  }
+  for (; bit >= 0 && !exact; --bit) {
     const uint32_t t = least | 1u << bit;
     const int c = count([&](int s) { return x[s] >= t; });
     if (c >= top_k) least = t;
@@ -359,7 +419,6 @@ __device__ __forceinline__ void select_wave(const uint32_t (&x)[RK], int n, int 
   const uint64_t lower = (1ull << lane) - 1;
 #pragma unroll
   for (int s = 0; s < RK; ++s) {
-    if (s * 64 >= n) break;
     const bool in = s * 64 + lane < n;
     const bool up = in && (exact ? x[s] >= least : x[s] > least), same = in && !exact && x[s] == least;
     const uint64_t ups = __ballot(up), sames = __ballot(same);
@@ -369,7 +428,29 @@ __device__ __forceinline__ void select_wave(const uint32_t (&x)[RK], int n, int 
     same_before += __popcll(sames);
   }
 }
-constexpr int kWaveKeys = 16;  // per lane
+
+// One wavefront alone takes up to 64 keys times this, with as few registers of them as n
+// needs; key(i) is that of place i < n.
+constexpr int kWaveKeys = 16;
+template <typename Key, typename Emit>
+__device__ __forceinline__ void select_few(int n, int top_k, Key key, Emit emit) {
+  const int lane = threadIdx.x & 63;
+  auto run = [&](auto keys) {
+    constexpr int RK = decltype(keys)::value;
+    uint32_t x[RK];
+#pragma unroll
+    for (int s = 0; s < RK; ++s) x[s] = s * 64 + lane < n ? key(s * 64 + lane) : kAbsent;
+    select_wave(x, n, top_k, emit);
+  };
+  if (n <= 128)
+    run(std::integral_constant<int, 2>{});
+  else if (n <= 256)
+    run(std::integral_constant<int, 4>{});
+  else if (n <= 512)
+    run(std::integral_constant<int, 8>{});
+  else
+    run(std::integral_constant<int, kWaveKeys>{});
+}
 
 // Codes round(127 x / top) of a group's queries, top its largest magnitude, ties to even.
 // With bf16 significands a and b of x and top, 128 to 255, the quotient is 127 a / (b 2^e).
@@ -445,8 +526,9 @@ constexpr int kScoreThreads = 256;
 // neighbouring chunks, and their codes pass through the wave's part of LDS into the
 // operand's layout.  (Loaded straight into that layout, each instruction took 16 bytes
 // of each of 64 lines, which the L1 cache did not keep for the next one: 52 us with
-// 16384 tokens, 32 heads on 8.)  More rows take further passes.  Bound by the queries, which are read once, and by the
-// selection; of the products there are 8 MFMAs per wave and 32 blocks.
+// 16384 tokens, 32 heads on 8, against 45 to 49.)  More rows take further passes.  Bound by the
+// queries, which are read once, and by the selection; of the products there are 8 MFMAs per
+// wave and 32 blocks.
 template <int D>
 struct SelTiles {
   static constexpr int kTiles = 256 / D;     // row tiles of a wave (32 registers of codes)
@@ -590,10 +672,7 @@ __global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArg
   };
   if (n <= 64 * kWaveKeys) {
     if (wave) return;
-    uint32_t x[kWaveKeys];
-#pragma unroll
-    for (int s = 0; s < kWaveKeys; ++s) x[s] = s * 64 + lane < n ? key_of(s * 64 + lane) : kAbsent;
-    select_wave(x, n, a.top_k, emit);
+    select_few(n, a.top_k, key_of, emit);
     return;
   }
   uint32_t* const keys = (uint32_t*)best;
@@ -721,10 +800,7 @@ __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
   const uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   auto emit = [&](int rank, int i) { list[rank] = i; };
   if constexpr (NT == 64) {
-    uint32_t x[kWaveKeys];
-#pragma unroll
-    for (int s = 0; s < kWaveKeys; ++s) x[s] = s * 64 + tid < n && n > a.top_k ? keys[s * 64 + tid] : kAbsent;
-    select_wave(x, n, a.top_k, emit);
+    select_few(n, a.top_k, [&](int i) { return n > a.top_k ? keys[i] : kAbsent; }, emit);
   } else if constexpr (HELD) {
     uint32_t x[kPickHeld];
     if (n > a.top_k) {
