@@ -160,7 +160,7 @@ def merge_bytes(wl, cover):
 
 def kernel_source_hash():
     h = hashlib.sha256()
-    for f in ("da_kernels.hip", "da_api.cpp", "da_internal.hpp"):
+    for f in ("da_kernels.hip", "da_device.hpp", "da_api.cpp", "da_internal.hpp"):
         with open(os.path.join(ROOT, "paper_2505_11254_amd", "csrc", f), "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
