@@ -396,7 +396,10 @@ da_status da_launch_workgroups(int B, int max_seqlen, int packed, int Hq, int Hk
  * sequence as in the prefill calls; rows of a sequence past max_seqlen are ignored.
  * Other conventions (streams, validation, errors) are those above; integer arrays
  * are 4-byte aligned, `result` of resize and compact 16-byte.  Only bf16, d 64 or
- * 128, any Hq / Hkv.
+ * 128, any Hq / Hkv.  Launches have at most 2^32 - 1 threads: of 256 per kv head of a page
+ * that may be copied or compacted (n * layers * 2 * Hkv), of a query block, of 4 pages to
+ * be summarised, of 8 query heads of new tokens, of 16 KB to be appended, and of a token to
+ * select pages for (1024 there with max_len over 262,208); more is DA_ERR_SHAPE.
  */
 #define DA_PAGE_TOKENS 64
 #define DA_PAGES_MAX_REQUESTS 1024
@@ -431,7 +434,7 @@ da_status da_pages_resize(void* k_pages, void* v_pages, int layers, int Hkv, int
 /*
  * Writes the keys and values k, v [layers, T, Hkv, d] of new tokens as the last ones of
  * their slots, which da_pages_resize has made room for: row i of the m rows of
- * sequence b goes to token lens[slot] - m + i.
+ * sequence b goes to token lens[slot] - m + i.  k and v lie outside the pages.
  */
 da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
                           int layers, int Hkv, int d, const int32_t* table, const int32_t* lens,
@@ -446,7 +449,8 @@ da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages
  * result [n, 4]: {tokens kept from start on, ...}, the rest for the call's own use; -1: a
  * slot out of range or named before, a start outside the slot, places that do not
  * ascend or lie outside it, offsets outside [0, n_keep], or a page that would be
- * written while another slot holds it.
+ * written while another slot holds it (pages that the call itself gives back are
+ * held until its end).
  */
 da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, int d,
                            int32_t* table, int32_t* lens, int32_t* refs, int S, int M, int P,
@@ -508,7 +512,8 @@ da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* ta
  * block.  Writes lists for blocksparse_attn_prefill and
  * delta_attn_prefill_blocksparse: block_ptr [B, Hkv, ceil(max_seqlen / block_q) + 1]
  * and block_idx of da_select_blocks_entries(B, max_seqlen, Hkv, top_k, block_q) entries
- * (-1 where a shorter sequence has no lists; may be 0).  Up to 1,572,864 tokens.
+ * (-1 where a shorter sequence has no lists; may be 0).  Up to 1,572,864 tokens, and
+ * query blocks below 4 GiB.
  *
  * da_select_pages (decode): a group is one token in the heads of one kv head, its
  * candidates the pages before the token's own.  Writes page positions (indices into

@@ -628,7 +628,7 @@ def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_ke
     return result
 
 
-def _queries(q, out, lse, Hkv, d, on):
+def _queries(q, k_pages, v_pages, out, lse, Hkv, d, on):
     _halves("q", q, on.dev)
     if q.dim() != 3 or q.shape[2] != d or q.shape[1] % Hkv:
         raise ValueError(f"q must be [T, Hq, {d}] with Hq a multiple of {Hkv}")
@@ -639,9 +639,10 @@ def _queries(q, out, lse, Hkv, d, on):
         if out.shape != q.shape:
             raise ValueError(f"out must have the shape of q {tuple(q.shape)}")
         o0, o1 = _span(out)
-        t0, t1 = _span(q)
-        if o0 < t1 and t0 < o1:
-            raise ValueError("out must not overlap q")
+        for name, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages)):
+            t0, t1 = _span(t)
+            if o0 < t1 and t0 < o1:
+                raise ValueError(f"out must not overlap {name}")
     if lse is not None:
         _on_device("lse", lse, on.dev, torch.float32)
         if tuple(lse.shape) != tuple(q.shape[:2]):
@@ -664,7 +665,7 @@ def tree_attn_paged(q, k_pages, v_pages, table, lens, *, mask=None, slots=None, 
     dev, _, P, Hkv, d = _pages(k_pages, v_pages)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
-    out = _queries(q, out, lse, Hkv, d, on)
+    out = _queries(q, k_pages, v_pages, out, lse, Hkv, d, on)
     T, Hq = q.shape[:2]
     B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
     words = 0
@@ -689,7 +690,7 @@ def selected_attn_paged(q, k_pages, v_pages, table, lens, pages, *, slots=None, 
     dev, _, P, Hkv, d = _pages(k_pages, v_pages)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
-    out = _queries(q, out, lse, Hkv, d, on)
+    out = _queries(q, k_pages, v_pages, out, lse, Hkv, d, on)
     T, Hq = q.shape[:2]
     B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
     _ints("pages", pages, dev)

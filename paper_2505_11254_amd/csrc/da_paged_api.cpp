@@ -10,6 +10,9 @@ namespace {
 
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// Whether a launch can have so many workgroups: its threads are counted in 32 bits.
+bool fits(int64_t wgs, int threads) { return wgs <= (int64_t)UINT32_MAX / threads; }
+
 da_status check_table(const Table& t) {
   if (!t.table || !t.lens) return DA_ERR_NULL;
   if (t.S < 1 || t.M < 1 || t.P < 1) return DA_ERR_SHAPE;
@@ -33,10 +36,13 @@ da_status check_batch(int B, int N, int Hq, int Hkv, int d) {
   if (d != 64 && d != 128) return DA_ERR_UNSUPPORTED;
   return DA_OK;
 }
-// The same where a workgroup or a partial result goes with each of its rows.
+// The same where a workgroup or a partial result goes with each of its rows (256 threads
+// merge eight of them).
 da_status check_rows(int B, int N, int Hq, int Hkv, int d) {
   const da_status st = check_batch(B, N, Hq, Hkv, d);
-  return st == DA_OK && (int64_t)B * N * Hq > INT32_MAX ? DA_ERR_SHAPE : st;
+  if (st != DA_OK) return st;
+  const int64_t tokens = (int64_t)B * N;
+  return tokens > INT32_MAX || tokens * Hq > INT32_MAX || !fits((tokens * Hq + 7) / 8, 256) ? DA_ERR_SHAPE : DA_OK;
 }
 
 da_status launched(hipError_t e) { return e == hipSuccess ? DA_OK : fail_hip(e); }
@@ -80,8 +86,9 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   // (lengths below the longest are taken to make four fifths of the work)
   const double rounds = (double)segs / (double)slots;
   p->row_tiles = rt;
-  p->whole = (seg_us < 12. && rounds >= 0.25) ||
-             seg_us * (double)((segs + slots - 1) / slots) < 0.8 * seg_us * rounds + kCutUs[c];
+  p->whole = fits(segs, 512) &&
+             ((seg_us < 12. && rounds >= 0.25) ||
+              seg_us * (double)((segs + slots - 1) / slots) < 0.8 * seg_us * rounds + kCutUs[c]);
   if (p->whole) {
     p->min_units = 1;
     p->n_wgs = (int)segs;
@@ -170,7 +177,8 @@ da_status da_pages_resize(void* k_pages, void* v_pages, int layers, int Hkv, int
   if (st != DA_OK) return st;
   st = check_pages(k_pages, v_pages, layers, Hkv, d);
   if (st != DA_OK) return st;
-  if (n < 1 || n > kMaxRequests || (int64_t)n * layers * 2 * Hkv > INT32_MAX) return DA_ERR_SHAPE;
+  if (n < 1 || n > kMaxRequests || Hkv > INT32_MAX / 2 / n / layers || !fits((int64_t)n * layers * 2 * Hkv, 256))
+    return DA_ERR_SHAPE;
   if (!aligned(slots, 4) || !aligned(new_lens, 4) || !aligned(result, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
@@ -192,7 +200,7 @@ da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages
   if (!cu_seqlens && (int64_t)B * max_seqlen != T) return DA_ERR_SHAPE;
   // chunks of 16 bytes per sequence and layer, and workgroups of at least 1024 of them
   const int64_t chunks = (int64_t)max_seqlen * Hkv * (d / 8);
-  if (chunks > INT32_MAX || (chunks / 1024 + 1) * B > INT32_MAX) return DA_ERR_SHAPE;
+  if (chunks > INT32_MAX || !fits((chunks / 1024 + 1) * B, 256)) return DA_ERR_SHAPE;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cu_seqlens, 4)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
@@ -211,7 +219,9 @@ da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, in
   if (st != DA_OK) return st;
   st = check_pages(k_pages, v_pages, layers, Hkv, d);
   if (st != DA_OK) return st;
-  if (n < 1 || n > kMaxRequests || n_keep < 0 || (int64_t)n * layers * 2 * Hkv > INT32_MAX) return DA_ERR_SHAPE;
+  if (n < 1 || n > kMaxRequests || n_keep < 0 || Hkv > INT32_MAX / 2 / n / layers ||
+      !fits((int64_t)n * layers * 2 * Hkv, 256))
+    return DA_ERR_SHAPE;
   if (!aligned(slots, 4) || !aligned(start, 4) || !aligned(keep, 4) || !aligned(cu_keep, 4) ||
       !aligned(result, 16))
     return DA_ERR_ALIGN;
@@ -235,7 +245,7 @@ da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* ta
   // max_new tokens from anywhere in a page on end up to this many pages
   int64_t nblk = pages_of(max_new) + (first ? 1 : 0);
   if (nblk > M) nblk = M;
-  if ((int64_t)B * nblk * Hkv > INT32_MAX) return DA_ERR_SHAPE;
+  if ((int64_t)B * nblk > INT32_MAX || !fits((int64_t)B * nblk * Hkv / 4 + 1, 256)) return DA_ERR_SHAPE;
   st = check_device();
   if (st != DA_OK) return st;
   a.k = (const uint16_t*)k_pages;
@@ -262,7 +272,7 @@ da_status da_key_summary(const void* k, const int32_t* cu_seqlens, int B, int ma
   if (d != 64 && d != 128) return DA_ERR_UNSUPPORTED;
   if (!cu_seqlens && (int64_t)B * max_seqlen > INT32_MAX) return DA_ERR_SHAPE;
   const int64_t nblk = max_seqlen / kPage;
-  if ((int64_t)B * nblk * Hkv > INT32_MAX) return DA_ERR_SHAPE;
+  if ((int64_t)B * nblk > INT32_MAX || !fits((int64_t)B * nblk * Hkv / 4 + 1, 256)) return DA_ERR_SHAPE;
   if (!aligned(k, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(cu_seqlens, 4)) return DA_ERR_ALIGN;
   da_status st = check_device();
   if (st != DA_OK) return st;
@@ -303,7 +313,9 @@ da_status da_select_blocks(const void* q, const void* codes, const float* scales
   if (nqb * block_q / kPage > kMaxCandBlocks) return DA_ERR_UNSUPPORTED;
   const int64_t total = list_total(max_seqlen, top_k, block_q);
   if (total > 0 && da_select_blocks_entries(B, max_seqlen, Hkv, top_k, block_q) == 0) return DA_ERR_SHAPE;
-  if ((int64_t)B * Hkv * (nqb + 1) > INT32_MAX) return DA_ERR_SHAPE;
+  if ((int64_t)B * Hkv > INT32_MAX || !fits((int64_t)B * Hkv * (nqb + 1), 256)) return DA_ERR_SHAPE;
+  // (byte offsets inside a query block are 32-bit)
+  if ((int64_t)block_q * Hq > (int64_t)UINT32_MAX / (2 * d)) return DA_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(cu_seqlens, 4) ||
       !aligned(block_ptr, 4) || !aligned(block_idx, 4))
     return DA_ERR_ALIGN;
@@ -353,7 +365,7 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
   const int64_t room = (int64_t)M * kPage;
   if (max_len > room) max_len = (int)room;
   if (max_len / kPage > kMaxCandPages) return DA_ERR_UNSUPPORTED;
-  if ((int64_t)B * max_seqlen * Hkv * top_k > ((int64_t)1 << 40)) return DA_ERR_SHAPE;
+  if (!fits((int64_t)B * max_seqlen * Hkv, max_len / kPage > 4096 ? 1024 : 256)) return DA_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(cu_seqlens, 4) ||
       !aligned(slots, 4) || !aligned(pages, 4) || !aligned(workspace, 4))
     return DA_ERR_ALIGN;

@@ -110,6 +110,26 @@ def test_calls_refuse_bad_arguments(lib, fn, status, names, value):
         assert getattr(lib, fn)(*args.values()) == status, (name, value)
 
 
+@pytest.mark.parametrize("fn,sizes", [
+    ("da_pages_resize", dict(layers=32767, Hkv=(1 << 31) - 1)),
+    ("da_pages_resize", dict(n=1024, layers=128, Hkv=65)),
+    ("da_pages_compact", dict(n=1024, layers=128, Hkv=65)),
+    ("da_pages_append", dict(B=16, slots=PTR, N=(1 << 27) - 1, Hkv=1)),
+    ("tree_attn_paged", dict(B=4, N=1 << 20, Hq=64, Hkv=64, words=1 << 20)),
+    ("tree_attn_paged", dict(B=4, N=(1 << 31) - 1, Hq=(1 << 31) - 1, Hkv=1, words=1 << 30)),
+    ("selected_attn_paged", dict(B=4, N=1 << 20, Hq=32, Hkv=32)),
+    ("da_key_summary", dict(B=1 << 15, cu=PTR, N=1 << 20, Hkv=1)),
+    ("da_page_summary", dict(B=1 << 26, slots=PTR, max_new=64, Hkv=1)),
+    ("da_select_blocks", dict(B=1 << 20, cu=PTR, N=64, Hkv=8)),
+    ("da_select_blocks", dict(B=1, N=512, Hq=1 << 16, Hkv=1, block_q=256)),
+    ("da_select_pages", dict(B=4, N=1 << 20, Hq=4, Hkv=4)),
+    ("da_select_pages", dict(B=1, N=1 << 20, Hq=4, Hkv=4, M=8192, max_len=8192 * 64)),
+])
+def test_calls_refuse_what_no_launch_can_hold(lib, fn, sizes):
+    """Threads are counted in 32 bits in a launch, byte offsets inside a query block too."""
+    assert getattr(lib, fn)(*dict(ARGS[fn], **sizes).values()) == SHAPE
+
+
 @pytest.mark.parametrize("fn", sorted(ARGS))
 def test_the_arguments_above_are_good(lib, fn):
     """(so that each refusal is that of the one argument that was changed)"""
