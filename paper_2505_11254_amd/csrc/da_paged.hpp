@@ -106,9 +106,10 @@ struct PagedArgs {
   // rows, at least min_units pages each; or, with `whole`, segments (a kv head's rows of
   // a sequence, a workgroup's worth of them) as they are, min_units of them each.
   // Workgroups begin at segments where that costs at most align_pages pages each.
-  int row_tiles, n_wgs, min_units, whole, align_pages;
+  // row_groups: of the sequence with most rows, where workgroups may team up (1: they do not).
+  int row_tiles, n_wgs, min_units, whole, align_pages, row_groups;
   // Workspace (nullptr where no rows are cut)
-  int32_t* units;        // [B + 2] pages before each sequence's, the share, whether aligned
+  int32_t* units;        // [B + 3] pages before each sequence's, the share, whether aligned, team
   float* part_o;         // [n_wgs][2][row_tiles * 32][d] partial results of cut segments
   float* part_ml;        // [n_wgs][2][row_tiles * 32][2]
 };

@@ -66,7 +66,7 @@ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 //    keys 60.5 -> 58.7; eight of 2000 keys, 8 heads on 2, d 64, one token 13.0 -> 10.6.
 constexpr int kAlignPages = 8;
 struct PagedPlan {
-  int row_tiles, n_wgs, min_units, whole, align_pages;
+  int row_tiles, n_wgs, min_units, whole, align_pages, row_groups;
   size_t units_bytes, part_rows, bytes;
 };
 da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
@@ -77,7 +77,8 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   static const int kSlots[2][4] = {{256, 256, 512, 256}, {256, 256, 512, 512}};
   static const double kPageUs[2][4] = {{0.46, 0.9, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
   static const double kCutUs[4] = {4., 6., 8., 25.};
-  const int64_t segs = (n_list ? (int64_t)B * N : B) * Hkv * ((rows + 32 * rt - 1) / (32 * rt));
+  const int64_t groups = (rows + 32 * rt - 1) / (32 * rt);
+  const int64_t segs = (n_list ? (int64_t)B * N : B) * Hkv * groups;
   if (n_list) pages = n_list + 1;
   if (pages < 1) pages = 1;
   if ((double)segs * (double)pages > (double)INT32_MAX) return DA_ERR_SHAPE;
@@ -98,8 +99,9 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
     p->n_wgs = (int)(most < slots ? most : slots);
   }
   p->align_pages = kAlignPages;
+  p->row_groups = !n_list && !p->whole && B <= 64 && groups <= p->n_wgs ? (int)groups : 1;
   p->part_rows = p->whole || p->n_wgs == 1 ? 0 : (size_t)p->n_wgs * 2 * rt * 32;
-  p->units_bytes = p->part_rows ? ((size_t)B + 2 + 63) / 64 * 256 : 0;  // (the merge's alone)
+  p->units_bytes = p->part_rows ? ((size_t)B + 3 + 63) / 64 * 256 : 0;  // (the merge's alone)
   p->bytes = p->units_bytes + p->part_rows * (size_t)(d + 2) * 4;
   return DA_OK;
 }
@@ -142,6 +144,7 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   a.min_units = p.min_units;
   a.whole = p.whole;
   a.align_pages = p.align_pages;
+  a.row_groups = p.row_groups;
   a.units = p.bytes ? (int32_t*)workspace : nullptr;
   a.part_o = (float*)((char*)workspace + p.units_bytes);
   a.part_ml = a.part_o + p.part_rows * a.d;

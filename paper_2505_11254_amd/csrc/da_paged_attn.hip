@@ -86,9 +86,9 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int b, int group
 __device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
   return a.whole ? x.segs : x.segs * x.np;
 }
-// Units per workgroup, of `total`.
-__device__ __forceinline__ int share_of(const PagedArgs& a, int total) {
-  return max(a.min_units, (total + a.n_wgs - 1) / a.n_wgs);
+// Units per workgroup or team, of `total` for n of them.
+__device__ __forceinline__ int share_of(const PagedArgs& a, int total, int n) {
+  return max(a.min_units, (total + n - 1) / n);
 }
 
 template <int D, int RT, bool LISTS>
@@ -128,35 +128,49 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   SeqWork held{};
   int b, off, left;
   bool aligned = false;  // segments begin with workgroups
+  int team = 1;          // workgroups that take one stretch, a row group each
   if (few) {
     if (lane < a.B) held = seq_work<LISTS>(a, lane, RT * 32);
-    const int mine = lane < a.B ? units_of(a, held) : 0;
+    int mine = lane < a.B ? units_of(a, held) : 0;
+    if (!LISTS && a.row_groups > 1) {
+      // The row groups of a kv head read the same pages: workgroups next to each other take
+      // one stretch of them in step and meet in the L2, where sequences with fewer row groups
+      // than others leave at most a sixteenth of the workgroups' time idle.
+      const int columns = lane < a.B && held.segs ? a.Hkv * held.np : 0;
+      if ((int64_t)wave_add(columns) * a.row_groups * 16 <= (int64_t)wave_add(mine) * 17) {
+        team = a.row_groups;
+        held.segs = held.segs ? a.Hkv : 0;
+        mine = columns;
+      }
+    }
+    const int n_wgs = a.n_wgs / team, wt = w / team;
     int upto = wave_scan_add(mine), units = mine;
     int total = __builtin_amdgcn_readlane(upto, 63);
-    int share = share_of(a, total);
+    int share = share_of(a, total, n_wgs);
     if (!a.whole) {
       // Where segments are few against workgroups, whole workgroups go to each: a
       // second segment would cost a workgroup another start, more than the pages that
       // the even share saves.
       const int segs = wave_add(lane < a.B ? held.segs : 0);
-      if (segs < a.n_wgs && (double)total * segs < (double)a.align_pages * a.n_wgs * (a.n_wgs - segs)) {
+      if (segs < n_wgs && (double)total * segs < (double)a.align_pages * n_wgs * (n_wgs - segs)) {
         aligned = true;
-        share = max(a.min_units, (total + a.n_wgs - segs - 1) / (a.n_wgs - segs));
+        share = share_of(a, total, n_wgs - segs);
         units = lane < a.B ? held.segs * ((held.np + share - 1) / share * share) : 0;
         upto = wave_scan_add(units);
         total = __builtin_amdgcn_readlane(upto, 63);
       }
     }
     const int before = upto - units;
-    const int64_t x0 = (int64_t)w * share;
+    const int64_t x0 = (int64_t)wt * share;
     if (w == 0 && tid < 64 && a.units) {  // (for the merge)
       if (lane < a.B) a.units[lane] = before;
       if (lane == 0) {
         a.units[a.B] = share;
         a.units[a.B + 1] = aligned;
+        a.units[a.B + 2] = team;
       }
     }
-    if (x0 >= total) return;
+    if (wt >= n_wgs || x0 >= total) return;
     left = min(share, total - (int)x0);
     b = __builtin_ctzll(__ballot(before <= x0 && x0 < upto));
     off = (int)x0 - __builtin_amdgcn_readlane(before, b);
@@ -186,11 +200,12 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       total += more;
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    const int share = share_of(a, total);
+    const int share = share_of(a, total, a.n_wgs);
     const int64_t x0 = (int64_t)w * share;
     if (w == 0 && tid == 0 && a.units) {
       a.units[a.B] = share;
       a.units[a.B + 1] = 0;
+      a.units[a.B + 2] = 1;
     }
     if (x0 >= total) return;
     left = min(share, total - (int)x0);
@@ -224,8 +239,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
 
   // ---- segment after segment
   while (true) {
-  const int head = sq.n_rg == 1 ? seg : (unsigned)seg / (unsigned)sq.n_rg;
-  const int rg = seg - head * sq.n_rg;
+  const int head = sq.n_rg == 1 || team > 1 ? seg : (unsigned)seg / (unsigned)sq.n_rg;
+  const int rg = team > 1 ? w % team : seg - head * sq.n_rg;
   const int tok = LISTS ? (int)fdiv(head, a.fd_Hkv) : 0;  // the token of a list
   const int g = head - tok * a.Hkv;
   const int p1 = a.whole ? sq.np : min(sq.np, p0 + left);
@@ -269,7 +284,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
 
   // ---- the segment's pages, as many at a time as there is room for ids
-  const int p_end = last_key < 0 ? p0 : p1;
+  const int p_end = last_key < 0 || row0 >= n_rows ? p0 : p1;
   for (int q0 = p0; q0 < p_end; q0 += kIdPages) {
   const int q1 = min(q0 + kIdPages, p_end), n_pages = q1 - q0;
   if (q0 > p0) __syncthreads();  // (the ids before are read)
@@ -624,15 +639,18 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a)
   if (i >= sq.m) return;
   const int g = fdiv(h, a.fd_G);
   const unsigned in_head = (LISTS ? 0 : i * a.G) + h - g * a.G;  // row of the (token and) kv head
-  const int seg = ((LISTS ? i * a.Hkv : 0) + g) * sq.n_rg + in_head / group_rows;
+  const int team = a.units[a.B + 2], member = team > 1 ? in_head / group_rows : 0;
+  const int seg = team > 1 ? g : ((LISTS ? i * a.Hkv : 0) + g) * sq.n_rg + in_head / group_rows;
   const unsigned share = a.units[a.B];
   const int np = a.units[a.B + 1] ? (sq.np + share - 1) / share * share : sq.np;
   const unsigned u0 = a.units[b] + seg * np;
   const int w0 = u0 / share, n = (int)((u0 + sq.np - 1) / share) - w0 + 1;
   if (n <= 1) return;  // written by the one workgroup that has all its keys
   const int64_t orow = (sq.base + i) * a.Hq + h;
-  // part 0 lies in place 1 of workgroup w0, part j in place 0 of workgroup w0 + j
-  auto place = [&](int j) { return (int64_t)(2 * (w0 + j) + (j == 0 ? 1 : 0)) * group_rows + in_head % group_rows; };
+  // part 0 lies in place 1 of workgroup (or team) w0, part j in place 0 of w0 + j
+  auto place = [&](int j) {
+    return (int64_t)(2 * ((w0 + j) * team + member) + (j == 0 ? 1 : 0)) * group_rows + in_head % group_rows;
+  };
   const f32x2* ml = (const f32x2*)a.part_ml;
   float top = -1e30f;
   if (MANY) {
