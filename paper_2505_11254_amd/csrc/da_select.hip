@@ -256,7 +256,8 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
     int upto = wave_scan_add(sum);
     if (lane == 63) t.scan[2][wave] = upto;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += t.scan[2][w];
+#pragma unroll
+    for (int w = 0; w < W; ++w) upto += w < wave ? t.scan[2][w] : 0;
     int before = upto - sum;
     if (before < need && upto >= need) {
 #pragma unroll
@@ -350,7 +351,8 @@ __device__ __forceinline__ void select_top(TopK<NT, MAX>& t, int n, int top_k, E
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    for (int w = 0; w < wave; ++w) before[q] += t.scan[q][w];
+#pragma unroll
+    for (int w = 0; w < W; ++w) before[q] += w < wave ? t.scan[q][w] : 0;
     for (int j = 0; j < per; ++j) {
       const int e = tid * per + j;
       if (e < entries) {
