@@ -55,11 +55,14 @@ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 // even share of all pages.  A workgroup alone takes kPageUs per page.
 //  - Segments are left whole where their even shares would gain less than the cuts cost:
 //    kCutUs for a second start in a workgroup, two tiles of partial results written and
-//    read, and the merge's launch.  Whole against shared (us; 32 heads on 8, d 128 unless
-//    said): one token, 300 keys 9.8, 15.4; 1000 keys 14.7, 11.2; 64 sequences up to
-//    1000 keys 36, 42, up to 8192 keys 257, 240; 30 trees of 64 up to 1500 keys 61, 74, 9
-//    of them up to 5000 keys 151, 62; 24 of 40 drafts, 20 heads on 4, d 64, up to 700
-//    keys 16, 20.
+//    read, and the merge's launch.  Whole against shared (us; d 128 unless said).  One row
+//    tile: 8 segments of 7 pages 11.4, 14.0, of 16 pages 14.7, 11.2; 64 of 118 pages
+//    61, 43; 384 of 161 pages 240, 230.  Two: 28 of 6 pages 12.9, 16.5; 24 of 34 pages 33, 19.
+//    Four: 21 of 11 pages 18.8, 27.7; 136 of 74 pages 88, 54; d 64, 240 of 27 pages 28, 34, 82
+//    of 29 pages 28, 19.  Eight: 32 of 19 pages 35, 47; 24 of 50 pages 78, 38; 408 of 23 pages
+//    79, 99.  (The rule's choices over 290 drawn sizes are within what two runs differ by of
+//    the better of the two everywhere but for one row tile and more segments than slots: up
+//    to 12 % there.)
 //  - Workgroups begin at segments (and some stay idle) where that costs each at most
 //    kAlignPages pages, less than a second start and its partial results: one sequence of
 //    9000 keys, 14 drafts 26.5 -> 21.8 us; six of them 40.4 -> 37.3; 16 of 24 drafts, 6000
@@ -76,7 +79,7 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   const int c = rt == 1 ? 0 : rt == 2 ? 1 : rt == 4 ? 2 : 3;
   static const int kSlots[2][4] = {{256, 256, 512, 256}, {256, 256, 512, 512}};
   static const double kPageUs[2][4] = {{0.46, 0.9, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
-  static const double kCutUs[4] = {4., 6., 8., 25.};
+  static const double kCutUs[4] = {6., 8., 17., 35.};
   const int64_t groups = (rows + 32 * rt - 1) / (32 * rt);
   const int64_t segs = (n_list ? (int64_t)B * N : B) * Hkv * groups;
   if (n_list) pages = n_list + 1;

@@ -211,3 +211,24 @@ def test_outputs_inside_the_cache_are_refused():
             binding.tree_attn_paged(q, k, v, table, L, out=out, slots=_t(c.slots))
         with pytest.raises(ValueError, match="overlap"):
             binding.selected_attn_paged(q, k, v, table, L, lists, out=out, slots=_t(c.slots))
+
+
+@pytest.mark.parametrize("lens,news,Hq,Hkv,d", [
+    ([9000, 5000], [64, 62], 16, 2, 128),        # two row groups of 256 rows each
+    ([9000, 700, 64, 4000], [64, 0, 63, 61], 16, 2, 128),
+    ([9000, 5000], [64, 20], 16, 2, 128),        # (one sequence has one group only)
+    ([7000, 6500, 6800], [64, 64, 60], 20, 4, 64),  # three of 128
+    ([20000], [30], 5, 1, 64),                   # two, on a single kv head
+    ([6400] * 3 + [5000] * 67, [34] * 70, 8, 1, 64),
+])
+def test_row_groups_over_long_contexts(lens, news, Hq, Hkv, d):
+    """Sequences whose rows fill several workgroups and whose pages are shared among many."""
+    from paper_2505_11254_amd import binding
+    c = Case(lens, news, Hq, Hkv, d, seed=len(lens))
+    q, k, v, table, L = c.gpu()
+    lse = torch.zeros(q.shape[:2], device="cuda")
+    assert binding.paged_workspace_bytes(len(lens), max(news), Hq, Hkv, d, max(lens)) > 0
+    out = binding.tree_attn_paged(q, k, v, table, L, lse=lse, max_len=max(lens), **c.kw())
+    c.check(out, lse, lambda b, i, g: torch.arange(lens[b]) <= lens[b] - news[b] + i)
+    again = binding.tree_attn_paged(q, k, v, table, L, max_len=max(lens), **c.kw())
+    assert torch.equal(out, again)
