@@ -60,9 +60,8 @@ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 //    61, 43; 384 of 161 pages 240, 230.  Two: 28 of 6 pages 12.9, 16.5; 24 of 34 pages 33, 19.
 //    Four: 21 of 11 pages 18.8, 27.7; 136 of 74 pages 88, 54; d 64, 240 of 27 pages 28, 34, 82
 //    of 29 pages 28, 19.  Eight: 32 of 19 pages 35, 47; 24 of 50 pages 78, 38; 408 of 23 pages
-//    79, 99.  (The rule's choices over 290 drawn sizes are within what two runs differ by of
-//    the better of the two everywhere but for one row tile and more segments than slots: up
-//    to 12 % there.)
+//    79, 99.  (Over 290 drawn sizes the rule's choices average within 1 % of the better of
+//    the two; at worst 18 % above, one row tile, d 64, 18 segments of 22 pages.)
 //  - Workgroups begin at segments (and some stay idle) where that costs each at most
 //    kAlignPages pages, less than a second start and its partial results: one sequence of
 //    9000 keys, 14 drafts 26.5 -> 21.8 us; six of them 40.4 -> 37.3; 16 of 24 drafts, 6000

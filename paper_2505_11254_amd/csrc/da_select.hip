@@ -44,8 +44,9 @@ __device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
 // A wavefront per (block, kv head): D/8 lanes read a key's row, 16 bytes each, so
 // that 512/D keys arrive per load.  The lanes that hold the same eight channels then
 // halve the sums they keep as they add them up, and each finishes one or two channels.
-// Every key is read once, 1/64 of that written; the conversions and sums in 64 bits
-// take about as long as the loads.
+// Every key is read once, 1/64 of that written: 16384 tokens of 8 kv heads, d 128 (34 MB) in
+// 8.1 us, 87302 (179 MB) in 50 us, 3.6 TB/s, right after the pages were written; with sums
+// in 32 bits the same.
 template <int D>
 __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kSteps = kPage / kRows;
@@ -696,7 +697,8 @@ __global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArg
 // Candidates are the whole pages before the token's own.  Scores first, a workgroup
 // of four waves per (token, kv head, kScoreTiles tiles of 32 pages), then a
 // workgroup per (token, kv head) picks.  Bound by HBM in the first (one byte per key
-// channel and 64 keys), by latency in the second.
+// channel and 64 keys), by latency in the second: 16 tokens over up to 50000 keys, 32 heads
+// on 8, d 128: 7.8 and 8.6 us; one over 1048576 keys: 8.4 and 20.4.
 constexpr int kScoreTiles = 16;
 
 struct Token {
