@@ -399,7 +399,7 @@ da_status da_launch_workgroups(int B, int max_seqlen, int packed, int Hq, int Hk
  * 128, any Hq / Hkv.  Launches have at most 2^32 - 1 threads: of 256 per kv head of a page
  * that may be copied or compacted (n * layers * 2 * Hkv), of a query block, of 4 pages to
  * be summarised, of 8 query heads of new tokens, of 16 KB to be appended, and of a token to
- * select pages for (1024 there with max_len over 262,208); more is DA_ERR_SHAPE.
+ * select pages for (512 there up to max_len 65599, 1024 past 262207); more is DA_ERR_SHAPE.
  */
 #define DA_PAGE_TOKENS 64
 #define DA_PAGES_MAX_REQUESTS 1024
@@ -518,7 +518,8 @@ da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* ta
  * da_select_pages (decode): a group is one token in the heads of one kv head, its
  * candidates the pages before the token's own.  Writes page positions (indices into
  * the slot's table row) pages [T, Hkv, top_k], ascending, -1 behind the last.
- * workspace: da_select_pages_workspace_bytes() bytes; none when max_len / 64 <= top_k.
+ * workspace: da_select_pages_workspace_bytes() bytes (0 up to max_len 65599); none when
+ * max_len / 64 <= top_k.
  */
 int64_t da_select_blocks_entries(int B, int max_seqlen, int Hkv, int top_k, int block_q);
 da_status da_select_blocks(const void* q, const void* codes, const float* scales,

@@ -16,6 +16,8 @@ namespace da {
 constexpr int kPage = DA_PAGE_TOKENS;  // tokens per page: the attention kernels' key tile
 // Most candidates of a group: their ranks and, in the prefill, their scores are in LDS.
 constexpr int kMaxCandPages = 131072, kMaxCandBlocks = 24576;
+// Candidate pages that one launch scores and picks from, without a workspace.
+constexpr int kFewCandPages = 1024;
 constexpr int kMaxRequests = DA_PAGES_MAX_REQUESTS;
 
 // The integers of a cache: page table [S][M], lengths [S], reference counts [P].
@@ -79,7 +81,7 @@ struct SelectArgs {
   int64_t total;         // list entries of one (sequence, kv head)
   int max_blocks;        // candidates any group can have
   int32_t* pages;        // decode: [T][Hkv][top_k]
-  uint32_t* keys;        // decode: workspace [B * N][Hkv][max_blocks]
+  uint32_t* keys;        // decode: workspace [B * N][Hkv][max_blocks], past kFewCandPages of them
 };
 hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t s);
 hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s);

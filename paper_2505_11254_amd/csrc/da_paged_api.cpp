@@ -351,7 +351,7 @@ da_status da_select_blocks(const void* q, const void* codes, const float* scales
 }
 
 size_t da_select_pages_workspace_bytes(int B, int max_seqlen, int Hkv, int max_len) {
-  if (B < 1 || max_seqlen < 1 || Hkv < 1 || max_len < 1) return 0;
+  if (B < 1 || max_seqlen < 1 || Hkv < 1 || max_len < 1 || max_len / kPage <= kFewCandPages) return 0;
   return (size_t)B * max_seqlen * Hkv * (size_t)(max_len / kPage) * 4;
 }
 
@@ -370,12 +370,13 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
   const int64_t room = (int64_t)M * kPage;
   if (max_len > room) max_len = (int)room;
   if (max_len / kPage > kMaxCandPages) return DA_ERR_UNSUPPORTED;
-  if (!fits((int64_t)B * max_seqlen * Hkv, max_len / kPage > 4096 ? 1024 : 256)) return DA_ERR_SHAPE;
+  const int blocks = max_len / kPage;
+  if (!fits((int64_t)B * max_seqlen * Hkv, blocks > 4096 ? 1024 : blocks > kFewCandPages ? 256 : 512)) return DA_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(cu_seqlens, 4) ||
       !aligned(slots, 4) || !aligned(pages, 4) || !aligned(workspace, 4))
     return DA_ERR_ALIGN;
   const size_t need = da_select_pages_workspace_bytes(B, max_seqlen, Hkv, max_len);
-  if (max_len / kPage > top_k && (!workspace || workspace_bytes < need)) return DA_ERR_WORKSPACE;
+  if (need && max_len / kPage > top_k && (!workspace || workspace_bytes < need)) return DA_ERR_WORKSPACE;
   st = check_device();
   if (st != DA_OK) return st;
   SelectArgs a{};

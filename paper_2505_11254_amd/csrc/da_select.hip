@@ -694,13 +694,12 @@ __global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArg
 
 // ------------------------------------------------- decode: a list per query token
 //
-// Candidates are the whole pages before the token's own.  Scores first, a workgroup
-// of four waves per (token, kv head, kScoreTiles tiles of 32 pages), then a
-// workgroup per (token, kv head) picks.  Bound by HBM in the first (one byte per key
-// channel and 64 keys), by latency in the second: 16 tokens over up to 50000 keys, 32 heads
-// on 8, d 128: 7.8 and 8.6 us; one over 1048576 keys: 8.4 and 20.4.
-constexpr int kScoreTiles = 16;
-
+// Candidates are the whole pages before the token's own.  Up to kFewCandPages of them a
+// workgroup per (token, kv head) scores and picks; with more, scores come first, a
+// workgroup of four waves per 512 pages, then a workgroup per (token, kv head) picks.  Bound
+// by HBM in the scores (one byte per key channel and 64 keys), by latency otherwise: 16
+// tokens over up to 50000 keys, 32 heads on 8, d 128: 12.5 us (as two launches 13.5, and 3 us
+// more on the host); one over 1048576 keys: 8.4 and 20.4.
 struct Token {
   int b, s, pos;
   int64_t t;  // row of q
@@ -717,28 +716,23 @@ __device__ __forceinline__ bool token_of(const SelectArgs& a, uint32_t item, Tok
   return true;
 }
 
-// The codes of the token's rows are made once per workgroup, through LDS, while the
-// first pages' codes are on their way.
+// Keys of the candidates t0 to t0 + 2 NT - 1 of n, by the NT threads of a workgroup: put(j, key)
+// for each.  The codes of the token's rows are made once, through LDS, while the first
+// pages' codes are on their way.
+constexpr int kTilesPerWave = 4;
 template <int D>
-__global__ __launch_bounds__(kScoreThreads) void score_pages_kernel(SelectArgs a) {
-  constexpr int kPer = kScoreTiles / (kScoreThreads / 64);  // tiles of a wave
-  constexpr int kRowBytes = D + 16;  // padded against bank conflicts
-  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * kRowBytes];
+constexpr int kCodeRowBytes = D + 16;  // padded against bank conflicts
+template <int D, int NT, typename Put>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, const Token& tk, int g, int n, int t0,
+                                            uint8_t* rows_lds, Put put) {
+  constexpr int kPer = kTilesPerWave, kRowBytes = kCodeRowBytes<D>;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31, wave = tid >> 6;
   const int G = a.Hq / a.Hkv;
-  const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
-  const int g = blockIdx.x % (unsigned)a.Hkv;
-  Token tk;
-  if (!token_of(a, item, &tk)) return;
-  const int n = min(max(tk.pos, 0) / kPage, a.max_blocks);
-  const int t0 = blockIdx.y * (kScoreTiles * 32);
-  if (t0 >= n || n <= a.top_k) return;  // (all are chosen without scores)
   const uint16_t* const q0 = a.q + (tk.t * a.Hq + (int64_t)g * G) * D;
   const int32_t* const row = a.table + (int64_t)tk.s * a.M;
-  uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   int page[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) page[i] = row[min(t0 + (i * (kScoreThreads / 64) + wave) * 32 + col, n - 1)];
+  for (int i = 0; i < kPer; ++i) page[i] = row[min(t0 + (i * (NT / 64) + wave) * 32 + col, n - 1)];
   u16x2 most = {0, 0};
   for (int c = lane; c < G * (D / 8); c += 64) most = max_bits(most, *(const u32x4*)(q0 + c * 8));
   float scale[kPer];
@@ -758,7 +752,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_pages_kernel(SelectArgs a
   for (int u = 0; u < G; u += 32) {  // (more than one turn for more than 32 heads only)
     if (u) __syncthreads();
     // (rows past the last repeat it, which changes no maximum)
-    for (int c = tid; c < 32 * (D / 8); c += kScoreThreads)
+    for (int c = tid; c < 32 * (D / 8); c += NT)
       *(uint2*)(rows_lds + c / (D / 8) * kRowBytes + c % (D / 8) * 8) =
           coder.codes(*(const u32x4*)(q0 + min(u + c / (D / 8), G - 1) * D + c % (D / 8) * 8));
     __syncthreads();
@@ -777,22 +771,62 @@ __global__ __launch_bounds__(kScoreThreads) void score_pages_kernel(SelectArgs a
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     m[i] = max(m[i], __shfl_xor(m[i], 32));
-    const int j = t0 + (i * (kScoreThreads / 64) + wave) * 32 + col;
+    const int j = t0 + (i * (NT / 64) + wave) * 32 + col;
     if (half == 0 && j < n) {
       // (a page that the table does not name comes last: nothing of it is attended to)
       const uint32_t key = (unsigned)page[i] < (unsigned)a.P ? order_bits((float)m[i] * scale[i]) : kAbsent;
-      keys[j] = j < a.n_sink || j >= n - a.n_recent ? kForced : key;
+      put(j, j < a.n_sink || j >= n - a.n_recent ? kForced : key);
     }
   }
 }
 
-// One wavefront takes up to 1024 candidates.  Workgroups of 256 threads take up to 4096,
-// whose keys they hold in registers, 1024 up to 16384 likewise, and more from memory:
-// barriers of four waves cost less than those of sixteen.
+template <int D>
+__global__ __launch_bounds__(kScoreThreads) void score_pages_kernel(SelectArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * kCodeRowBytes<D>];
+  const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
+  const int g = blockIdx.x % (unsigned)a.Hkv;
+  Token tk;
+  if (!token_of(a, item, &tk)) return;
+  const int n = min(max(tk.pos, 0) / kPage, a.max_blocks);
+  const int t0 = blockIdx.y * (kScoreThreads * 2);
+  if (t0 >= n || n <= a.top_k) return;  // (all are chosen without scores)
+  uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
+  score_pages<D, kScoreThreads>(a, tk, g, n, t0, rows_lds, [&](int j, uint32_t key) { keys[j] = key; });
+}
+
+// Up to 1024 candidates: one launch, whose workgroups score them, keys in LDS, and whose first
+// waves then pick.
+constexpr int kFewThreads = 512;
+static_assert(kFewThreads * 2 == kFewCandPages && kFewCandPages == 64 * kWaveKeys, "as many as one wave takes");
+template <int D>
+__global__ __launch_bounds__(kFewThreads) void few_pages_kernel(SelectArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t rows_lds[32 * kCodeRowBytes<D>];
+  __shared__ uint32_t keys[64 * kWaveKeys];
+  const int tid = threadIdx.x;
+  const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
+  const int g = blockIdx.x % (unsigned)a.Hkv;
+  Token tk;
+  if (!token_of(a, item, &tk)) return;
+  const int n = min(max(tk.pos, 0) / kPage, a.max_blocks);
+  int32_t* const list = a.pages + (tk.t * a.Hkv + g) * a.top_k;
+  for (int i = min(n, a.top_k) + tid; i < a.top_k; i += kFewThreads) list[i] = -1;
+  if (n <= a.top_k) {
+    for (int i = tid; i < n; i += kFewThreads) list[i] = i;
+    return;
+  }
+  score_pages<D, kFewThreads>(a, tk, g, n, 0, rows_lds, [&](int j, uint32_t key) { keys[j] = key; });
+  __syncthreads();
+  if (tid >= 64) return;
+  select_few(n, a.top_k, [&](int i) { return keys[i]; }, [&](int rank, int i) { list[rank] = i; });
+}
+
+// More: workgroups of 256 threads take up to 4096, whose keys they hold in registers, 1024 up
+// to 16384 likewise, and more from memory: barriers of four waves cost less than those of
+// sixteen.
 constexpr int kPickHeld = 16;  // keys per thread held in registers
 template <int NT, bool HELD>
 __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
-  __shared__ std::conditional_t<NT == 64, char, TopK<NT == 64 ? 256 : NT, HELD ? NT * kPickHeld : kMaxCandPages>> topk;
+  __shared__ TopK<NT, HELD ? NT * kPickHeld : kMaxCandPages> topk;
   const int tid = threadIdx.x;
   const uint32_t item = blockIdx.x / (unsigned)a.Hkv;
   const int g = blockIdx.x % (unsigned)a.Hkv;
@@ -803,9 +837,7 @@ __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
   for (int i = min(n, a.top_k) + tid; i < a.top_k; i += NT) list[i] = -1;
   const uint32_t* const keys = a.keys + ((int64_t)item * a.Hkv + g) * a.max_blocks;
   auto emit = [&](int rank, int i) { list[rank] = i; };
-  if constexpr (NT == 64) {
-    select_few(n, a.top_k, [&](int i) { return n > a.top_k ? keys[i] : kAbsent; }, emit);
-  } else if constexpr (HELD) {
+  if constexpr (HELD) {
     uint32_t x[kPickHeld];
     if (n > a.top_k) {
 #pragma unroll
@@ -857,23 +889,27 @@ hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s) {
-  const int64_t items = (int64_t)a.B * a.N * a.Hkv;
+  const dim3 items((unsigned)((int64_t)a.B * a.N * a.Hkv));
+  if (a.max_blocks <= kFewCandPages) {
+    if (a.d == 128)
+      hipLaunchKernelGGL(few_pages_kernel<128>, items, dim3(kFewThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL(few_pages_kernel<64>, items, dim3(kFewThreads), 0, s, a);
+    return hipGetLastError();
+  }
   if (a.max_blocks > a.top_k) {
-    const dim3 grid((unsigned)items, (unsigned)((a.max_blocks + kScoreTiles * 32 - 1) / (kScoreTiles * 32)));
+    const dim3 grid(items.x, (unsigned)((a.max_blocks + kScoreThreads * 2 - 1) / (kScoreThreads * 2)));
     if (a.d == 128)
       hipLaunchKernelGGL(score_pages_kernel<128>, grid, dim3(kScoreThreads), 0, s, a);
     else
       hipLaunchKernelGGL(score_pages_kernel<64>, grid, dim3(kScoreThreads), 0, s, a);
   }
-  const dim3 grid((unsigned)items);
-  if (a.max_blocks <= 64 * kWaveKeys)
-    hipLaunchKernelGGL((pick_pages_kernel<64, true>), grid, dim3(64), 0, s, a);
-  else if (a.max_blocks <= 256 * kPickHeld)
-    hipLaunchKernelGGL((pick_pages_kernel<256, true>), grid, dim3(256), 0, s, a);
+  if (a.max_blocks <= 256 * kPickHeld)
+    hipLaunchKernelGGL((pick_pages_kernel<256, true>), items, dim3(256), 0, s, a);
   else if (a.max_blocks <= 1024 * kPickHeld)
-    hipLaunchKernelGGL((pick_pages_kernel<1024, true>), grid, dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((pick_pages_kernel<1024, true>), items, dim3(1024), 0, s, a);
   else
-    hipLaunchKernelGGL((pick_pages_kernel<1024, false>), grid, dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((pick_pages_kernel<1024, false>), items, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 

@@ -96,8 +96,6 @@ REFUSED = [
     ("da_select_pages", NULL, ["q", "codes", "scales", "table", "lens", "pages"], None),
     ("da_select_pages", PARAM, ["top_k"], 1),
     ("da_select_pages", PARAM, ["n_recent"], 4),
-    ("da_select_pages", WORKSPACE, ["ws"], None),
-    ("da_select_pages", WORKSPACE, ["size"], 2 * 3 * 2 * 8 * 4 - 1),
 ]
 
 
@@ -150,6 +148,12 @@ def test_workspaces_that_are_too_small(lib):
         assert need > 0 and getattr(lib, fn)(*a.values()) == WORKSPACE
         a["size"], a["ws"] = need, None
         assert getattr(lib, fn)(*a.values()) == WORKSPACE
+    need = lib.da_select_pages_workspace_bytes(2, 3, 2, 1025 * 64)
+    a = dict(ARGS["da_select_pages"], M=1025, max_len=1025 * 64, size=need - 1)
+    assert need == 2 * 3 * 2 * 1025 * 4 and lib.da_select_pages(*a.values()) == WORKSPACE
+    a["size"], a["ws"] = need, None
+    assert lib.da_select_pages(*a.values()) == WORKSPACE
+    assert lib.da_select_pages_workspace_bytes(2, 3, 2, 1025 * 64 - 1) == 0
     # few pages: no rows are cut, nothing is needed
     assert binding.paged_workspace_bytes(2, 3, 8, 2, 128, 512) == binding.paged_workspace_bytes(2, 3, 8, 2, 128, 1, 4) == 0
 
