@@ -698,8 +698,8 @@ __global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArg
 // workgroup per (token, kv head) scores and picks; with more, scores come first, a
 // workgroup of four waves per 512 pages, then a workgroup per (token, kv head) picks.  Bound
 // by HBM in the scores (one byte per key channel and 64 keys), by latency otherwise: 16
-// tokens over up to 50000 keys, 32 heads on 8, d 128: 12.5 us (as two launches 13.5, and 3 us
-// more on the host); one over 1048576 keys: 8.4 and 20.4.
+// tokens over up to 50000 keys, 32 heads on 8, d 128: 14 us (as two launches 16 and the gap
+// between, and 3 us more on the host); one over 1048576 keys: 8.4 and 20.4.
 struct Token {
   int b, s, pos;
   int64_t t;  // row of q
