@@ -471,6 +471,13 @@ class _On:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.dev)
 
+    def like(self, t, shape=None):
+        """A new tensor of t's type (and shape); t lies on the device (cheaper than `empty`)."""
+        if self.stream is None:
+            return torch.empty_like(t) if shape is None else t.new_empty(shape)
+        with torch.cuda.stream(self.stream):
+            return torch.empty_like(t) if shape is None else t.new_empty(shape)
+
     def workspace(self, given, nbytes):
         """(tensor, address, size) of the caller's workspace, or of one that lasts for this call."""
         if given is None:
@@ -545,9 +552,9 @@ def _new_rows(T, B, cu_seqlens, max_seqlen, dev):
     return cu_seqlens.shape[0] - 1, int(max_seqlen)
 
 
-def _requests(result, shape, on):
+def _requests(result, shape, ints, on):
     if result is None:
-        return on.empty(shape, torch.int32)
+        return on.like(ints, shape)
     _ints("result", result, on.dev, shape)
     return result
 
@@ -561,7 +568,7 @@ def pages_fork(table, lens, refs, src, dst, *, result=None, stream=None):
     n = src.numel()
     _ints("src", src, on.dev, (n,))
     _ints("dst", dst, on.dev, (n,))
-    result = _requests(result, (n,), on)
+    result = _requests(result, (n,), src, on)
     on.call("da_pages_fork", _ptr(table), _ptr(lens), _ptr(refs), S, M, refs.numel(), _ptr(src), _ptr(dst), n,
             _ptr(result))
     return result
@@ -579,7 +586,7 @@ def pages_resize(k_pages, v_pages, table, lens, refs, slots, new_lens=None, *, r
     _ints("slots", slots, dev, (n,))
     if new_lens is not None:
         _ints("new_lens", new_lens, dev, (n,))
-    result = _requests(result, (n, 4), on)
+    result = _requests(result, (n, 4), slots, on)
     on.call("da_pages_resize", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
             P, _ptr(slots), _ptr(new_lens), n, _ptr(result))
     return result
@@ -617,7 +624,7 @@ def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_ke
     _ints("start", start, dev, (n,))
     _ints("keep", keep, dev, (keep.numel(),))
     _ints("cu_keep", cu_keep, dev, (n + 1,))
-    result = _requests(result, (n, 4), on)
+    result = _requests(result, (n, 4), slots, on)
     if not keep.numel():  # (an empty tensor has no address; no place is read)
         keep = cu_keep
         n_keep = 0
@@ -633,7 +640,7 @@ def _queries(q, k_pages, v_pages, out, lse, Hkv, d, on):
     if q.dim() != 3 or q.shape[2] != d or q.shape[1] % Hkv:
         raise ValueError(f"q must be [T, Hq, {d}] with Hq a multiple of {Hkv}")
     if out is None:
-        out = on.empty(q.shape, torch.bfloat16)
+        out = on.like(q)
     else:
         _halves("out", out, on.dev)
         if out.shape != q.shape:
@@ -795,7 +802,7 @@ def select_pages(q, codes, scales, table, lens, *, top_k, n_sink=1, n_recent=1, 
     room = M * PAGE_TOKENS
     max_len = room if max_len is None else min(int(max_len), room)
     if pages is None:
-        pages = on.empty((T, Hkv, top_k), torch.int32)
+        pages = on.like(lens, (T, Hkv, top_k))
     _ints("pages", pages, on.dev, (T, Hkv, top_k))
     need = int(load_library().da_select_pages_workspace_bytes(B, N, Hkv, max_len)) if workspace is None else 0
     ws, ptr, size = on.workspace(workspace, need)
