@@ -83,6 +83,13 @@ struct SelectArgs {
   int32_t* pages;        // decode: [T][Hkv][top_k]
   uint32_t* keys;        // decode: workspace [B * N][Hkv][max_blocks], past kFewCandPages of them
 };
+// Entries of the lists of one (sequence, kv head) before query block qb: min(top_k, j * R) for
+// each block j, R key tiles long.  In 64 bits: top_k may be the largest int, "all of them".
+__host__ __device__ __forceinline__ int64_t list_entries_before(int64_t qb, int top_k, int R) {
+  const int64_t whole = (int64_t)(top_k / R) + 1;  // lists with j * R <= top_k
+  const int64_t m = qb < whole ? qb : whole;
+  return m * (m - 1) / 2 * R + (qb - m) * top_k;
+}
 hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t s);
 hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s);
 

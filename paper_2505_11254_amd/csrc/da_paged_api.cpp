@@ -108,11 +108,9 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   return DA_OK;
 }
 
-// Entries of the lists of one (sequence, kv head): min(top_k, qb * R) each.
+// Entries of the lists of one (sequence, kv head).
 int64_t list_total(int max_seqlen, int top_k, int block_q) {
-  const int64_t nqb = ((int64_t)max_seqlen + block_q - 1) / block_q, R = block_q / kPage;
-  const int64_t m = nqb < top_k / R + 1 ? nqb : top_k / R + 1;
-  return m * (m - 1) / 2 * R + (nqb - m) * top_k;
+  return list_entries_before(((int64_t)max_seqlen + block_q - 1) / block_q, top_k, block_q / kPage);
 }
 
 da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_bytes, void* stream) {

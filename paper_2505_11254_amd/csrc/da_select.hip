@@ -562,11 +562,8 @@ __global__ __launch_bounds__(kSelThreads, 3) void select_blocks_kernel(SelectArg
   const int R = a.block_q / kPage;
   const int n_qb = max(0, (L + a.block_q - 1) / a.block_q);
 
-  // list sizes are known ahead: min(top_k, qb * R) each
-  auto before = [&](int qb_) -> int64_t {  // entries of the lists before qb_
-    const int64_t m = min(qb_, a.top_k / R + 1);  // lists with j * R <= top_k
-    return m * (m - 1) / 2 * R + (qb_ - m) * a.top_k;
-  };
+  // list sizes are known ahead
+  auto before = [&](int j) { return list_entries_before(j, a.top_k, R); };
   const int64_t list0 = ((int64_t)b * a.Hkv + g) * a.total;
   int32_t* const ptr = a.block_ptr + ((int64_t)b * a.Hkv + g) * (a.nqb + 1);
   if (tid == 0) {

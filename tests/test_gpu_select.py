@@ -279,3 +279,23 @@ def test_prompt_then_decode_end_to_end():
             hist[s] = tuple(x[:L0[i] + len(keep)] for x in hist[s])
     binding.pages_resize(*cache, _t([0, 2]))
     assert int(refs.sum()) == 0 and (table == -1).all() and int(lens.sum()) == 0
+
+
+@pytest.mark.parametrize("block_q", [64, 128, 256])
+@pytest.mark.parametrize("top_k", [200, 2 ** 31 - 2, 2 ** 31 - 1])
+def test_more_blocks_than_there_are(block_q, top_k):
+    """top_k past all candidates, the largest integer too: every tile before a query block, in a
+    ragged batch."""
+    from paper_2505_11254_amd import binding
+    cu, Hq, Hkv, d = [0, 1000, 1000, 1064, 3000], 4, 2, 64
+    g = torch.Generator().manual_seed(block_q)
+    q = torch.randn((cu[-1], Hq, d), generator=g).to(torch.bfloat16).cuda()
+    k = torch.randn((cu[-1], Hkv, d), generator=g).to(torch.bfloat16).cuda()
+    kw = dict(cu_seqlens=torch.tensor(cu, dtype=torch.int32).cuda(), max_seqlen=1936)
+    ptr, idx = binding.select_blocks(q, *binding.key_summary(k, **kw), top_k=top_k, block_q=block_q, **kw)
+    ptr, idx, R = ptr.tolist(), idx.tolist(), block_q // 64
+    for b in range(4):
+        n_qb = -(-(cu[b + 1] - cu[b]) // block_q)
+        for h in range(Hkv):
+            for j in range(n_qb):
+                assert idx[ptr[b][h][j]:ptr[b][h][j + 1]] == list(range(min(top_k, j * R)))

@@ -52,3 +52,18 @@ def test_abi_host_layer_under_sanitizers(tmp_path):
     r = _run([exe], env=ENV)
     assert r.returncode == 0 and "runtime error" not in r.stderr, r.stdout + r.stderr
     assert "abi driver ok" in r.stdout
+
+
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.exists(ROCM_LIB + "/libamdhip64.so"),
+                    reason="g++ or the HIP runtime library not found")
+def test_serving_host_layer_under_sanitizers(tmp_path):
+    exe = str(tmp_path / "paged_driver")
+    csrc = os.path.join(ROOT, "paper_2505_11254_amd", "csrc")
+    b = _run(["g++", "-std=c++17", *SAN, "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+              "-I" + os.path.join(ROOT, "include"), "-I" + csrc,
+              os.path.join(HERE, "paged_driver.cpp"), os.path.join(csrc, "da_paged_api.cpp"),
+              "-o", exe, "-L" + ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lamdhip64"])
+    assert b.returncode == 0, b.stderr
+    r = _run([exe], env=ENV)
+    assert r.returncode == 0 and "runtime error" not in r.stderr, r.stdout + r.stderr
+    assert "paged driver ok" in r.stdout
