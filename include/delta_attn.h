@@ -538,7 +538,7 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
  * Attention of the last m tokens of each sequence over selected pages: the row of
  * token p in kv head g sees the whole pages pages[row][g][0 .. top_k-1] (positions below
  * p / 64, each at most once; other values are skipped) and its own page up to itself.
- * lse as tree_attn_paged; workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d,
+ * top_k is at most 2^30.  lse as tree_attn_paged; workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d,
  * 1, top_k) bytes.
  */
 da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out,

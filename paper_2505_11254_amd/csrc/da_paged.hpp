@@ -18,6 +18,8 @@ constexpr int kPage = DA_PAGE_TOKENS;  // tokens per page: the attention kernels
 constexpr int kMaxCandPages = 131072, kMaxCandBlocks = 24576;
 // Candidate pages that one launch scores and picks from, without a workspace.
 constexpr int kFewCandPages = 1024;
+// Longest list of pages: places in it, and a workgroup's step past them, are 32-bit in the kernels.
+constexpr int kMaxList = 1 << 30;
 constexpr int kMaxRequests = DA_PAGES_MAX_REQUESTS;
 
 // The integers of a cache: page table [S][M], lengths [S], reference counts [P].

@@ -72,6 +72,7 @@ struct PagedPlan {
   size_t units_bytes, part_rows, bytes;
 };
 da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
+  if (n_list > kMaxList) return DA_ERR_SHAPE;
   const int G = Hq / Hkv;
   const int64_t rows = n_list ? G : (int64_t)N * G;
   const int rt = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
@@ -81,7 +82,7 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   static const double kCutUs[4] = {6., 8., 17., 35.};
   const int64_t groups = (rows + 32 * rt - 1) / (32 * rt);
   const int64_t segs = (n_list ? (int64_t)B * N : B) * Hkv * groups;
-  if (n_list) pages = n_list + 1;
+  if (n_list) pages = (int64_t)n_list + 1;
   if (pages < 1) pages = 1;
   if ((double)segs * (double)pages > (double)INT32_MAX) return DA_ERR_SHAPE;
   const int64_t slots = kSlots[d == 64][c];

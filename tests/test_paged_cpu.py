@@ -128,6 +128,14 @@ def test_calls_refuse_what_no_launch_can_hold(lib, fn, sizes):
     assert getattr(lib, fn)(*dict(ARGS[fn], **sizes).values()) == SHAPE
 
 
+@pytest.mark.parametrize("top_k", [(1 << 30) + 1, (1 << 31) - 2, (1 << 31) - 1])
+def test_attention_refuses_lists_past_what_is_counted(lib, top_k):
+    """A list and its own page are counted in 32 bits: one page more than the largest int is no small list."""
+    assert lib.selected_attn_paged(*dict(ARGS["selected_attn_paged"], B=1, N=1, Hq=4, Hkv=1, top_k=top_k).values()) == SHAPE
+    assert binding.paged_workspace_bytes(1, 1, 4, 1, 128, 1, top_k) == 0
+    assert binding.paged_workspace_bytes(1, 1, 4, 1, 128, 1, 1 << 30) > 0
+
+
 @pytest.mark.parametrize("fn", sorted(ARGS))
 def test_the_arguments_above_are_good(lib, fn):
     """(so that each refusal is that of the one argument that was changed)"""
