@@ -136,6 +136,12 @@ def test_attention_refuses_lists_past_what_is_counted(lib, top_k):
     assert binding.paged_workspace_bytes(1, 1, 4, 1, 128, 1, 1 << 30) > 0
 
 
+@pytest.mark.parametrize("top_k", [(1 << 30) + 1, (1 << 31) - 1])
+def test_selection_refuses_lists_past_what_is_counted(lib, top_k):
+    """Threads step past the end of a list in 32 bits."""
+    assert lib.da_select_pages(*dict(ARGS["da_select_pages"], top_k=top_k).values()) == SHAPE
+
+
 @pytest.mark.parametrize("fn", sorted(ARGS))
 def test_the_arguments_above_are_good(lib, fn):
     """(so that each refusal is that of the one argument that was changed)"""
