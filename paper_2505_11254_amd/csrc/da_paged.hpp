@@ -124,6 +124,11 @@ struct PagedArgs {
   float* part_o;         // [n_wgs][2][row_tiles * 32][d] partial results of cut segments
   float* part_ml;        // [n_wgs][2][row_tiles * 32][2]
 };
+// Units per workgroup or team, of `total` for n of them (up to the largest int: the sum is unsigned).
+__host__ __device__ __forceinline__ int share_of(int min_units, int total, int n) {
+  const int even = (int)(((uint32_t)total + (uint32_t)n - 1) / (uint32_t)n);
+  return even > min_units ? even : min_units;
+}
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s);
 
 }  // namespace da

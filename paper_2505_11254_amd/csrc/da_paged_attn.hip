@@ -93,10 +93,6 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int b, int group
 __device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
   return a.whole ? x.segs : x.segs * x.np;
 }
-// Units per workgroup or team, of `total` for n of them.
-__device__ __forceinline__ int share_of(const PagedArgs& a, int total, int n) {
-  return max(a.min_units, (total + n - 1) / n);
-}
 
 template <int D, int RT, bool LISTS>
 __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) void paged_attn_kernel(PagedArgs a) {
@@ -155,7 +151,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     const int n_wgs = a.n_wgs / team, wt = w / team;
     int upto = wave_scan_add(mine), units = mine;
     int total = __builtin_amdgcn_readlane(upto, 63);
-    int share = share_of(a, total, n_wgs);
+    int share = share_of(a.min_units, total, n_wgs);
     if (!a.whole) {
       // Where segments are few against workgroups, whole workgroups go to each: a
       // second segment would cost a workgroup another start, more than the pages that
@@ -163,7 +159,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       const int segs = wave_add(lane < a.B ? held.segs : 0);
       if (segs < n_wgs && (double)total * segs < (double)a.align_pages * n_wgs * (n_wgs - segs)) {
         aligned = true;
-        share = share_of(a, total, n_wgs - segs);
+        share = share_of(a.min_units, total, n_wgs - segs);
         units = lane < a.B ? held.segs * ((held.np + share - 1) / share * share) : 0;
         upto = wave_scan_add(units);
         total = __builtin_amdgcn_readlane(upto, 63);
@@ -209,7 +205,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       total += more;
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    const int share = share_of(a, total, a.n_wgs);
+    const int share = share_of(a.min_units, total, a.n_wgs);
     const int64_t x0 = (int64_t)w * share;
     if (w == 0 && tid == 0 && a.units) {
       a.units[a.B] = share;

@@ -53,8 +53,20 @@ static void lists_of_any_top_k() {
     }
 }
 
+// As many pages as are counted at all are shared out whole, however many workgroups there are.
+static void shares_of_any_total() {
+  for (int total : {0, 1, 7, 1000, INT32_MAX - 511, INT32_MAX - 1, INT32_MAX})
+    for (int n : {1, 3, 85, 256, 511, 512})
+      for (int least : {1, 2, 16}) {
+        const int64_t share = share_of(least, total, n);
+        expect(share >= least && share * n >= total, 1, "shares hold all units");
+        expect(share == least || (share - 1) * n < total, 1, "shares are even");
+      }
+}
+
 int main() {
   lists_of_any_top_k();
+  shares_of_any_total();
   if (failures) return 1;
   printf("paged driver ok\n");
   return 0;
