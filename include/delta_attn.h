@@ -435,11 +435,21 @@ da_status da_pages_resize(void* k_pages, void* v_pages, int layers, int Hkv, int
  * Writes the keys and values k, v [layers, T, Hkv, d] of new tokens as the last ones of
  * their slots, which da_pages_resize has made room for: row i of the m rows of
  * sequence b goes to token lens[slot] - m + i.  k and v lie outside the pages.
+ * A slot whose growth was refused has its old tokens there, perhaps in pages that other
+ * slots hold too.  da_pages_append_to leaves such slots as they are: it writes the rows of
+ * sequence b only where lens[slot] is new_lens[b] (new_lens [B], what da_pages_resize was
+ * asked for; NULL: whatever the length).  da_pages_append is for callers that have looked
+ * at the results; steps that are enqueued or captured whole take da_pages_append_to.
+ * (The attention of such a step is over the slot as it is: its outputs are to be dropped.)
  */
 da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
                           int layers, int Hkv, int d, const int32_t* table, const int32_t* lens,
                           int S, int M, int P, const int32_t* slots, const int32_t* cu_seqlens,
                           int B, int max_seqlen, void* stream);
+da_status da_pages_append_to(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
+                             int layers, int Hkv, int d, const int32_t* table, const int32_t* lens,
+                             int S, int M, int P, const int32_t* slots, const int32_t* cu_seqlens,
+                             int B, int max_seqlen, const int32_t* new_lens, void* stream);
 
 /*
  * Keeps some of a slot's tokens from start[i] on: those at start[i] + keep[j], j in

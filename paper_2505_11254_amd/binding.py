@@ -40,6 +40,7 @@ SIGNATURES = {
     "da_pages_fork": "pppiiippipp",
     "da_pages_resize": "ppiiipppiiippipp",
     "da_pages_append": "pplppiiippiiippiip",
+    "da_pages_append_to": "pplppiiippiiippiipp",
     "da_pages_compact": "ppiiipppiiippplpipp",
     "tree_attn_paged": "pppppppiiippiiiiiipipzp",
     "selected_attn_paged": "pppppppiiippiiiiipipzp",
@@ -593,9 +594,12 @@ def pages_resize(k_pages, v_pages, table, lens, refs, slots, new_lens=None, *, r
 
 
 def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_seqlens=None, max_seqlen=None,
-                 stream=None):
+                 new_lens=None, stream=None):
     """Writes the keys and values of new tokens, [T, Hkv, d] or [layers, T, Hkv, d], as the last
-    ones of their sequences, which pages_resize has made room for (da_pages_append)."""
+    ones of their sequences, which pages_resize has made room for (da_pages_append).  With
+    ``new_lens`` [B], the lengths asked of pages_resize, a sequence that has another length stays as
+    it is: a growth that was refused leaves old tokens where the new ones belong
+    (da_pages_append_to).  A caller that does not look at pages_resize's result before passes it."""
     dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
@@ -607,8 +611,13 @@ def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_
         raise ValueError("k and v must have the same shape")
     T = k.shape[-3]
     B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
-    on.call("da_pages_append", _ptr(k), _ptr(v), T, _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table),
-            _ptr(lens), S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N)
+    args = (_ptr(k), _ptr(v), T, _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), S, M, P,
+            _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N)
+    if new_lens is None:
+        on.call("da_pages_append", *args)
+    else:
+        _ints("new_lens", new_lens, dev, (B,))
+        on.call("da_pages_append_to", *args, _ptr(new_lens))
 
 
 def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_keep, *, result=None, stream=None):

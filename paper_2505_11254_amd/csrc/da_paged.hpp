@@ -43,7 +43,7 @@ hipError_t launch_pages_resize(const Table& t, const Pages& p, const int32_t* sl
                                const int32_t* new_lens, int n, int32_t* result, hipStream_t s);
 hipError_t launch_pages_append(const Table& t, const Pages& p, const uint16_t* k,
                                const uint16_t* v, int64_t T, const int32_t* slots,
-                               const int32_t* cu, int B, int N, hipStream_t s);
+                               const int32_t* cu, int B, int N, const int32_t* new_lens, hipStream_t s);
 hipError_t launch_pages_compact(const Table& t, const Pages& p, const int32_t* slots,
                                 const int32_t* start, const int32_t* keep, int64_t n_keep,
                                 const int32_t* cu_keep, int n, int32_t* result, hipStream_t s);

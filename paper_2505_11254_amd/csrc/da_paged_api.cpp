@@ -194,6 +194,14 @@ da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages
                           int layers, int Hkv, int d, const int32_t* table, const int32_t* lens, int S,
                           int M, int P, const int32_t* slots, const int32_t* cu_seqlens, int B,
                           int max_seqlen, void* stream) {
+  return da_pages_append_to(k, v, T, k_pages, v_pages, layers, Hkv, d, table, lens, S, M, P, slots, cu_seqlens, B,
+                            max_seqlen, nullptr, stream);
+}
+
+da_status da_pages_append_to(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
+                             int layers, int Hkv, int d, const int32_t* table, const int32_t* lens, int S,
+                             int M, int P, const int32_t* slots, const int32_t* cu_seqlens, int B,
+                             int max_seqlen, const int32_t* new_lens, void* stream) {
   const Table t{const_cast<int32_t*>(table), const_cast<int32_t*>(lens), nullptr, S, M, P};
   if (!k || !v) return DA_ERR_NULL;
   da_status st = check_table(t);
@@ -205,12 +213,13 @@ da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages
   // chunks of 16 bytes per sequence and layer, and workgroups of at least 1024 of them
   const int64_t chunks = (int64_t)max_seqlen * Hkv * (d / 8);
   if (chunks > INT32_MAX || !fits((chunks / 1024 + 1) * B, 256)) return DA_ERR_SHAPE;
-  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cu_seqlens, 4)) return DA_ERR_ALIGN;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cu_seqlens, 4) || !aligned(new_lens, 4))
+    return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
   const Pages p{(uint16_t*)k_pages, (uint16_t*)v_pages, layers, Hkv, d};
   return launched(launch_pages_append(t, p, (const uint16_t*)k, (const uint16_t*)v, T, slots, cu_seqlens, B,
-                                      max_seqlen, (hipStream_t)stream));
+                                      max_seqlen, new_lens, (hipStream_t)stream));
 }
 
 da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, int d, int32_t* table,

@@ -16,7 +16,7 @@ da_status check_device() { return DA_OK; }
 da_status fail_hip(hipError_t) { return DA_ERR_HIP; }
 hipError_t launch_pages_fork(const Table&, const int32_t*, const int32_t*, int, int32_t*, hipStream_t) { ++g_launched; return hipSuccess; }
 hipError_t launch_pages_resize(const Table&, const Pages&, const int32_t*, const int32_t*, int, int32_t*, hipStream_t) { ++g_launched; return hipSuccess; }
-hipError_t launch_pages_append(const Table&, const Pages&, const uint16_t*, const uint16_t*, int64_t, const int32_t*, const int32_t*, int, int, hipStream_t) { ++g_launched; return hipSuccess; }
+hipError_t launch_pages_append(const Table&, const Pages&, const uint16_t*, const uint16_t*, int64_t, const int32_t*, const int32_t*, int, int, const int32_t*, hipStream_t) { ++g_launched; return hipSuccess; }
 hipError_t launch_pages_compact(const Table&, const Pages&, const int32_t*, const int32_t*, const int32_t*, int64_t, const int32_t*, int, int32_t*, hipStream_t) { ++g_launched; return hipSuccess; }
 hipError_t launch_summary(const SummaryArgs&, hipStream_t) { ++g_launched; return hipSuccess; }
 hipError_t launch_select_blocks(const SelectArgs& a, hipStream_t) { ++g_launched; g_select = a; return hipSuccess; }

@@ -244,3 +244,69 @@ def test_calls_replay_in_a_graph():
         step()  # (an eager pass between the replays)
         host()
         c.equal(*g)
+
+
+def test_append_after_a_refused_growth():
+    """Branches that share a page grow past the pool: slots whose growth was refused, and the pages that
+    others hold with them, keep every token, in a step that is captured whole, until pages are
+    free again."""
+    from paper_2505_11254_amd import binding
+    c = Cache(2, 7, 2, 64, 5, 4, 8)
+    c.put(0, 100, [5, 2])
+    c.fork([0, 0, 0], [1, 2, 3])
+    c.put(4, 128, [0, 6])
+    g = c.gpu()
+    slots, kept = [3, 1, 2, 0], _t([4])
+    new = _t([0] * 4)
+    m, cu = [2, 30, 1, 5], [0, 2, 32, 33, 38]
+    k, v = (torch.randn((2, cu[-1], 2, 64), generator=torch.Generator().manual_seed(x)).to(torch.bfloat16) for x in (1, 2))
+    on = (k.cuda(), v.cuda(), _t(slots), _t(cu))
+    res = _t([[0] * 4] * 4)
+
+    def step():
+        binding.pages_resize(*g, on[2], new, result=res)
+        binding.pages_append(*on[:2], *g[:4], slots=on[2], cu_seqlens=on[3], max_seqlen=30, new_lens=new)
+
+    def host(ask):
+        got = c.resize(slots, ask)
+        ok = [x[0] >= 0 for x in got]
+        rows = [i for b in range(4) if ok[b] for i in range(cu[b], cu[b + 1])]
+        ends = [0]
+        for b in range(4):
+            if ok[b]:
+                ends.append(ends[-1] + m[b])
+        c.append([s for b, s in enumerate(slots) if ok[b]], ends, k[:, rows], v[:, rows])
+        return got
+    # (three pages are free: slot 3 copies the shared page, slot 1 copies it and takes one more; slot 2, which
+    # would copy it too, finds none, and slot 0 comes after it)
+    ask = [102, 130, 101, 105]
+    new.copy_(_t(ask))
+    step()
+    got = host(ask)
+    assert [x[0] for x in got] == [102, 130, -1, -1] and res.tolist() == [list(x) for x in got]
+    c.equal(*g)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        if i == 2:  # pages are free again
+            binding.pages_resize(*g, kept)
+            c.resize([4], [0])
+        ask = [int(c.lens[s]) + x for s, x in zip(slots, m)]
+        new.copy_(_t(ask))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = host(ask)
+        assert res.tolist() == [list(x) for x in got]
+        c.equal(*g)
+        assert (min(x[0] for x in got) < 0) == (i < 2)
+
+
+def test_append_checks_new_lens():
+    from paper_2505_11254_amd import binding
+    c = Cache(1, 4, 1, 64, 3, 2, 1)
+    g = c.gpu()
+    k = torch.ones((4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (_t([1]), _t([1, 2, 3]), _t([1, 2]).long(), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises((ValueError, TypeError)):
+            binding.pages_append(k, k, g[0][0], g[1][0], g[2], g[3], B=2, new_lens=bad)

@@ -142,6 +142,17 @@ def test_selection_refuses_lists_past_what_is_counted(lib, top_k):
     assert lib.da_select_pages(*dict(ARGS["da_select_pages"], top_k=top_k).values()) == SHAPE
 
 
+def test_append_to_refuses_as_append_does(lib):
+    """The call with lengths to append to: the same checks, and its own argument's."""
+    for fn, status, names, value in REFUSED:
+        for name in names if fn == "da_pages_append" else ():
+            *args, stream = dict(ARGS[fn], **{name: value}).values()
+            for lens in (None, PTR):
+                assert lib.da_pages_append_to(*args, lens, stream) == status, (name, value)
+    *args, stream = ARGS["da_pages_append"].values()
+    assert lib.da_pages_append_to(*args, PTR + 2, stream) == ALIGN
+
+
 @pytest.mark.parametrize("fn", sorted(ARGS))
 def test_the_arguments_above_are_good(lib, fn):
     """(so that each refusal is that of the one argument that was changed)"""
