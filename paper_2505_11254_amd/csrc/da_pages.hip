@@ -350,7 +350,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Table t, Pages p, cons
   const int len = t.lens[s], pos0 = len - m;
   if (new_lens && len != new_lens[b]) return;
   // (in phases, so that the loads of a thread's chunks are under way together)
-  int at[kAppendPer], e[kAppendPer];
+  int64_t at[kAppendPer];  // (a page of 2^18 kv heads passes 2^31 elements)
+  int e[kAppendPer];
   u32x4 x[kAppendPer];
 #pragma unroll
   for (int j = 0; j < kAppendPer; ++j) {
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Table t, Pages p, cons
     const bool inside = c < chunks && pos >= 0 && pos < t.M * kPage;
     e[j] = inside ? t.table[(int64_t)s * t.M + pos / kPage] : -1;
     x[j] = *(const u32x4*)(src + (base + i) * (int64_t)p.Hkv * p.d + w * 8);
-    at[j] = (w / per_head * kPage + pos % kPage) * p.d + w % per_head * 8;
+    at[j] = (int64_t)(w / per_head * kPage + pos % kPage) * p.d + w % per_head * 8;
   }
 #pragma unroll
   for (int j = 0; j < kAppendPer; ++j)

@@ -310,3 +310,18 @@ def test_append_checks_new_lens():
     for bad in (_t([1]), _t([1, 2, 3]), _t([1, 2]).long(), torch.zeros(2, dtype=torch.int32)):
         with pytest.raises((ValueError, TypeError)):
             binding.pages_append(k, k, g[0][0], g[1][0], g[2], g[3], B=2, new_lens=bad)
+
+
+def test_append_to_a_page_past_32_bits():
+    """One page of more than 2^31 elements: its last kv heads' rows."""
+    from paper_2505_11254_amd import binding
+    Hkv, d = (1 << 18) + 3, 128
+    kp = torch.zeros((1, Hkv, PAGE, d), dtype=torch.bfloat16, device="cuda")
+    vp = torch.zeros_like(kp)
+    assert kp.numel() > 1 << 31
+    k = torch.randn((3, Hkv, d), device="cuda", dtype=torch.bfloat16)
+    v = torch.randn_like(k)
+    binding.pages_append(k, v, kp, vp, _t([[0]]), _t([PAGE - 1]), B=1)
+    for pages, want in ((kp, k), (vp, v)):
+        assert torch.equal(pages[0, :, 60:63], want.transpose(0, 1))
+        assert not pages[0, :, :60].any() and not pages[0, :, 63:].any()
