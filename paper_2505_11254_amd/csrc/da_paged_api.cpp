@@ -211,8 +211,8 @@ da_status da_pages_append_to(const void* k, const void* v, int64_t T, void* k_pa
   if (B < 1 || max_seqlen < 1 || T < 0 || (!slots && B > S)) return DA_ERR_SHAPE;
   if (!cu_seqlens && (int64_t)B * max_seqlen != T) return DA_ERR_SHAPE;
   // chunks of 16 bytes per sequence and layer, and workgroups of at least 1024 of them
-  const int64_t chunks = (int64_t)max_seqlen * Hkv * (d / 8);
-  if (chunks > INT32_MAX || !fits((chunks / 1024 + 1) * B, 256)) return DA_ERR_SHAPE;
+  const int64_t row = (int64_t)Hkv * (d / 8);
+  if (row > INT32_MAX / max_seqlen || !fits((max_seqlen * row / 1024 + 1) * B, 256)) return DA_ERR_SHAPE;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cu_seqlens, 4) || !aligned(new_lens, 4))
     return DA_ERR_ALIGN;
   st = check_device();

@@ -128,6 +128,13 @@ def test_calls_refuse_what_no_launch_can_hold(lib, fn, sizes):
     assert getattr(lib, fn)(*dict(ARGS[fn], **sizes).values()) == SHAPE
 
 
+@pytest.mark.parametrize("sizes", [dict(N=(1 << 31) - 1, Hkv=(1 << 31) - 1), dict(N=(1 << 31) - 1, Hkv=1 << 30, d=64),
+                                   dict(N=1 << 30, Hkv=1 << 30), dict(N=3, Hkv=1 << 28)])
+def test_append_refuses_sizes_whose_product_wraps(lib, sizes):
+    a = dict(ARGS["da_pages_append"], B=1, T=1, **sizes)
+    assert lib.da_pages_append(*a.values()) == SHAPE
+
+
 @pytest.mark.parametrize("top_k", [(1 << 30) + 1, (1 << 31) - 2, (1 << 31) - 1])
 def test_attention_refuses_lists_past_what_is_counted(lib, top_k):
     """A list and its own page are counted in 32 bits: one page more than the largest int is no small list."""
