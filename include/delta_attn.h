@@ -528,7 +528,7 @@ da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* ta
  * da_select_pages (decode): a group is one token in the heads of one kv head, its
  * candidates the pages before the token's own.  Writes page positions (indices into
  * the slot's table row) pages [T, Hkv, top_k], ascending, -1 behind the last; top_k is at
- * most 2^30.
+ * most 2^30, and a group has less than 2^31 channels.
  * workspace: da_select_pages_workspace_bytes() bytes (0 up to max_len 65599); none when
  * max_len / 64 <= top_k.
  */

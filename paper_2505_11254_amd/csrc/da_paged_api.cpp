@@ -376,6 +376,8 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
   if (max_len < 1 || (!slots && B > S)) return DA_ERR_SHAPE;
   if (top_k < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > top_k) return DA_ERR_PARAM;
   if (top_k > kMaxList) return DA_ERR_SHAPE;
+  // (places inside a token's heads of one kv head are 32-bit)
+  if (Hq / Hkv > INT32_MAX / d) return DA_ERR_SHAPE;
   const int64_t room = (int64_t)M * kPage;
   if (max_len > room) max_len = (int)room;
   if (max_len / kPage > kMaxCandPages) return DA_ERR_UNSUPPORTED;

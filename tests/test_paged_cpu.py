@@ -135,6 +135,13 @@ def test_append_refuses_sizes_whose_product_wraps(lib, sizes):
     assert lib.da_pages_append(*a.values()) == SHAPE
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(1 << 24, 1, 128), (1 << 26, 2, 64), ((1 << 27) - 1, 1, 128)])
+def test_page_selection_refuses_groups_past_32_bits(lib, Hq, Hkv, d):
+    """Channels of a token's heads on one kv head are counted in 32 bits."""
+    a = dict(ARGS["da_select_pages"], B=1, N=1, Hq=Hq, Hkv=Hkv, d=d)
+    assert lib.da_select_pages(*a.values()) == SHAPE
+
+
 @pytest.mark.parametrize("top_k", [(1 << 30) + 1, (1 << 31) - 2, (1 << 31) - 1])
 def test_attention_refuses_lists_past_what_is_counted(lib, top_k):
     """A list and its own page are counted in 32 bits: one page more than the largest int is no small list."""
