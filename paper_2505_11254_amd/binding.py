@@ -472,6 +472,12 @@ class _On:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.dev)
 
+    def full(self, n, value, dtype):
+        if self.stream is None:
+            return torch.full((n,), value, dtype=dtype, device=self.dev)
+        with torch.cuda.stream(self.stream):
+            return torch.full((n,), value, dtype=dtype, device=self.dev)
+
     def like(self, t, shape=None):
         """A new tensor of t's type (and shape); t lies on the device (cheaper than `empty`)."""
         if self.stream is None:
@@ -767,7 +773,8 @@ def select_blocks(q, codes, scales, *, top_k, block_q, n_sink=1, n_recent=1, B=N
                   block_ptr=None, block_idx=None, stream=None):
     """The key tiles that each query block of block_q rows attends to, by score against key_summary's
     summaries: (block_ptr, block_idx) for blocksparse_attn_prefill and delta_attn_prefill_blocksparse
-    (da_select_blocks)."""
+    (da_select_blocks).  A prompt within one query block has no lists: block_idx is then one -1, as
+    those calls take no empty tensor."""
     on = _On(q.device, stream)
     _on_device("q", q, on.dev, torch.bfloat16)
     if q.dim() != 3 or codes.dim() != 3:
@@ -784,7 +791,7 @@ def select_blocks(q, codes, scales, *, top_k, block_q, n_sink=1, n_recent=1, B=N
     if block_ptr is None:
         block_ptr = on.empty((B, Hkv, nqb + 1), torch.int32)
     if block_idx is None:
-        block_idx = on.empty(max(entries, 1), torch.int32)[:entries] if entries else on.empty(1, torch.int32)
+        block_idx = on.empty(entries, torch.int32) if entries else on.full(1, -1, torch.int32)
     _ints("block_ptr", block_ptr, on.dev, (B, Hkv, nqb + 1))
     _ints("block_idx", block_idx, on.dev)
     if block_idx.numel() < max(entries, 1):

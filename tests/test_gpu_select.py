@@ -299,3 +299,27 @@ def test_more_blocks_than_there_are(block_q, top_k):
         for h in range(Hkv):
             for j in range(n_qb):
                 assert idx[ptr[b][h][j]:ptr[b][h][j + 1]] == list(range(min(top_k, j * R)))
+
+
+@pytest.mark.parametrize("lens,block_q", [([1], 64), ([64], 64), ([200, 256, 0, 13], 256)])
+def test_prompts_within_one_query_block(lens, block_q):
+    """No lists at all: block_idx holds nothing but -1, on another stream too, and the attention over it is
+    each block's own tiles."""
+    from paper_2505_11254_amd import binding
+    g = torch.Generator().manual_seed(block_q)
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    q, k, v = (torch.randn((cu[-1], h, 64), generator=g).to(torch.bfloat16).cuda() for h in (8, 2, 2))
+    kw = dict(cu_seqlens=torch.tensor(cu, dtype=torch.int32).cuda(), max_seqlen=max(lens))
+    sums = binding.key_summary(k, **kw)
+    torch.full((1000,), 7, dtype=torch.int32, device="cuda")  # (freed memory that is not -1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        ptr, idx = binding.select_blocks(q, *sums, top_k=4, block_q=block_q, stream=stream, **kw)
+        side.synchronize()
+        assert idx.tolist() == [-1] and not ptr.any()
+    out = binding.blocksparse_attn_prefill(q, k, v, block_q=block_q, block_ptr=ptr, block_idx=idx, **kw)
+    dense = binding.dense_causal_attn_prefill(q, k, v, **kw)
+    assert (out.float() - dense.float()).abs().max() <= 2 ** -6 * v.abs().max()
