@@ -477,7 +477,10 @@ da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, in
  *     is set (64 * mask_words >= max_seqlen), itself included or not.
  * A row that sees no token is 0.  Keys and values of all L tokens must be finite.
  * max_len: no slot is longer; tokens past it are ignored.  lse (fp32 [T, Hq], may be
- * NULL): log of the sum of exp(q.k / sqrt d), -inf for a row that sees nothing.
+ * NULL): log of the sum of exp(q.k / sqrt d), -inf for a row that sees nothing.  Where more
+ * than 32 rows (new tokens times heads) share a kv head its terms are rounded to bf16, by at
+ * most 2^-8 of each, as the weights of the values are, and lse is off by up to 2^-8; with
+ * up to 32 rows (max_seqlen * Hq / Hkv of them) the terms are fp32.
  * workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, 0) bytes (may
  * be 0).  At most 2^31 - 1 pages may be read in all, counted per kv head and workgroup's
  * worth of rows (32 to 256), with every length max_len: else DA_ERR_SHAPE.
@@ -549,8 +552,8 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
  * Attention of the last m tokens of each sequence over selected pages: the row of
  * token p in kv head g sees the whole pages pages[row][g][0 .. top_k-1] (positions below
  * p / 64, each at most once; other values are skipped) and its own page up to itself.
- * top_k is at most 2^30.  lse as tree_attn_paged; workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d,
- * 1, top_k) bytes.
+ * top_k is at most 2^30.  lse as tree_attn_paged, its rows being the heads of one token;
+ * workspace: da_paged_workspace_bytes(B, max_seqlen, Hq, Hkv, d, 1, top_k) bytes.
  */
 da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out,
                               float* lse, const int32_t* table, const int32_t* lens, int S, int M,

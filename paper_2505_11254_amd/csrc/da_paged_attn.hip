@@ -54,6 +54,13 @@ struct Shape {
   static constexpr int regions = UNIT * D * 2 / 1024;  // 1 KB DMA regions per tile
   static constexpr int RPW = regions / RT;             // of a wave
   static constexpr int ldsBytes = ringElems * 2 + kIdPages * 4 + 256;
+  // Weights as two bf16 parts, the nearest value and what it leaves (2^-16 of a weight is lost
+  // instead of 2^-8): the root mean square error of the outputs is that of their own rounding.
+  // One row tile has matrix cores to spare behind HBM: 64 single tokens over 8192 keys 239.8 -> 241.1
+  // us, one over 131072 104.9 -> 105.6, 16 over 64 pages each 64.1 -> 65.3.  More tiles do not: two
+  // 52.9 -> 58.8 (16 trees of 12), 31.5 -> 36.1 (d = 64), four 58.5 -> 73.1 (16 of 24), eight 255 ->
+  // 353 (4 of 64, 64 heads); their weights are rounded once.
+  static constexpr bool TWO_PARTS = RT == 1;
   // waves per SIMD that LDS has room for
   static constexpr int WAVES = ldsBytes > 81920 ? 1 : 2;
   __device__ static constexpr int kswz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
@@ -423,9 +430,10 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
         for (int q = 0; q < 16; ++q) sc[nb][q] = (vis >> (8 * (q >> 2) + (q & 3))) & 1u ? sc[nb][q] : -INFINITY;
       }
     }
-    // Weights are rounded to bf16 for the second product; the normaliser sums the
-    // rounded ones, so that the rounding cancels where one key dominates.
-    bf16x8 pf[2 * NB];
+    // Weights are bf16 in the second product: two parts of each, and the normaliser sums the
+    // fp32 ones; or the nearest value, and the normaliser sums those, so that the rounding
+    // cancels where one key dominates.
+    bf16x8 pf[2 * NB], rest[2 * NB];
     auto weights = [&]() {
       f32x16 p[NB];
 #pragma unroll
@@ -438,6 +446,20 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
         pf[2 * nb + 1] = __builtin_convertvector(p[nb].hi, bf16x8);
       }
       float ta = 0.f, tb = 0.f;
+      if constexpr (SH::TWO_PARTS) {
+        auto left = [](f32x8 x, bf16x8 y) { return __builtin_convertvector(x - __builtin_convertvector(y, f32x8), bf16x8); };
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          rest[2 * nb] = left(p[nb].lo, pf[2 * nb]);
+          rest[2 * nb + 1] = left(p[nb].hi, pf[2 * nb + 1]);
+#pragma unroll
+          for (int q = 0; q < 16; q += 2) {
+            ta += p[nb][q];
+            tb += p[nb][q + 1];
+          }
+        }
+        return ta + tb;
+      }
 #pragma unroll
       for (int f = 0; f < 2 * NB; ++f) {
         ta = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pf[f], pf[f], 0, 1), ones2, ta, false);
@@ -495,6 +517,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     for (int i = 0; i < kSums; ++i) {
       __builtin_amdgcn_sched_barrier(0);
       o[i % MB] = mfma32(vf[i % kAhead], pf[i / MB], o[i % MB]);
+      if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf[i % kAhead], rest[i / MB], o[i % MB]);
       if (i + kAhead < kSums) vf[i % kAhead] = vfrag(i + kAhead);
     }
     __builtin_amdgcn_sched_barrier(0);
