@@ -323,3 +323,41 @@ def test_prompts_within_one_query_block(lens, block_q):
     out = binding.blocksparse_attn_prefill(q, k, v, block_q=block_q, block_ptr=ptr, block_idx=idx, **kw)
     dense = binding.dense_causal_attn_prefill(q, k, v, **kw)
     assert (out.float() - dense.float()).abs().max() <= 2 ** -6 * v.abs().max()
+
+
+def test_selection_finds_the_blocks_that_queries_look_for():
+    """Blocks whose keys share a direction, and queries along one of them each: that block is chosen in
+    every query block and for every decoded token, and with it the softmax keeps its mass.  Directions
+    are orthogonal: a query's score of its own block is |q| 3, of another |q| times what the noise of 64
+    keys leaves of its mean, 0.5 / 8 a channel."""
+    from paper_2505_11254_amd import binding
+    g = torch.Generator().manual_seed(3)
+    n, Hq, Hkv, d, top_k = 64, 8, 2, 128, 4
+    T, G = n * 64, Hq // Hkv
+    dirs = torch.linalg.qr(torch.randn((Hkv, d, d), generator=g, dtype=torch.float64))[0].transpose(1, 2)[:, :n]
+    k = 3 * dirs.transpose(0, 1).repeat_interleave(64, 0) + 0.5 * torch.randn((T, Hkv, d), generator=g)
+    want = torch.tensor([[int(torch.randint(0, max(j, 1), (1,), generator=g)) for _ in range(Hkv)] for j in range(n)])
+    aim = torch.stack([dirs[h, want[:, h]] for h in range(Hkv)], 1).repeat_interleave(64, 0)  # [T, Hkv, d]
+    size = 16 + 16 * torch.rand((T, Hq, 1), generator=g)  # (rows of other norms)
+    q = size * aim.repeat_interleave(G, 1) + 0.5 * torch.randn((T, Hq, d), generator=g)
+    q, k = q.to(torch.bfloat16), k.to(torch.bfloat16)
+    ptr, idx = binding.select_blocks(q.cuda(), *binding.key_summary(k.cuda()), top_k=top_k, block_q=64)
+    ptr, idx = ptr.tolist(), idx.tolist()
+    for h in range(Hkv):
+        for j in range(n):
+            mine = idx[ptr[0][h][j]:ptr[0][h][j + 1]]
+            assert j == 0 or int(want[j, h]) in mine
+            if j == n - 1:
+                a = q[j * 64:(j + 1) * 64, h * G:(h + 1) * G].double().reshape(-1, d) @ k[:j * 64, h].double().T / d ** 0.5
+                mass = torch.softmax(a, 1).reshape(len(a), j, 64).sum(2)
+                best = mass.sort(1, descending=True).values[:, :top_k].sum(1)
+                assert (mass[:, mine].sum(1) >= 0.95 * best).all()
+    # decoding: tokens of their own, each with its own block to find
+    kp = k.reshape(n, 64, Hkv, d).transpose(1, 2).contiguous().cuda()
+    table, lens = torch.arange(n, dtype=torch.int32).reshape(1, n).cuda(), torch.tensor([T], dtype=torch.int32).cuda()
+    codes, scales = torch.zeros((n, Hkv, d), dtype=torch.int8, device="cuda"), torch.zeros((n, Hkv), device="cuda")
+    binding.page_summary(kp, table, lens, codes, scales)
+    pages = binding.select_pages(q[::64][-32:].contiguous().cuda(), codes, scales, table, lens, top_k=top_k).tolist()
+    for i, j in enumerate(range(n - 32, n)):
+        for h in range(Hkv):
+            assert int(want[j, h]) in pages[i][h]
