@@ -682,8 +682,10 @@ def tree_attn_paged(q, k_pages, v_pages, table, lens, *, mask=None, slots=None, 
                     max_seqlen=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
     """Attention of the last tokens of each sequence, whose keys and values are in the cache:
     single tokens or causal chunks, or trees of drafts where ``mask`` int64 [T, words] has a bit for
-    each drafted token that a row sees.  ``max_len`` bounds the lengths (default: the table's room).
-    Returns ``out`` [T, Hq, d] (tree_attn_paged)."""
+    each drafted token that a row sees.  ``max_len`` bounds the lengths (default: the table's room):
+    the work is shared out as for sequences that long, which suits short ones in a table with far more
+    room less well (8 of 500 tokens, room for 262144: 13.4 us, with max_len 500 11.5).  Returns ``out``
+    [T, Hq, d] (tree_attn_paged)."""
     dev, _, P, Hkv, d = _pages(k_pages, v_pages)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)

@@ -56,8 +56,8 @@ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 //  - Segments are left whole where their even shares would gain less than the cuts cost:
 //    kCutUs for a second start in a workgroup, two tiles of partial results written and
 //    read, and the merge's launch.  Whole against shared (us; d 128 unless said).  One row
-//    tile: 8 segments of 7 pages 11.4, 14.0, of 16 pages 14.7, 11.2; 64 of 118 pages
-//    61, 43; 384 of 161 pages 240, 230.  Two: 28 of 6 pages 12.9, 16.5; 24 of 34 pages 33, 19.
+//    tile, equal lengths: 8 segments of 7 pages 11.4, 13.2, of 16 pages 16.0, 13.3; 64 of 118
+//    pages 72, 46; 384 of 161 pages 343, 343.  Two: 28 of 6 pages 12.9, 16.5; 24 of 34 pages 33, 19.
 //    Four: 21 of 11 pages 18.8, 27.7; 136 of 74 pages 88, 54; d 64, 240 of 27 pages 28, 34, 82
 //    of 29 pages 28, 19.  Eight: 32 of 19 pages 35, 47; 24 of 50 pages 78, 38; 408 of 23 pages
 //    79, 99.  (Over 290 drawn sizes the rule's choices average within 1 % of the better of

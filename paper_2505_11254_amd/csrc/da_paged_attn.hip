@@ -20,10 +20,10 @@
 // stretch of it, whatever sequences that touches.  Rows whose keys several workgroups
 // have are merged by a second launch.
 //
-// Measured (32 heads on 8, d 128): 64 single tokens over up to 8192 keys, 1.37 GB in 238 us,
-// 5.7 TB/s; one over 131072 keys, 0.54 GB in 96 us; 16 trees of 24 over up to 6000 keys, 0.25 GB
+// Measured (32 heads on 8, d 128): 64 single tokens over up to 8192 keys, 1.37 GB in 239 us,
+// 5.7 TB/s; one over 131072 keys, 0.54 GB in 97 us; 16 trees of 24 over up to 6000 keys, 0.25 GB
 // and 20 GFLOP in 50 us; 64 heads on 8, 4 trees of 64 over up to 40000 keys, 0.50 GB and 238
-// GFLOP in 241 to 256 us, 0.93 to 0.99 PFLOP/s, the matrix cores busy half the time.  (There
+// GFLOP in 234 to 256 us, 0.93 to 1.02 PFLOP/s, the matrix cores busy half the time.  (There
 // rings of 3 and 4 stages took as long as 2: not the latency of the transfers.)  With keys
 // that stay in the L2 it takes a fifth less.
 #include "da_device.hpp"
@@ -57,7 +57,8 @@ struct Shape {
   // Weights as two bf16 parts, the nearest value and what it leaves (2^-16 of a weight is lost
   // instead of 2^-8): the root mean square error of the outputs is that of their own rounding.
   // One row tile has matrix cores to spare behind HBM: 64 single tokens over 8192 keys 239.8 -> 241.1
-  // us, one over 131072 104.9 -> 105.6, 16 over 64 pages each 64.1 -> 65.3.  More tiles do not: two
+  // us, one over 131072 104.9 -> 105.6, 16 over 64 pages each 64.1 -> 65.3 (at worst, bound by
+  // latency, one over 448: 10.5 -> 11.3).  More tiles do not: two
   // 52.9 -> 58.8 (16 trees of 12), 31.5 -> 36.1 (d = 64), four 58.5 -> 73.1 (16 of 24), eight 255 ->
   // 353 (4 of 64, 64 heads); their weights are rounded once.
   static constexpr bool TWO_PARTS = RT == 1;

@@ -127,8 +127,9 @@ __device__ __forceinline__ int block_scan(int x, int* lds, int* total) {
 // its ranks among the free pages, which a scan of the reference counts hands out in
 // ascending order.  Of the holders of one page that all grow in this call, as many
 // copy as there are others left: the last one keeps the page.  Bound by latency, its
-// barriers and dependent reads: 10.5 us for 64 requests that take three pages each or 256
-// that copy one (5 for one or two).
+// barriers and dependent reads: 5 to 6 us for one or two requests, 11 for 64 that take up to
+// a page each, 32 for 256 that copy one (the thread that owns sixteen counts hands out its free
+// pages one after the other).
 constexpr int kPlanThreads = 1024;
 constexpr int kRefsPerThread = 16;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Table t, const int32_t* __restrict__ slots,

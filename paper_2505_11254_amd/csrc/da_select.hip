@@ -46,7 +46,8 @@ __device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
 // halve the sums they keep as they add them up, and each finishes one or two channels.
 // Every key is read once, 1/64 of that written: 16384 tokens of 8 kv heads, d 128 (34 MB) in
 // 8.1 us, 87302 (179 MB) in 50 us, 3.6 TB/s, right after the pages were written; with sums
-// in 32 bits the same.
+// in 32 bits the same: not the arithmetic bounds it, but that a wave ends with its block and
+// reads nothing while it reduces.
 template <int D>
 __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kSteps = kPage / kRows;
