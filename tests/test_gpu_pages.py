@@ -325,3 +325,26 @@ def test_append_to_a_page_past_32_bits():
     for pages, want in ((kp, k), (vp, v)):
         assert torch.equal(pages[0, :, 60:63], want.transpose(0, 1))
         assert not pages[0, :, :60].any() and not pages[0, :, 63:].any()
+
+
+def test_compaction_after_a_refused_growth():
+    """The drafts of a slot that found no page are not there to be kept: its compaction is refused and the
+    slot stays as it was; with nothing to keep it changes nothing either."""
+    from paper_2505_11254_amd import binding
+    c = Cache(2, 3, 1, 64, 2, 3, 5)
+    c.put(0, 60, [2])
+    c.put(1, 128, [0, 1])
+    g = c.gpu()
+    slots, new, cu = [0, 1], [62, 131], [0, 2, 5]
+    k = torch.randn((2, 5, 1, 64)).to(torch.bfloat16)
+    got = binding.pages_resize(*g, _t(slots), _t(new)).tolist()
+    assert [tuple(x) for x in got] == c.resize(slots, new) and [x[0] for x in got] == [62, -1]
+    on = k.cuda()
+    binding.pages_append(on, on, *g[:4], slots=_t(slots), cu_seqlens=_t(cu), max_seqlen=3, new_lens=_t(new))
+    c.append([0], [0, 2], k[:, :2], k[:, :2])
+    c.equal(*g)
+    for keep in ([[1], [0, 2]], [[0], []]):
+        flat, ends = keep[0] + keep[1], [0, len(keep[0]), len(keep[0] + keep[1])]
+        got = binding.pages_compact(*g, _t(slots), _t([60, 128]), _t(flat), _t(ends))[:, 0].tolist()
+        assert got == c.compact(slots, [60, 128], keep) == ([1, -1] if keep[1] else [1, 0])
+        c.equal(*g)
