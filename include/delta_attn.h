@@ -259,6 +259,34 @@ da_status dense_causal_attn_prefill_varlen(const void* q, const void* k, const v
                                            void* stream);
 
 /*
+ * The same attentions under changed scores, for models that cap them or bias them by distance:
+ *   s_ij = q_i.k_j / sqrt d,  s' = cap tanh(s / cap) if cap > 0, else s,
+ *   weight_ij = exp(s'_ij - slopes[h] |i - j|) over the keys that row i sees.
+ * cap: 0 (none), or from 2^-10 to 2^10; a capped score is off by up to cap 2^-21.
+ * slopes: fp32 [Hq] on the device, finite, or NULL (none); a biased score is off by up to |slope| 2^-16.
+ * prefix (dense rows only): int32 [B] on the device, or NULL: rows of sequence b see its first
+ *   prefix[b] tokens (as many as there are; none below 1) whole, and the others up to themselves.
+ * cu_seqlens may be NULL (B sequences of max_seqlen tokens); packed documents see only themselves,
+ * as in the other calls.  The correction is DA_CORR_DELTA's, its workspace
+ * da_workspace_bytes(); everything else, errors included, is as in dense_causal_attn_prefill_varlen,
+ * sparse_attn_prefill_varlen and delta_attn_prefill_varlen, whose results these calls give with
+ * cap 0 and no slopes (dense: nor prefix), and DA_ERR_PARAM for another cap.
+ */
+da_status dense_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* cu_seqlens, int B, int max_seqlen, int Hq,
+                                    int Hkv, int d, float cap, const float* slopes,
+                                    const int32_t* prefix, void* stream);
+da_status sparse_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                     const int32_t* cu_seqlens, int B, int max_seqlen, int Hq,
+                                     int Hkv, int d, int window, int n_sink, float cap,
+                                     const float* slopes, void* stream);
+da_status delta_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* cu_seqlens, int B, int max_seqlen, int Hq,
+                                    int Hkv, int d, int window, int n_sink, int gamma, float cap,
+                                    const float* slopes, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/*
  * For callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid hipMalloc): the whole
  * Delta path of delta_attn_prefill[_varlen] (cu_seqlens NULL: B sequences of
@@ -561,7 +589,93 @@ da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_
                               int max_seqlen, int Hq, int Hkv, int d, const int32_t* pages,
                               int top_k, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace of tree_attn_paged (top_k 0) and selected_attn_paged (max_len 1); 0 if none is
+/*
+ * As tree_attn_paged, under the changed scores of dense_attn_prefill_scored (lse is of those).
+ * The distance is that of the tokens' places, which a tree of drafts does not tell: slopes with
+ * a mask give DA_ERR_PARAM.
+ */
+da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void* v_pages,
+                                 void* out, float* lse, const int32_t* table, const int32_t* lens,
+                                 int S, int M, int P, const int32_t* slots,
+                                 const int32_t* cu_seqlens, int B, int max_seqlen, int max_len,
+                                 int Hq, int Hkv, int d, const uint64_t* mask, int mask_words,
+                                 float cap, const float* slopes, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * The cache in 8 bits, half the bytes of a bf16 one: k_pages and v_pages hold e4m3 codes
+ * (OCP "fn", a byte each) in the same layout, [P, Hkv, 64, d] or [layers, P, Hkv, 64, d], and
+ *   k_scales, v_scales  fp32 [P, Hkv] or [layers, P, Hkv]
+ * the power of two that the codes of each page and kv head count in: value = code * scale,
+ * which bf16 holds exactly.  A scale is 2^e with the least e, from -110 to 119, for which no value
+ * of its page passes 448 * 2^e; codes are the nearest, ties to even, and so a value is off
+ * by at most 2^-4 of itself, or 2^-10 of the scale if that is more.  Magnitudes past 448 * 2^119
+ * count as that; what is not finite becomes NaN and does not count for the scale.
+ * Table, lens, refs, slots and requests are as above: da_pages_fork serves both kinds of cache.
+ * The scales are what these calls leave there; a page that holds no token needs none.
+ *
+ * da_pages8_resize, da_pages8_compact: as da_pages_resize and da_pages_compact.
+ * da_pages8_append: as da_pages_append_to (new_lens may be NULL: whatever the length).  New tokens
+ *   that begin a page set its scale anew; others raise it where they need to, and the page's
+ *   older codes then count in the new one (exactly, as long as they stay above 2^-6 of it, the
+ *   range in which e4m3 keeps its 4 bits; below they are rounded to multiples of 2^-9).
+ * In a compaction a page that tokens move into gets the largest of the scales that its tokens
+ *   had, and their codes count in that likewise.
+ * da_pages8_read: the values of cached tokens as rows k, v [layers, T, Hkv, d] of bf16: row i of
+ *   the m rows of sequence b is token first[b] + i (first NULL: 0); rows of tokens that the
+ *   slot does not hold are left as they are.
+ * da_page8_summary: as da_page_summary, of the values.
+ * append and read take one workgroup of 256 threads per sequence, page touched (up to
+ * (max_seqlen + 62) / 64 + 1), layer, keys or values and kv head: more than 2^24 - 1 is DA_ERR_SHAPE.
+ */
+da_status da_pages8_resize(void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                           int layers, int Hkv, int d, int32_t* table, int32_t* lens,
+                           int32_t* refs, int S, int M, int P, const int32_t* slots,
+                           const int32_t* new_lens, int n, int32_t* result, void* stream);
+da_status da_pages8_append(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
+                           float* k_scales, float* v_scales, int layers, int Hkv, int d,
+                           const int32_t* table, const int32_t* lens, int S, int M, int P,
+                           const int32_t* slots, const int32_t* cu_seqlens, int B,
+                           int max_seqlen, const int32_t* new_lens, void* stream);
+da_status da_pages8_compact(void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                            int layers, int Hkv, int d, int32_t* table, int32_t* lens,
+                            int32_t* refs, int S, int M, int P, const int32_t* slots,
+                            const int32_t* start, const int32_t* keep, int64_t n_keep,
+                            const int32_t* cu_keep, int n, int32_t* result, void* stream);
+da_status da_pages8_read(void* k, void* v, int64_t T, const void* k_pages, const void* v_pages,
+                         const float* k_scales, const float* v_scales, int layers, int Hkv, int d,
+                         const int32_t* table, const int32_t* lens, int S, int M, int P,
+                         const int32_t* slots, const int32_t* cu_seqlens, int B, int max_seqlen,
+                         const int32_t* first, void* stream);
+da_status da_page8_summary(const void* k_pages, const float* k_scales, int Hkv, int d,
+                           const int32_t* table, const int32_t* lens, int S, int M, int P,
+                           const int32_t* slots, const int32_t* first, int B, int max_new,
+                           void* codes, float* scales, void* stream);
+
+/*
+ * Attention over that cache: as tree_attn_paged_scored (cap 0 and slopes NULL: as
+ * tree_attn_paged) and selected_attn_paged of the values.  workspace:
+ * da_paged8_workspace_bytes(), with the arguments of da_paged_workspace_bytes().
+ */
+da_status tree_attn_paged8(const void* q, const void* k_pages, const void* v_pages,
+                           const float* k_scales, const float* v_scales, void* out, float* lse,
+                           const int32_t* table, const int32_t* lens, int S, int M, int P,
+                           const int32_t* slots, const int32_t* cu_seqlens, int B,
+                           int max_seqlen, int max_len, int Hq, int Hkv, int d,
+                           const uint64_t* mask, int mask_words, float cap, const float* slopes,
+                           void* workspace, size_t workspace_bytes, void* stream);
+da_status selected_attn_paged8(const void* q, const void* k_pages, const void* v_pages,
+                               const float* k_scales, const float* v_scales, void* out,
+                               float* lse, const int32_t* table, const int32_t* lens, int S,
+                               int M, int P, const int32_t* slots, const int32_t* cu_seqlens,
+                               int B, int max_seqlen, int Hq, int Hkv, int d,
+                               const int32_t* pages, int top_k, void* workspace,
+                               size_t workspace_bytes, void* stream);
+size_t da_paged8_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len,
+                                 int top_k);
+
+/* Workspace of tree_attn_paged[_scored] (top_k 0) and selected_attn_paged (max_len 1); 0 if none is
  * needed or the sizes are invalid.  Its contents on entry do not matter. */
 size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len,
                                 int top_k);

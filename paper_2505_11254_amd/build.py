@@ -11,8 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdelta_attn.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("da_kernels.hip", "da_api.cpp", "da_pages.hip", "da_select.hip",
-                                          "da_paged_attn.hip", "da_paged_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("da_kernels.hip", "da_api.cpp", "da_pages.hip", "da_pages8.hip", "da_select.hip",
+                                          "da_paged_attn.hip", "da_paged_api.cpp", "da_pages8_api.cpp")]
 ARCH = "gfx950"
 
 

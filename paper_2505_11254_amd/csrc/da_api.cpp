@@ -197,6 +197,10 @@ struct Problem {
   const int32_t* blk_ptr = nullptr;
   const int32_t* blk_idx = nullptr;
   int block_q = 0;
+  // changed scores
+  float cap = 0.f;
+  const float* slopes = nullptr;
+  const int32_t* prefix = nullptr;
 };
 
 // Rows per query head of one sparse workgroup; with key-block lists they must
@@ -223,8 +227,10 @@ da_status validate(const Problem& P, bool need_window, bool need_gamma) {
     if ((int64_t)P.B * P.Hkv * ((int64_t)(P.N + P.block_q - 1) / P.block_q + 1) > INT32_MAX)
       return DA_ERR_SHAPE;
   }
+  if (!cap_ok(P.cap)) return DA_ERR_PARAM;
   if (!aligned16(P.q) || !aligned16(P.k) || !aligned16(P.v) || !aligned16(P.out))
     return DA_ERR_ALIGN;
+  if (((uintptr_t)P.slopes & 3u) != 0 || ((uintptr_t)P.prefix & 3u) != 0) return DA_ERR_ALIGN;
   return DA_OK;
 }
 
@@ -447,6 +453,10 @@ Args base_args(const Problem& P) {
   a.gamma = P.gamma > 0 ? P.gamma : 1;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)P.d));
   a.head_chunk = 8192 / P.d;
+  a.scored = P.cap != 0.f || P.slopes || P.prefix;
+  set_cap(P.cap, P.d, &a.cap2, &a.cap_in);
+  a.slopes = P.slopes;
+  a.prefix = P.prefix;
   return a;
 }
 
@@ -703,6 +713,35 @@ da_status dense_causal_attn_prefill_varlen(const void* q, const void* k, const v
   if (!cu_seqlens) return DA_ERR_NULL;
   Problem P{q, k, v, out, cu_seqlens, B, max_seqlen, Hq, Hkv, d, 1, 0, 1};
   return da::run_plain(P, false, stream);
+}
+
+da_status dense_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv, int d,
+                                    float cap, const float* slopes, const int32_t* prefix, void* stream) {
+  Problem P{q, k, v, out, cu_seqlens, B, max_seqlen, Hq, Hkv, d, 1, 0, 1};
+  P.cap = cap;
+  P.slopes = slopes;
+  P.prefix = prefix;
+  return da::run_plain(P, false, stream);
+}
+
+da_status sparse_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                     const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv, int d,
+                                     int window, int n_sink, float cap, const float* slopes, void* stream) {
+  Problem P{q, k, v, out, cu_seqlens, B, max_seqlen, Hq, Hkv, d, window, n_sink, 1};
+  P.cap = cap;
+  P.slopes = slopes;
+  return da::run_plain(P, true, stream);
+}
+
+da_status delta_attn_prefill_scored(const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv, int d,
+                                    int window, int n_sink, int gamma, float cap, const float* slopes,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  Problem P{q, k, v, out, cu_seqlens, B, max_seqlen, Hq, Hkv, d, window, n_sink, gamma};
+  P.cap = cap;
+  P.slopes = slopes;
+  return da::run_delta(P, workspace, workspace_bytes, stream, DA_STEP_ALL, true);
 }
 
 int da_fused_supported(int Hq, int Hkv, int gamma) {

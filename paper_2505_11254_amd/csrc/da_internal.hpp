@@ -4,6 +4,7 @@
 
 #include <stddef.h>
 #include <stdint.h>
+#include <string.h>
 
 #include <hip/hip_runtime.h>
 
@@ -22,6 +23,25 @@ constexpr int kAttnWaves = 8;
 constexpr int kAttnStages = 2;
 // Delta epilogue workgroups.
 constexpr int kEpiThreads = 256;
+
+// Whether `cap` is one that the scored kernels take: 0 (none), or from 2^-10 to 2^10.  (By its bits,
+// of which the compiler must not know that they are a number's: the library is compiled for numbers
+// without NaN.)
+inline bool cap_ok(float cap) {
+  uint32_t copy;
+  memcpy(&copy, &cap, 4);
+  volatile uint32_t hidden = copy;
+  const uint32_t bits = hidden;
+  const int exponent = (int)(bits >> 23);  // of a positive one
+  return bits << 1 == 0 || (exponent >= 127 - 10 && exponent < 127 + 10) || bits == 0x44800000u;
+}
+// Its coefficients: log2(e) cap, and 2 log2(e) / (cap sqrt(d)).
+inline void set_cap(float cap, int d, float* cap2, float* cap_in) {
+  *cap2 = *cap_in = 0.f;
+  if (cap == 0.f) return;
+  *cap2 = (float)(1.4426950408889634 * cap);
+  *cap_in = (float)(2 * 1.4426950408889634 / (cap * (d == 128 ? 11.313708498984761 : 8.)));
+}
 
 // Division by a divisor fixed for a launch, for numerators below 2^31.  With
 // l = ceil(log2 d) and m = floor(2^(31+l) / d) + 1 < 2^32, floor(x / d) =
@@ -58,6 +78,12 @@ struct Args {
   int Hq, Hkv, d;
   int window, n_sink, gamma;
   float scale_log2;   // log2(e) / sqrt(d): scores are exponentiated with exp2
+  // Changed scores (scored: the kernels that know them; see delta_attn.h)
+  int scored;
+  float cap2;             // log2(e) cap, or 0
+  float cap_in;           // 2 log2(e) / (cap sqrt(d))
+  const float* slopes;    // [Hq], or nullptr
+  const int32_t* prefix;  // [B], or nullptr (dense causal rows only)
   // Anchors a < cover have a sparse key set equal to [0, a], so Delta = 0 there
   // and their groups keep the sparse rows: n_sink + window for sink + window
   // attention, 0 for key-block lists.

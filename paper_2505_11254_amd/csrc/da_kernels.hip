@@ -134,8 +134,9 @@ constexpr int lds_bytes(int pre_bytes) {
          (MODE == kSparse ? pre_bytes + (NW > 4 ? (NW - 4) * kRowsPerWave * D * 2 : 0) : 0);
 }
 
-// One attention workgroup, block `bid` of the launch's `nblk`.
-template <int D, int MODE, int NW>
+// One attention workgroup, block `bid` of the launch's `nblk`.  SC: scores are capped, biased by
+// distance, or (dense) a prefix of the keys is seen by every row.
+template <int D, int MODE, int NW, bool SC>
 __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t nblk) {
   using LD = Lds<D, NW>;
   constexpr int NS = kAttnStages;
@@ -235,6 +236,8 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   const int R1 = min(R0 + rows_per_block, n_rows);
   const int bpos_lo = row_pos<MODE>(R0, nA, Lc, a.gamma);
   const int bpos_hi = row_pos<MODE>(R1 - 1, nA, Lc, a.gamma);
+  // the last key that rows short of it see as well (-1: none)
+  const int see = SC && MODE == kDense && a.prefix ? min(a.prefix[b], L) - 1 : -1;
 
   // ---- key tiles the block visits: [ta0, ta1) then [tb0, tb1)
   int ta0 = 0, ta1 = 0, tb0 = 0, tb1 = 0;
@@ -256,7 +259,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
     tb0 = max(ws / kKeyTile, ta1);
     tb1 = max(tb0, bpos_hi / kKeyTile + 1);
   } else if (MODE == kDense) {
-    ta1 = bpos_hi / kKeyTile + 1;
+    ta1 = (SC ? max(bpos_hi, see) : bpos_hi) / kKeyTile + 1;
   } else {
     const int64_t kc0 = (int64_t)c * a.chunk;
     if (kc0 > bpos_hi) return;  // this key chunk lies past every row of the block
@@ -279,9 +282,10 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   const int my_r = wr0 + col;
   const bool row_valid = my_r < R1;
   const int my_pos = row_valid ? row_pos<MODE>(my_r, nA, Lc, a.gamma) : -1;
-  const int wpos_lo = wave_has_rows ? row_pos<MODE>(wr0, nA, Lc, a.gamma) : 0;
-  const int wpos_hi = wave_has_rows ? row_pos<MODE>(min(wr0 + kRowsPerWave, R1) - 1, nA, Lc,
-                                                    a.gamma) : -1;
+  auto sees = [&](int pos) { return SC ? max(pos, see) : pos; };  // the last key of a causal row
+  const int wpos_lo = sees(wave_has_rows ? row_pos<MODE>(wr0, nA, Lc, a.gamma) : 0);
+  const int wpos_hi = sees(wave_has_rows ? row_pos<MODE>(min(wr0 + kRowsPerWave, R1) - 1, nA, Lc,
+                                                         a.gamma) : -1);
 
   bf16x8 qf[D / 16];  // the wave's queries (loaded in the prologue below)
   const int64_t kv_stride = (int64_t)a.Hkv * D;  // elements between consecutive keys
@@ -355,7 +359,11 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
                 (tr_m & 1) * 4;
 
   // list entries outside [0, diag0) are not part of the key set (-1: skipped)
+  // (biased scores fall with the distance: the nearest keys first, so that the reference of the
+  // softmax, which only moves up, stays where they put it)
+  const bool back = SC && a.slopes;
   auto tile_at = [&](int it) -> int {
+    if (back) it = n_iter - 1 - it;
     if (it >= n_a) return tb0 + (it - n_a);
     if (MODE == kSparse && a.blk_ptr) {
       const int e = __builtin_amdgcn_readfirstlane(a.blk_idx[lst0 + it]);
@@ -391,7 +399,8 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // score accumulators start from, so that c times them is logit - ref.
   // (Scaling the queries by c ahead of the MFMA would round c q to bf16 once
   // more, an error proportional to the logits themselves.)
-  const float qscale = a.scale_log2, inv_qscale = 1.f / a.scale_log2;
+  // (Changed scores are in base-2 units, with ref subtracted, as they come.)
+  const float qscale = SC ? 1.f : a.scale_log2, inv_qscale = SC ? 1.f : 1.f / a.scale_log2;
   float ref = 0.f;
   bool has_ref = false;
   f32x16 nref = f32x16{};
@@ -406,17 +415,46 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // error 0.00246, as in one chunk, in place of 0.00296; 4021 tokens, window 2048
   // 0.00245, 0.00274 in two long chunks).  It costs the keys of one more tile per
   // workgroup, 0-1 % of a whole call.
-  const bool split = MODE == kDenseRows && a.split_ref && c > 0;
+  const bool split = MODE == kDenseRows && a.split_ref && c > 0 && !back;
   float ref0 = 0.f;
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+
+  // Changed scores, in base-2 units: cap tanh(q.k / (cap sqrt d)) - slope |i - j| - ref.  With
+  // e = exp2(2 log2(e) x), tanh x = 1 - 2 / (1 + e), whose error, some 2^-22, counts cap times:
+  // 2e-5 of a logit at cap 50.
+  const float slope = back ? a.slopes[h] * 1.4426950408889634f : 0.f;
+  auto change = [&](int tile, f32x16& s0, f32x16& s1) {
+    const float dist0 = (float)(tile * kKeyTile + 4 * half - my_pos);  // j - i of offset 0
+    const bool ahead = see >= 0;  // some rows see keys past them
+    const float base = (back && !ahead ? slope * dist0 : 0.f) - ref;
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float o0 = (float)(8 * (r >> 2) + (r & 3));
+        s0[r] = f(s0[r], o0);
+        s1[r] = f(s1[r], o0 + 32.f);
+      }
+    };
+    if (a.cap2 > 0.f) {
+      const float c = a.cap_in, m = -2.f * a.cap2, top = a.cap2 + base;
+      each([&](float x, float) { return __builtin_fmaf(m, __builtin_amdgcn_rcpf(1.f + fast_exp2(c * x)), top); });
+    } else {
+      const float c = a.scale_log2;
+      each([&](float x, float) { return __builtin_fmaf(c, x, base); });
+    }
+    if (back && !ahead)
+      each([&](float x, float o) { return __builtin_fmaf(slope, o, x); });
+    else if (back)
+      each([&](float x, float o) { return __builtin_fmaf(-slope, fabsf(dist0 + o), x); });
+  };
 
   // S^T of one tile against the wave's rows (register r of lane half h holds
   // key 8*(r/4) + 4*h + r%4 in s0, that key + 32 in s1); keys outside a row's
   // key set read -inf when `masked`.
   auto qk = [&](const uint16_t* ks, int tile, int masked, f32x16& s0, f32x16& s1) {
-    s0 = nref;
-    s1 = nref;
+    s0 = SC ? f32x16{} : nref;
+    s1 = SC ? f32x16{} : nref;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const bf16x8 ka = *(const bf16x8*)(ks + kread[kk]);
@@ -433,13 +471,14 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    if constexpr (SC) change(tile, s0, s1);
     // accumulator register r of lane half h holds key kbase_t + o with the
     // constant offset o = 8*(r/4) + r%4 (+32 in s1); the tests compare o
     // against per-lane bounds: causal o <= my_pos - kbase_t, window
     // o > my_pos - kbase_t - window, sink o < n_sink - kbase_t
     if (masked) {
       const int kbase_t = tile * kKeyTile + 4 * half;
-      const int lim_c = my_pos - kbase_t;
+      const int lim_c = sees(my_pos) - kbase_t;
       // (64-bit: the window may be as large as INT_MAX; every offset is >= 0,
       // so a bound clamped at -1 admits the whole tile, as such a window does)
       const int lim_w = (int)max((int64_t)lim_c - (int64_t)a.window, (int64_t)-1);
@@ -544,7 +583,8 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
       if (__any(grow)) {
         float up = mx;
         if (split) up = has_ref ? ceilf(mx) : ref0 + ceilf(mx - ref0);
-        const float dm = has_ref ? fmaxf(up, 0.f) : (seen ? up : 0.f);
+        float dm = has_ref ? fmaxf(up, 0.f) : (seen ? up : 0.f);
+        if constexpr (SC) dm = (ref + dm) - ref;  // (a bias may be large: what the sum rounds off counts)
         const float alpha = has_ref ? fast_exp2(-dm) : 0.f;  // l and O are still zero without one
         ref += dm;
         has_ref = has_ref || seen;
@@ -601,7 +641,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // written as zeros.  Only a block whose first NS tiles include its last one
   // (the only tile that can end inside the sequence's last 64 keys) clears
   // the ring first, so that no stage can hold bits left by an earlier kernel.
-  if (n_iter <= NS) {
+  if (n_iter <= NS || back) {
     for (int i = tid; i < NS * LD::stageElems / 8; i += kThreads)
       *(u32x4*)(smem + 8 * i) = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
@@ -948,9 +988,9 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
 #define DA_ATTN_KERNEL(D, NW) \
   __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 64 && NW == 4 ? 3 : 2)))
 
-template <int D, int MODE, int NW>
+template <int D, int MODE, int NW, bool SC>
 DA_ATTN_KERNEL(D, NW) void attn_kernel(Args a) {
-  attn_body<D, MODE, NW>(a, blockIdx.x, gridDim.x);
+  attn_body<D, MODE, NW, SC>(a, blockIdx.x, gridDim.x);
 }
 
 // The strided dense rows (`ar`, the first nr blocks: longer ones) and the sparse
@@ -962,12 +1002,12 @@ DA_ATTN_KERNEL(D, NW) void attn_kernel(Args a) {
 // tokens 36.0 -> 27.5 us, 4000 tokens 89 -> 77 us, 16000 tokens 302 -> 279 us;
 // Delta, GQA 3, gamma 48, 20K tokens 433 -> 402 us; EMA 64K tokens 2791 -> 2763
 // us; 131K tokens, 32 heads 6622 -> 6697 us (64 rounds of the CUs: not taken).
-template <int D, int NW>
+template <int D, int NW, bool SC>
 DA_ATTN_KERNEL(D, NW) void attn_pair_kernel(Args ar, Args as, uint32_t nr, uint32_t nr8) {
   if (blockIdx.x >= nr8)
-    attn_body<D, kSparse, NW>(as, blockIdx.x - nr8, gridDim.x - nr8);
+    attn_body<D, kSparse, NW, SC>(as, blockIdx.x - nr8, gridDim.x - nr8);
   else if (blockIdx.x < nr)
-    attn_body<D, kDenseRows, NW>(ar, blockIdx.x, nr);
+    attn_body<D, kDenseRows, NW, SC>(ar, blockIdx.x, nr);
 }
 #undef DA_ATTN_KERNEL
 
@@ -1480,15 +1520,15 @@ int pre_bytes(const Args& a) {
   return a.fuse && a.gamma > 1 ? a.hpw * (kRowsPerWave * a.ppw / a.gamma) * a.d * 4 : 0;
 }
 
-template <int MODE>
-hipError_t launch_attn(const Args& a0, hipStream_t s, int64_t nblocks) {
+template <int MODE, bool SC>
+hipError_t launch_attn_as(const Args& a0, hipStream_t s, int64_t nblocks) {
   if (nblocks <= 0) return hipSuccess;
   if (nblocks > INT32_MAX) return hipErrorInvalidValue;
   Args a = a0;
   prepare_attn<MODE>(a, nblocks);
   const int pre = MODE == kSparse ? pre_bytes(a) : 0;
 #define DA_ATTN(DD, W)                                                                          \
-  hipLaunchKernelGGL((attn_kernel<DD, MODE, W>), dim3((unsigned)nblocks), dim3(64 * W),         \
+  hipLaunchKernelGGL((attn_kernel<DD, MODE, W, SC>), dim3((unsigned)nblocks), dim3(64 * W),         \
                      (lds_bytes<DD, MODE, W>(pre)), s, a)
   const int waves = a.hpw * a.ppw;
   if (a.d == 128) {
@@ -1502,6 +1542,11 @@ hipError_t launch_attn(const Args& a0, hipStream_t s, int64_t nblocks) {
   }
 #undef DA_ATTN
   return hipGetLastError();
+}
+
+template <int MODE>
+hipError_t launch_attn(const Args& a, hipStream_t s, int64_t nblocks) {
+  return a.scored ? launch_attn_as<MODE, true>(a, s, nblocks) : launch_attn_as<MODE, false>(a, s, nblocks);
 }
 
 constexpr int kScratchDevices = 64;
@@ -1601,9 +1646,14 @@ hipError_t launch_sparse(const Args& a0, hipStream_t s) {
   prepare_attn<kSparse>(as, ns);
   const dim3 g((unsigned)(nr8 + ns));
   const int pre = pre_bytes(as);
-#define DA_PAIR(DD, W)                                                                          \
-  hipLaunchKernelGGL((attn_pair_kernel<DD, W>), g, dim3(64 * W), (lds_bytes<DD, kSparse, W>(pre)), \
+#define DA_PAIR_AS(DD, W, SC)                                                                      \
+  hipLaunchKernelGGL((attn_pair_kernel<DD, W, SC>), g, dim3(64 * W), (lds_bytes<DD, kSparse, W>(pre)), \
                      s, ar, as, (uint32_t)nr, (uint32_t)nr8)
+#define DA_PAIR(DD, W)              \
+  do {                              \
+    if (as.scored) DA_PAIR_AS(DD, W, true); \
+    else DA_PAIR_AS(DD, W, false);  \
+  } while (0)
   if (as.d == 128) {
     if (waves == 8) DA_PAIR(128, 8);
     else DA_PAIR(128, 4);
@@ -1611,6 +1661,7 @@ hipError_t launch_sparse(const Args& a0, hipStream_t s) {
     DA_PAIR(64, 4);
   }
 #undef DA_PAIR
+#undef DA_PAIR_AS
   return hipGetLastError();
 }
 

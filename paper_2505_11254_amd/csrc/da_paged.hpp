@@ -30,12 +30,26 @@ struct Table {
   int S, M, P;
 };
 
-// Its pages [layers][P][Hkv][64][d] (bf16).
+// Its pages [layers][P][Hkv][64][d] (bf16).  (Of codes a row counts as d / 2 of these elements, and
+// the scales [layers][P][Hkv] go with it.)
 struct Pages {
   uint16_t* k;
   uint16_t* v;
   int layers, Hkv, d;
+  float* k_scales = nullptr;
+  float* v_scales = nullptr;
 };
+
+// The same in 8 bits: e4m3 codes, and the powers of two they count in, [layers][P][Hkv].
+struct Pages8 {
+  uint8_t* k;
+  uint8_t* v;
+  float* k_scales;
+  float* v_scales;
+  int layers, Hkv, d;
+};
+// Pages that N tokens from anywhere in a page on can touch.
+__host__ __device__ __forceinline__ int pages8_parts(int N) { return (int)(((int64_t)N + kPage - 2) / kPage) + 1; }
 
 hipError_t launch_pages_fork(const Table& t, const int32_t* src, const int32_t* dst, int n,
                              int32_t* result, hipStream_t s);
@@ -47,11 +61,25 @@ hipError_t launch_pages_append(const Table& t, const Pages& p, const uint16_t* k
 hipError_t launch_pages_compact(const Table& t, const Pages& p, const int32_t* slots,
                                 const int32_t* start, const int32_t* keep, int64_t n_keep,
                                 const int32_t* cu_keep, int n, int32_t* result, hipStream_t s);
+// The check of a compaction, which sets the new lengths (its first launch).
+hipError_t launch_compact_check(const Table& t, const int32_t* slots, const int32_t* start, const int32_t* keep,
+                                int64_t n_keep, const int32_t* cu_keep, int n, int32_t* result, hipStream_t s);
+
+hipError_t launch_pages8_append(const Table& t, const Pages8& p, const uint16_t* k, const uint16_t* v,
+                                int64_t T, const int32_t* slots, const int32_t* cu, int B, int N,
+                                const int32_t* new_lens, hipStream_t s);
+hipError_t launch_pages8_read(const Table& t, const Pages8& p, uint16_t* k, uint16_t* v, int64_t T,
+                              const int32_t* slots, const int32_t* cu, int B, int N, const int32_t* first,
+                              hipStream_t s);
+hipError_t launch_pages8_compact(const Table& t, const Pages8& p, const int32_t* slots, const int32_t* start,
+                                 const int32_t* keep, int64_t n_keep, const int32_t* cu_keep, int n,
+                                 int32_t* result, hipStream_t s);
 
 // Where the keys of a summary lie: rows of a packed or fixed-length batch
 // (table == nullptr), or pages.
 struct SummaryArgs {
-  const uint16_t* k;
+  const void* k;         // bf16, or e4m3 codes
+  const float* k_scales;  // [P][Hkv] of codes, or nullptr: bf16
   const int32_t* cu;     // [B + 1], or nullptr for B sequences of N tokens
   const int32_t* table;  // [S][M], or nullptr
   const int32_t* lens;   // [S]
@@ -98,8 +126,14 @@ hipError_t launch_select_pages(const SelectArgs& a, hipStream_t s);
 // Attention over the pages.
 struct PagedArgs {
   const uint16_t* q;     // [T][Hq][d]
-  const uint16_t* k;     // [P][Hkv][64][d]
-  const uint16_t* v;
+  const void* k;         // [P][Hkv][64][d] bf16, or e4m3 codes
+  const void* v;
+  const float* k_scales;  // [P][Hkv] powers of two of the codes, or nullptr: bf16
+  const float* v_scales;
+  // Changed scores (scored: the kernels that know them; see delta_attn.h)
+  int scored;
+  float cap2, cap_in;    // log2(e) cap, or 0; 2 log2(e) / (cap sqrt(d))
+  const float* slopes;   // [Hq], or nullptr
   uint16_t* out;         // [T][Hq][d]
   float* lse;            // [T][Hq], or nullptr
   const int32_t* table;  // [S][M]
@@ -130,5 +164,30 @@ __host__ __device__ __forceinline__ int share_of(int min_units, int total, int n
   return even > min_units ? even : min_units;
 }
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s);
+
+// da_paged_api.cpp, for the calls of da_pages8_api.cpp as well: the argument checks, and the calls
+// behind them.
+bool aligned(const void* p, size_t to);
+da_status check_table(const Table& t);
+da_status check_pages(const void* k, const void* v, int layers, int Hkv, int d);
+da_status check_compact(const Table& t, const void* k_pages, const void* v_pages, int layers, int Hkv, int d,
+                        const int32_t* slots, const int32_t* start, const int32_t* keep, int64_t n_keep,
+                        const int32_t* cu_keep, int n, const int32_t* result);
+da_status launched(hipError_t e);
+// d: of the cache (that of p may count otherwise)
+da_status resize_pages(const Pages& p, int d, const Table& t, const int32_t* slots, const int32_t* new_lens, int n,
+                       int32_t* result, void* stream);
+da_status summarise_pages(const void* k_pages, const float* k_scales, int Hkv, int d, const Table& t,
+                          const int32_t* slots, const int32_t* first, int B, int max_new, void* codes, float* scales,
+                          void* stream);
+PagedArgs paged_args(const void* q, const void* k_pages, const void* v_pages, void* out, float* lse,
+                     const int32_t* table, const int32_t* lens, int S, int M, int P, const int32_t* slots,
+                     const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv, int d);
+// over every page, of slots up to max_len (a.mask, a.slopes, a.k_scales as they are)
+da_status attend_pages(PagedArgs a, int max_len, float cap, void* workspace, size_t workspace_bytes, void* stream);
+// over the lists `pages`
+da_status attend_lists(PagedArgs a, const int32_t* pages, int top_k, void* workspace, size_t workspace_bytes,
+                       void* stream);
+size_t paged_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len, int n_list, bool eight);
 
 }  // namespace da

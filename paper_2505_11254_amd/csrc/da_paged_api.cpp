@@ -6,12 +6,10 @@
 #include "da_paged.hpp"
 
 namespace da {
-namespace {
 
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-// Whether a launch can have so many workgroups: its threads are counted in 32 bits.
-bool fits(int64_t wgs, int threads) { return wgs <= (int64_t)UINT32_MAX / threads; }
+da_status launched(hipError_t e) { return e == hipSuccess ? DA_OK : fail_hip(e); }
 
 da_status check_table(const Table& t) {
   if (!t.table || !t.lens) return DA_ERR_NULL;
@@ -30,6 +28,11 @@ da_status check_pages(const void* k, const void* v, int layers, int Hkv, int d) 
   return DA_OK;
 }
 
+namespace {
+
+// Whether a launch can have so many workgroups: its threads are counted in 32 bits.
+bool fits(int64_t wgs, int threads) { return wgs <= (int64_t)UINT32_MAX / threads; }
+
 // A batch of B sequences of up to N tokens with Hq heads on Hkv.
 da_status check_batch(int B, int N, int Hq, int Hkv, int d) {
   if (B < 1 || N < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return DA_ERR_SHAPE;
@@ -44,8 +47,6 @@ da_status check_rows(int B, int N, int Hq, int Hkv, int d) {
   const int64_t tokens = (int64_t)B * N;
   return tokens > INT32_MAX || tokens * Hq > INT32_MAX || !fits((tokens * Hq + 7) / 8, 256) ? DA_ERR_SHAPE : DA_OK;
 }
-
-da_status launched(hipError_t e) { return e == hipSuccess ? DA_OK : fail_hip(e); }
 
 int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 
@@ -71,7 +72,7 @@ struct PagedPlan {
   int row_tiles, n_wgs, min_units, whole, align_pages, row_groups;
   size_t units_bytes, part_rows, bytes;
 };
-da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, PagedPlan* p) {
+da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_list, bool eight, PagedPlan* p) {
   if (n_list > kMaxList) return DA_ERR_SHAPE;
   const int G = Hq / Hkv;
   const int64_t rows = n_list ? G : (int64_t)N * G;
@@ -114,13 +115,16 @@ int64_t list_total(int max_seqlen, int top_k, int block_q) {
   return list_entries_before(((int64_t)max_seqlen + block_q - 1) / block_q, top_k, block_q / kPage);
 }
 
-da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_bytes, void* stream) {
+da_status paged_attn(PagedArgs a, int n_list, float cap, void* workspace, size_t workspace_bytes, void* stream) {
   if (!a.q || !a.k || !a.v || !a.out) return DA_ERR_NULL;
   da_status st = check_table({const_cast<int32_t*>(a.table), const_cast<int32_t*>(a.lens), nullptr, a.S, a.M, a.P});
   if (st != DA_OK) return st;
   st = check_rows(a.B, a.N, a.Hq, a.Hkv, a.d);
   if (st != DA_OK) return st;
   if (!a.slots && a.B > a.S) return DA_ERR_SHAPE;
+  // (the places of a tree's drafts do not tell their distances)
+  if (!cap_ok(cap) || (a.slopes && a.mask)) return DA_ERR_PARAM;
+  if (!aligned(a.slopes, 4)) return DA_ERR_ALIGN;
   if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.out, 16) ||
       !aligned(a.cu, 4) || !aligned(a.slots, 4) || !aligned(a.lse, 4) || !aligned(a.mask, 8) ||
       !aligned(a.lists, 4))
@@ -128,12 +132,14 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
   const int64_t room = (int64_t)a.M * kPage;
   if (a.max_len > room) a.max_len = (int)room;
   PagedPlan p;
-  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, &p);
+  st = paged_plan(a.B, a.N, a.Hq, a.Hkv, a.d, pages_of(a.max_len), n_list, a.k_scales != nullptr, &p);
   if (st != DA_OK) return st;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return DA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
+  a.scored = cap != 0.f || a.slopes;
+  set_cap(cap, a.d, &a.cap2, &a.cap_in);
   a.scale_log2 = 1.4426950408889634f / (a.d == 128 ? 11.313708498984761f : 8.f);
   a.G = a.Hq / a.Hkv;
   a.fd_G = make_fastdiv(a.G);
@@ -153,6 +159,123 @@ da_status paged_attn(PagedArgs a, int n_list, void* workspace, size_t workspace_
 }
 
 }  // namespace
+
+da_status resize_pages(const Pages& p, int d, const Table& t, const int32_t* slots, const int32_t* new_lens, int n,
+                       int32_t* result, void* stream) {
+  if (!t.refs || !slots || !result) return DA_ERR_NULL;
+  da_status st = check_table(t);
+  if (st != DA_OK) return st;
+  st = check_pages(p.k, p.v, p.layers, p.Hkv, d);
+  if (st != DA_OK) return st;
+  if (n < 1 || n > kMaxRequests || p.Hkv > INT32_MAX / 2 / n / p.layers ||
+      !fits((int64_t)n * p.layers * 2 * p.Hkv, 256))
+    return DA_ERR_SHAPE;
+  if (!aligned(slots, 4) || !aligned(new_lens, 4) || !aligned(result, 16)) return DA_ERR_ALIGN;
+  st = check_device();
+  if (st != DA_OK) return st;
+  return launched(launch_pages_resize(t, p, slots, new_lens, n, result, (hipStream_t)stream));
+}
+
+da_status check_compact(const Table& t, const void* k_pages, const void* v_pages, int layers, int Hkv, int d,
+                        const int32_t* slots, const int32_t* start, const int32_t* keep, int64_t n_keep,
+                        const int32_t* cu_keep, int n, const int32_t* result) {
+  if (!t.refs || !slots || !start || !keep || !cu_keep || !result) return DA_ERR_NULL;
+  da_status st = check_table(t);
+  if (st != DA_OK) return st;
+  st = check_pages(k_pages, v_pages, layers, Hkv, d);
+  if (st != DA_OK) return st;
+  if (n < 1 || n > kMaxRequests || n_keep < 0 || Hkv > INT32_MAX / 2 / n / layers ||
+      !fits((int64_t)n * layers * 2 * Hkv, 256))
+    return DA_ERR_SHAPE;
+  if (!aligned(slots, 4) || !aligned(start, 4) || !aligned(keep, 4) || !aligned(cu_keep, 4) ||
+      !aligned(result, 16))
+    return DA_ERR_ALIGN;
+  return check_device();
+}
+
+da_status summarise_pages(const void* k_pages, const float* k_scales, int Hkv, int d, const Table& t,
+                          const int32_t* slots, const int32_t* first, int B, int max_new, void* codes, float* scales,
+                          void* stream) {
+  if (!k_pages || !codes || !scales) return DA_ERR_NULL;
+  da_status st = check_table(t);
+  if (st != DA_OK) return st;
+  if (B < 1 || Hkv < 1 || max_new < 1 || (!slots && B > t.S)) return DA_ERR_SHAPE;
+  if (d != 64 && d != 128) return DA_ERR_UNSUPPORTED;
+  if (!aligned(k_pages, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(slots, 4) || !aligned(first, 4))
+    return DA_ERR_ALIGN;
+  SummaryArgs a{};
+  // max_new tokens from anywhere in a page on end up to this many pages
+  int64_t nblk = pages_of(max_new) + (first ? 1 : 0);
+  if (nblk > t.M) nblk = t.M;
+  if ((int64_t)B * nblk > INT32_MAX || !fits((int64_t)B * nblk * Hkv / 4 + 1, 256)) return DA_ERR_SHAPE;
+  st = check_device();
+  if (st != DA_OK) return st;
+  a.k = k_pages;
+  a.k_scales = k_scales;
+  a.table = t.table;
+  a.lens = t.lens;
+  a.slots = slots;
+  a.first = first;
+  a.codes = (int8_t*)codes;
+  a.scales = scales;
+  a.B = B;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.S = t.S;
+  a.M = t.M;
+  a.P = t.P;
+  a.nblk = (int)nblk;
+  return launched(launch_summary(a, (hipStream_t)stream));
+}
+
+PagedArgs paged_args(const void* q, const void* k_pages, const void* v_pages, void* out, float* lse,
+                     const int32_t* table, const int32_t* lens, int S, int M, int P, const int32_t* slots,
+                     const int32_t* cu_seqlens, int B, int max_seqlen, int Hq, int Hkv, int d) {
+  PagedArgs a{};
+  a.q = (const uint16_t*)q;
+  a.k = k_pages;
+  a.v = v_pages;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  a.table = table;
+  a.lens = lens;
+  a.slots = slots;
+  a.cu = cu_seqlens;
+  a.B = B;
+  a.N = max_seqlen;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.S = S;
+  a.M = M;
+  a.P = P;
+  return a;
+}
+
+da_status attend_pages(PagedArgs a, int max_len, float cap, void* workspace, size_t workspace_bytes, void* stream) {
+  if (max_len < 1) return DA_ERR_SHAPE;
+  if (a.mask && (a.mask_words < 1 || (int64_t)a.mask_words * 64 < a.N)) return DA_ERR_PARAM;
+  a.max_len = max_len;
+  return paged_attn(a, 0, cap, workspace, workspace_bytes, stream);
+}
+
+da_status attend_lists(PagedArgs a, const int32_t* pages, int top_k, void* workspace, size_t workspace_bytes,
+                       void* stream) {
+  if (!pages) return DA_ERR_NULL;
+  if (top_k < 1) return DA_ERR_PARAM;
+  a.lists = pages;
+  a.n_list = top_k;
+  a.max_len = INT32_MAX;
+  return paged_attn(a, top_k, 0.f, workspace, workspace_bytes, stream);
+}
+
+size_t paged_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len, int n_list, bool eight) {
+  PagedPlan p;
+  if (check_rows(B, max_seqlen, Hq, Hkv, d) != DA_OK || max_len < 1 || n_list < 0) return 0;
+  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, eight, &p) != DA_OK) return 0;
+  return p.bytes;
+}
+
 }  // namespace da
 
 using namespace da;
@@ -175,19 +298,8 @@ da_status da_pages_fork(int32_t* table, int32_t* lens, int32_t* refs, int S, int
 da_status da_pages_resize(void* k_pages, void* v_pages, int layers, int Hkv, int d, int32_t* table,
                           int32_t* lens, int32_t* refs, int S, int M, int P, const int32_t* slots,
                           const int32_t* new_lens, int n, int32_t* result, void* stream) {
-  const Table t{table, lens, refs, S, M, P};
-  if (!refs || !slots || !result) return DA_ERR_NULL;
-  da_status st = check_table(t);
-  if (st != DA_OK) return st;
-  st = check_pages(k_pages, v_pages, layers, Hkv, d);
-  if (st != DA_OK) return st;
-  if (n < 1 || n > kMaxRequests || Hkv > INT32_MAX / 2 / n / layers || !fits((int64_t)n * layers * 2 * Hkv, 256))
-    return DA_ERR_SHAPE;
-  if (!aligned(slots, 4) || !aligned(new_lens, 4) || !aligned(result, 16)) return DA_ERR_ALIGN;
-  st = check_device();
-  if (st != DA_OK) return st;
   const Pages p{(uint16_t*)k_pages, (uint16_t*)v_pages, layers, Hkv, d};
-  return launched(launch_pages_resize(t, p, slots, new_lens, n, result, (hipStream_t)stream));
+  return resize_pages(p, d, {table, lens, refs, S, M, P}, slots, new_lens, n, result, stream);
 }
 
 da_status da_pages_append(const void* k, const void* v, int64_t T, void* k_pages, void* v_pages,
@@ -227,55 +339,18 @@ da_status da_pages_compact(void* k_pages, void* v_pages, int layers, int Hkv, in
                            const int32_t* start, const int32_t* keep, int64_t n_keep,
                            const int32_t* cu_keep, int n, int32_t* result, void* stream) {
   const Table t{table, lens, refs, S, M, P};
-  if (!refs || !slots || !start || !keep || !cu_keep || !result) return DA_ERR_NULL;
-  da_status st = check_table(t);
-  if (st != DA_OK) return st;
-  st = check_pages(k_pages, v_pages, layers, Hkv, d);
-  if (st != DA_OK) return st;
-  if (n < 1 || n > kMaxRequests || n_keep < 0 || Hkv > INT32_MAX / 2 / n / layers ||
-      !fits((int64_t)n * layers * 2 * Hkv, 256))
-    return DA_ERR_SHAPE;
-  if (!aligned(slots, 4) || !aligned(start, 4) || !aligned(keep, 4) || !aligned(cu_keep, 4) ||
-      !aligned(result, 16))
-    return DA_ERR_ALIGN;
-  st = check_device();
-  if (st != DA_OK) return st;
   const Pages p{(uint16_t*)k_pages, (uint16_t*)v_pages, layers, Hkv, d};
+  const da_status st = check_compact(t, k_pages, v_pages, layers, Hkv, d, slots, start, keep, n_keep, cu_keep, n, result);
+  if (st != DA_OK) return st;
   return launched(launch_pages_compact(t, p, slots, start, keep, n_keep, cu_keep, n, result, (hipStream_t)stream));
 }
 
 da_status da_page_summary(const void* k_pages, int Hkv, int d, const int32_t* table, const int32_t* lens,
                           int S, int M, int P, const int32_t* slots, const int32_t* first, int B,
                           int max_new, void* codes, float* scales, void* stream) {
-  if (!k_pages || !codes || !scales) return DA_ERR_NULL;
-  da_status st = check_table({const_cast<int32_t*>(table), const_cast<int32_t*>(lens), nullptr, S, M, P});
-  if (st != DA_OK) return st;
-  if (B < 1 || Hkv < 1 || max_new < 1 || (!slots && B > S)) return DA_ERR_SHAPE;
-  if (d != 64 && d != 128) return DA_ERR_UNSUPPORTED;
-  if (!aligned(k_pages, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(slots, 4) || !aligned(first, 4))
-    return DA_ERR_ALIGN;
-  SummaryArgs a{};
-  // max_new tokens from anywhere in a page on end up to this many pages
-  int64_t nblk = pages_of(max_new) + (first ? 1 : 0);
-  if (nblk > M) nblk = M;
-  if ((int64_t)B * nblk > INT32_MAX || !fits((int64_t)B * nblk * Hkv / 4 + 1, 256)) return DA_ERR_SHAPE;
-  st = check_device();
-  if (st != DA_OK) return st;
-  a.k = (const uint16_t*)k_pages;
-  a.table = table;
-  a.lens = lens;
-  a.slots = slots;
-  a.first = first;
-  a.codes = (int8_t*)codes;
-  a.scales = scales;
-  a.B = B;
-  a.Hkv = Hkv;
-  a.d = d;
-  a.S = S;
-  a.M = M;
-  a.P = P;
-  a.nblk = (int)nblk;
-  return launched(launch_summary(a, (hipStream_t)stream));
+  return summarise_pages(k_pages, nullptr, Hkv, d,
+                         {const_cast<int32_t*>(table), const_cast<int32_t*>(lens), nullptr, S, M, P}, slots, first, B,
+                         max_new, codes, scales, stream);
 }
 
 da_status da_key_summary(const void* k, const int32_t* cu_seqlens, int B, int max_seqlen, int Hkv, int d,
@@ -291,7 +366,7 @@ da_status da_key_summary(const void* k, const int32_t* cu_seqlens, int B, int ma
   if (st != DA_OK) return st;
   if (nblk == 0) return DA_OK;  // no whole block
   SummaryArgs a{};
-  a.k = (const uint16_t*)k;
+  a.k = k;
   a.cu = cu_seqlens;
   a.codes = (int8_t*)codes;
   a.scales = scales;
@@ -418,10 +493,7 @@ da_status da_select_pages(const void* q, const void* codes, const float* scales,
 }
 
 size_t da_paged_workspace_bytes(int B, int max_seqlen, int Hq, int Hkv, int d, int max_len, int n_list) {
-  PagedPlan p;
-  if (check_rows(B, max_seqlen, Hq, Hkv, d) != DA_OK || max_len < 1 || n_list < 0) return 0;
-  if (paged_plan(B, max_seqlen, Hq, Hkv, d, pages_of(max_len), n_list, &p) != DA_OK) return 0;
-  return p.bytes;
+  return paged_bytes(B, max_seqlen, Hq, Hkv, d, max_len, n_list, false);
 }
 
 da_status tree_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out, float* lse,
@@ -429,30 +501,11 @@ da_status tree_attn_paged(const void* q, const void* k_pages, const void* v_page
                           const int32_t* slots, const int32_t* cu_seqlens, int B, int max_seqlen,
                           int max_len, int Hq, int Hkv, int d, const uint64_t* mask, int mask_words,
                           void* workspace, size_t workspace_bytes, void* stream) {
-  if (max_len < 1) return DA_ERR_SHAPE;
-  if (mask && (mask_words < 1 || (int64_t)mask_words * 64 < max_seqlen)) return DA_ERR_PARAM;
-  PagedArgs a{};
-  a.q = (const uint16_t*)q;
-  a.k = (const uint16_t*)k_pages;
-  a.v = (const uint16_t*)v_pages;
-  a.out = (uint16_t*)out;
-  a.lse = lse;
-  a.table = table;
-  a.lens = lens;
-  a.slots = slots;
-  a.cu = cu_seqlens;
+  PagedArgs a = paged_args(q, k_pages, v_pages, out, lse, table, lens, S, M, P, slots, cu_seqlens, B, max_seqlen, Hq,
+                           Hkv, d);
   a.mask = mask;
   a.mask_words = mask_words;
-  a.B = B;
-  a.N = max_seqlen;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.d = d;
-  a.S = S;
-  a.M = M;
-  a.P = P;
-  a.max_len = max_len;
-  return paged_attn(a, 0, workspace, workspace_bytes, stream);
+  return attend_pages(a, max_len, 0.f, workspace, workspace_bytes, stream);
 }
 
 da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_pages, void* out, float* lse,
@@ -460,30 +513,9 @@ da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_
                               const int32_t* slots, const int32_t* cu_seqlens, int B, int max_seqlen,
                               int Hq, int Hkv, int d, const int32_t* pages, int top_k, void* workspace,
                               size_t workspace_bytes, void* stream) {
-  if (!pages) return DA_ERR_NULL;
-  if (top_k < 1) return DA_ERR_PARAM;
-  PagedArgs a{};
-  a.q = (const uint16_t*)q;
-  a.k = (const uint16_t*)k_pages;
-  a.v = (const uint16_t*)v_pages;
-  a.out = (uint16_t*)out;
-  a.lse = lse;
-  a.table = table;
-  a.lens = lens;
-  a.slots = slots;
-  a.cu = cu_seqlens;
-  a.lists = pages;
-  a.n_list = top_k;
-  a.B = B;
-  a.N = max_seqlen;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.d = d;
-  a.S = S;
-  a.M = M;
-  a.P = P;
-  a.max_len = INT32_MAX;
-  return paged_attn(a, top_k, workspace, workspace_bytes, stream);
+  return attend_lists(paged_args(q, k_pages, v_pages, out, lse, table, lens, S, M, P, slots, cu_seqlens, B, max_seqlen,
+                                 Hq, Hkv, d),
+                      pages, top_k, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -38,22 +38,25 @@ namespace {
 
 constexpr int kIdPages = 1024;  // page ids that a workgroup holds in LDS at a time
 
-// RT tiles of 32 rows and KS key streams per workgroup of NW waves.
-template <int D, int RT>
+// RT tiles of 32 rows and KS key streams per workgroup of NW waves.  E8: the pages hold e4m3
+// codes.
+template <int D, int RT, bool E8>
 struct Shape {
   static constexpr int NW = RT > 4 ? RT : 4;
   static constexpr int KS = NW / RT;
-  // Keys per unit: half a page where four streams share LDS, else a whole page.
-  static constexpr int UNIT = KS == 4 ? 32 : 64;
+  // Keys per unit: half a page where four streams of bf16 share LDS, else a whole page.
+  static constexpr int UNIT = KS == 4 && !E8 ? 32 : 64;
+  static constexpr int RB = E8 ? D : 2 * D;  // bytes of a row
   static constexpr int UPP = kPage / UNIT;  // units per page
   static constexpr int NB = UNIT / 32;      // 32-key blocks of scores
-  static constexpr int unitElems = 2 * UNIT * D;  // keys, then values
+  static constexpr int unitElems = UNIT * RB;  // of 16 bits: keys, then values
   // ring of each stream: 128 KB together at d = 128 where several stream, 64 KB for one
   static constexpr int DEPTH = 2;
   static constexpr int ringElems = KS * DEPTH * unitElems;
-  static constexpr int regions = UNIT * D * 2 / 1024;  // 1 KB DMA regions per tile
-  static constexpr int RPW = regions / RT;             // of a wave
-  static constexpr int ldsBytes = ringElems * 2 + kIdPages * 4 + 256;
+  static constexpr int regions = UNIT * RB / 1024;  // 1 KB DMA regions per tile
+  static constexpr int RPW = regions / RT;          // of a wave
+  // (behind the ring: page ids, the pages' scales, a few sums)
+  static constexpr int ldsBytes = ringElems * 2 + kIdPages * (E8 ? 8 : 4) + 256;
   // Weights as two bf16 parts, the nearest value and what it leaves (2^-16 of a weight is lost
   // instead of 2^-8): the root mean square error of the outputs is that of their own rounding.
   // One row tile has matrix cores to spare behind HBM: 64 single tokens over 8192 keys 239.8 -> 241.1
@@ -64,11 +67,40 @@ struct Shape {
   static constexpr bool TWO_PARTS = RT == 1;
   // waves per SIMD that LDS has room for
   static constexpr int WAVES = ldsBytes > 81920 ? 1 : 2;
-  __device__ static constexpr int kswz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
+  // Rows of codes: the 16 rows of a lane group that reads one chunk of each, keys in order and
+  // values four by four, cover all banks.
+  __device__ static constexpr int kswz(int r) {
+    if (E8) return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+    return D == 128 ? (r & 15) : ((r >> 1) & 7);
+  }
   __device__ static constexpr int vswz(int r) {
+    if (E8) return kswz(r);
     return D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2);
   }
 };
+
+// Eight e4m3 codes times a power of two, exact in bf16.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x8 values_of(uint32_t lo, uint32_t hi, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const auto b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const auto c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const auto d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+#else
+  return bf16x8{};
+#endif
+}
+// ds_read_b64_tr_b8: inside each group of 16 lanes, lane i receives byte i of the eight 16-byte
+// rows, row k read by lanes 2k and 2k + 1.
+__device__ __forceinline__ i32x2 lds_read_tr8(const uint8_t* p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(p));
+#else
+  return i32x2{};
+#endif
+}
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -102,14 +134,17 @@ __device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
   return a.whole ? x.segs : x.segs * x.np;
 }
 
-template <int D, int RT, bool LISTS>
-__global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) void paged_attn_kernel(PagedArgs a) {
-  using SH = Shape<D, RT>;
+// SC: scores are capped or biased by distance (see delta_attn.h).
+template <int D, int RT, bool LISTS, bool E8, bool SC>
+__global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAVES)) void paged_attn_kernel(PagedArgs a) {
+  using SH = Shape<D, RT, E8>;
+  static_assert(!(LISTS && SC), "lists have plain scores");
   constexpr int NW = SH::NW, KS = SH::KS, DEPTH = SH::DEPTH, RPW = SH::RPW, MB = D / 32;
   constexpr int UNIT = SH::UNIT, UPP = SH::UPP, NB = SH::NB;
   constexpr int kThreads = 64 * NW;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
   int* const ids = (int*)(smem + SH::ringElems);
+  int* const exps = ids + kIdPages;  // (of codes) exponents of the pages' scales: keys' | values' << 8
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -188,7 +223,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     b = __builtin_ctzll(__ballot(before <= x0 && x0 < upto));
     off = (int)x0 - __builtin_amdgcn_readlane(before, b);
   } else {
-    int* const red = ids + kIdPages;  // [NW] sums, then what is found
+    int* const red = ids + kIdPages * (E8 ? 2 : 1);  // [NW] sums, then what is found
     auto block_scan = [&](int x, int* total) {
       x = wave_scan_add(x);
       __syncthreads();
@@ -275,12 +310,15 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   const int64_t t = base + i_tok;
   const int h = g * G + (LISTS ? rc : rc - i_tok * G);
   const int pos = first + i_tok;
+  // (of codes a lane reads 16 dims at a time, for two products in a row: the queries likewise)
   bf16x8 qf[D / 16];
   {
-    const uint16_t* qp = a.q + (t * a.Hq + h) * (int64_t)D + half * 8;
+    const uint16_t* qp = a.q + (t * a.Hq + h) * (int64_t)D + half * (E8 ? 16 : 8);
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + kk * 16);
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + (E8 ? kk / 2 * 32 + kk % 2 * 8 : kk * 16));
   }
+  const bool biased = SC && a.slopes;
+  const float slope = biased ? a.slopes[h] * 1.4426950408889634f : 0.f;
 
   // ---- state of the rows
   f32x16 o[MB];
@@ -289,7 +327,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   // Online softmax against a lagging reference, as in the prefill kernels: `ref` in
   // base-2 units of the logits, -ref / c in every register of nref, from which the score
   // accumulators start, so that c times them is logit - ref.
-  const float c2 = a.scale_log2, inv_c2 = 1.f / a.scale_log2;
+  // (Changed scores are in base-2 units, with ref subtracted, as they come.)
+  const float c2 = SC ? 1.f : a.scale_log2, inv_c2 = SC ? 1.f : 1.f / a.scale_log2;
   float ref = 0.f, l = 0.f;
   bool has_ref = false;
   f32x16 nref = f32x16{};
@@ -308,7 +347,14 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       if (at < 0 || at > own || (at == own && q0 + j < a.n_list)) at = -1;
     }
     const int e = at >= 0 ? a.table[(int64_t)sq.s * a.M + at] : -1;
-    ids[j] = (unsigned)e < (unsigned)a.P ? e : -1;  // (-1: no such page, its keys are not seen)
+    const bool there = (unsigned)e < (unsigned)a.P;
+    ids[j] = there ? e : -1;  // (-1: no such page, its keys are not seen)
+    if constexpr (E8) {
+      if (there) {
+        const int64_t i = (int64_t)e * a.Hkv + g;
+        exps[j] = (int)(__float_as_uint(a.k_scales[i]) >> 23 & 255u) | (int)(__float_as_uint(a.v_scales[i]) >> 23 & 255u) << 8;
+      }
+    }
   }
   // the queries have landed: the loop's products must not wait for them behind the
   // transfers issued there
@@ -324,22 +370,31 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   const int n_it = (n_units + KS - 1) / KS;
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)smem;
   const uint32_t ring = smem_lds + (uint32_t)(ks * DEPTH * SH::unitElems) * 2;
-  const uint64_t page_bytes = (uint64_t)a.Hkv * kPage * D * 2;
-  const uint64_t head_off = (uint64_t)g * kPage * D * 2;
+  const uint64_t page_bytes = (uint64_t)a.Hkv * kPage * SH::RB;
+  const uint64_t head_off = (uint64_t)g * kPage * SH::RB;
   const uint64_t k0_addr = (uint64_t)a.k + head_off, v0_addr = (uint64_t)a.v + head_off;
   int dma_row[RPW], dma_kc[RPW], dma_vc[RPW];
 #pragma unroll
   for (int i = 0; i < RPW; ++i) {
     const int byte = (rt * RPW + i) * 1024 + 16 * lane;
-    dma_row[i] = byte / (2 * D);
-    const int pc = (byte % (2 * D)) / 16;
+    dma_row[i] = byte / SH::RB;
+    const int pc = (byte % SH::RB) / 16;
     dma_kc[i] = (pc ^ SH::kswz(dma_row[i])) * 16;
     dma_vc[i] = (pc ^ SH::vswz(dma_row[i])) * 16;
   }
-  auto page_of = [&](int it) -> int {  // -1: nothing to read (a vector register until dma)
+  // (biased scores fall with the distance: the nearest keys first, so that the reference of the
+  // softmax, which only moves up, stays where they put it)
+  auto unit_of = [&](int it) -> int {
     const int u = it * KS + ks;
-    const int e = ids[min(u, n_units - 1) / UPP];
-    return u < n_units ? e : -1;
+    return SC && biased ? n_units - 1 - u : u;
+  };
+  auto place_of = [&](int it) -> int {
+    const int u = unit_of(it);
+    return min(SC ? max(u, 0) : u, n_units - 1) / UPP;
+  };
+  auto page_of = [&](int it) -> int {  // -1: nothing to read (a vector register until dma)
+    const int e = ids[place_of(it)];
+    return it * KS + ks < n_units ? e : -1;
   };
   // Every call issues 2 * RPW transfers, so that waits can count them; a unit
   // without keys reads page 0.  Rows past the last key read that key: what lies
@@ -347,20 +402,20 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   // NaN.
   auto dma = [&](int it, int stage, int page) -> int {
     const int e = __builtin_amdgcn_readfirstlane(page);
-    const int u = it * KS + ks;
+    const int u = SC ? max(unit_of(it), 0) : unit_of(it);
     const int keys = e < 0 ? 1 : u == n_units - 1 ? tail_keys : UNIT;
-    const uint64_t off = (uint64_t)max(e, 0) * page_bytes + (uint64_t)(u % UPP * UNIT * D * 2);
+    const uint64_t off = (uint64_t)max(e, 0) * page_bytes + (uint64_t)(u % UPP * UNIT * SH::RB);
     const uint64_t ka = k0_addr + off, va = v0_addr + off;
-    i32x4 kr = {(int)(uint32_t)ka, (int)((uint32_t)(ka >> 32) & 0xffffu), UNIT * D * 2, 0x00020000};
-    i32x4 vr = {(int)(uint32_t)va, (int)((uint32_t)(va >> 32) & 0xffffu), UNIT * D * 2, 0x00020000};
+    i32x4 kr = {(int)(uint32_t)ka, (int)((uint32_t)(ka >> 32) & 0xffffu), UNIT * SH::RB, 0x00020000};
+    i32x4 vr = {(int)(uint32_t)va, (int)((uint32_t)(va >> 32) & 0xffffu), UNIT * SH::RB, 0x00020000};
     uint32_t dst = ring + (uint32_t)(stage * SH::unitElems) * 2;
     settle_sgprs(kr, vr, dst);
 #pragma unroll
     for (int i = 0; i < RPW; ++i) {
       const uint32_t region = (uint32_t)((rt * RPW + i) * 1024);
-      const int row = min(dma_row[i], keys - 1) * (2 * D);
+      const int row = min(dma_row[i], keys - 1) * SH::RB;
       dma16(kr, dst + region, row + dma_kc[i]);
-      dma16(vr, dst + UNIT * D * 2 + region, row + dma_vc[i]);
+      dma16(vr, dst + UNIT * SH::RB + region, row + dma_vc[i]);
     }
     return e;
   };
@@ -368,15 +423,24 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   // ---- LDS offsets of the operands (elements inside the stream's ring; the stage is a
   // constant of the loop's unrolled halves)
   const int ring0 = ks * DEPTH * SH::unitElems;
-  int kread[D / 16];
+  constexpr int KF = E8 ? D / 32 : D / 16;  // reads of a key's row, 16 bytes each
+  int kread[KF];
 #pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) kread[kk] = ring0 + col * D + (((2 * kk + half) ^ SH::kswz(col)) * 8);
+  for (int kk = 0; kk < KF; ++kk) kread[kk] = ring0 + col * (SH::RB / 2) + (((2 * kk + half) ^ SH::kswz(col)) * 8);
   const int tr_g1 = (lane >> 4) & 1, tr_k = (lane >> 2) & 3, tr_m = lane & 3;
-  const int vsw = SH::vswz(4 * half + tr_k);
-  int vread[MB];
+  int vread[MB];  // (of codes: in bytes)
+  if constexpr (E8) {
+    // the eight keys of a lane's half, in the order of the weights: 4 half + (0 .. 3), then 8 on
+    const int key = 4 * half + (lane >> 1 & 3) + (lane >> 3 & 1) * 8;
 #pragma unroll
-  for (int mb = 0; mb < MB; ++mb)
-    vread[mb] = ring0 + (4 * half + tr_k) * D + (((4 * mb + 2 * tr_g1 + (tr_m >> 1)) ^ vsw) * 8) + (tr_m & 1) * 4;
+    for (int mb = 0; mb < MB; ++mb)
+      vread[mb] = ring0 * 2 + key * D + ((2 * mb + tr_g1) ^ SH::vswz(key)) * 16 + (lane & 1) * 8;
+  } else {
+    const int vsw = SH::vswz(4 * half + tr_k);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+      vread[mb] = ring0 + (4 * half + tr_k) * D + (((4 * mb + 2 * tr_g1 + (tr_m >> 1)) ^ vsw) * 8) + (tr_m & 1) * 4;
+  }
 
   // Which of 32 keys from position k0 on this lane's row sees, bit by bit.
   auto visible = [&](int k0) -> uint32_t {
@@ -396,30 +460,75 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     return (uint32_t)(sh ? (lo >> sh) | (hi << (64 - sh)) : lo);
   };
 
-  auto compute = [&](int it, auto stage) {
-    const int u = it * KS + ks;
+  auto compute = [&](int it, auto stage, int scales) {
+    const int u = unit_of(it);
     const uint16_t* ku = smem + decltype(stage)::value * SH::unitElems;
-    const uint16_t* vu = ku + UNIT * D;
+    const uint16_t* vu = ku + UNIT * SH::RB / 2;
+    const uint32_t se = E8 ? (uint32_t)__builtin_amdgcn_readfirstlane(scales) : 0u;
+    const float k_scale = __uint_as_float((se & 255u) << 23), v_scale = __uint_as_float((se >> 8) << 23);
     f32x16 sc[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sc[nb] = nref;
+    for (int nb = 0; nb < NB; ++nb) sc[nb] = SC ? f32x16{} : nref;
     // K reads kAhead MFMAs ahead of their use, an order that the scheduling barriers hold
     // (left to itself the compiler pairs each MFMA with its own read and a wait)
-    constexpr int kAhead = 4, kProducts = NB * D / 16;
-    auto kfrag = [&](int i) { return *(const bf16x8*)(ku + kread[i / NB] + (i % NB) * 32 * D); };
-    bf16x8 kf[kAhead];
+    constexpr int kAhead = 4;
+    if constexpr (E8) {
+      constexpr int kReads = NB * KF;
+      auto kcodes = [&](int i) { return *(const u32x4*)(ku + kread[i / NB] + (i % NB) * 32 * (SH::RB / 2)); };
+      u32x4 kc[kReads < kAhead ? kReads : kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) kf[i] = kfrag(i);
+      for (int i = 0; i < kAhead && i < kReads; ++i) kc[i] = kcodes(i);
 #pragma unroll
-    for (int i = 0; i < kProducts; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      sc[i % NB] = mfma32(kf[i % kAhead], qf[i / NB], sc[i % NB]);
-      if (i + kAhead < kProducts) kf[i % kAhead] = kfrag(i + kAhead);
+      for (int i = 0; i < kReads; i += NB) {
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 kf[2 * NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const u32x4 x = kc[(i + nb) % kAhead];
+          kf[nb] = values_of(x[0], x[1], k_scale);
+          kf[NB + nb] = values_of(x[2], x[3], k_scale);
+          if (i + nb + kAhead < kReads) kc[(i + nb) % kAhead] = kcodes(i + nb + kAhead);
+        }
+#pragma unroll
+        for (int z = 0; z < 2 * NB; ++z) sc[z % NB] = mfma32(kf[z], qf[2 * (i / NB) + z / NB], sc[z % NB]);
+      }
+    } else {
+      constexpr int kProducts = NB * D / 16;
+      auto kfrag = [&](int i) { return *(const bf16x8*)(ku + kread[i / NB] + (i % NB) * 32 * D); };
+      bf16x8 kf[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) kf[i] = kfrag(i);
+#pragma unroll
+      for (int i = 0; i < kProducts; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        sc[i % NB] = mfma32(kf[i % kAhead], qf[i / NB], sc[i % NB]);
+        if (i + kAhead < kProducts) kf[i % kAhead] = kfrag(i + kAhead);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
-    // mask the units that some row does not see whole
     const int at = q0 + u / UPP;
     const int k0 = (LISTS ? own : at) * kPage + u % UPP * UNIT;
+    if constexpr (SC) {
+      // In base-2 units: cap tanh(q.k / (cap sqrt d)) - slope (i - j) - ref, tanh as in the prefill
+      // kernels.  (Biased rows see no key past their own.)
+      const float dist0 = (float)(k0 + 4 * half - pos);  // j - i of offset 0
+      const float base = (biased ? slope * dist0 : 0.f) - ref;
+      auto each = [&](auto f) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) sc[nb][q] = f(sc[nb][q], (float)(32 * nb + 8 * (q >> 2) + (q & 3)));
+      };
+      if (a.cap2 > 0.f) {
+        const float c = a.cap_in, m = -2.f * a.cap2, top = a.cap2 + base;
+        each([&](float x, float) { return __builtin_fmaf(m, __builtin_amdgcn_rcpf(1.f + fast_exp2(c * x)), top); });
+      } else {
+        const float c = a.scale_log2;
+        each([&](float x, float) { return __builtin_fmaf(c, x, base); });
+      }
+      if (biased) each([&](float x, float o) { return __builtin_fmaf(slope, o, x); });
+    }
+    // mask the units that some row does not see whole
     if (LISTS ? at >= a.n_list : k0 + UNIT > first) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -487,7 +596,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       // reference moves only up
       const bool seen = mx != -INFINITY;
       if (__any(has_ref ? mx > 8.f : seen)) {
-        const float dm = has_ref ? fmaxf(mx, 0.f) : (seen ? mx : 0.f);
+        float dm = has_ref ? fmaxf(mx, 0.f) : (seen ? mx : 0.f);
+        if constexpr (SC) dm = (ref + dm) - ref;  // (a bias may be large: what the sum rounds off counts)
         const float alpha = has_ref ? fast_exp2(-dm) : 0.f;  // l and O are still zero without one
         ref += dm;
         has_ref = has_ref || seen;
@@ -507,19 +617,34 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
     l += tsum;
     // V^T reads (two per MFMA) likewise
     constexpr int kSums = 2 * NB * MB;
-    auto vfrag = [&](int i) {
-      const uint16_t* p = vu + vread[i % MB] + (16 * (i / MB)) * D;
-      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(p), lds_read_tr(p + 8 * D), 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    bf16x8 vf[kAhead];
+    if constexpr (E8) {
+      auto vcodes = [&](int i) { return lds_read_tr8((const uint8_t*)vu + vread[i % MB] + (16 * (i / MB)) * D); };
+      i32x2 vc[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) vf[i] = vfrag(i);
+      for (int i = 0; i < kAhead; ++i) vc[i] = vcodes(i);
 #pragma unroll
-    for (int i = 0; i < kSums; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      o[i % MB] = mfma32(vf[i % kAhead], pf[i / MB], o[i % MB]);
-      if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf[i % kAhead], rest[i / MB], o[i % MB]);
-      if (i + kAhead < kSums) vf[i % kAhead] = vfrag(i + kAhead);
+      for (int i = 0; i < kSums; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        const bf16x8 vf = values_of((uint32_t)vc[i % kAhead][0], (uint32_t)vc[i % kAhead][1], v_scale);
+        o[i % MB] = mfma32(vf, pf[i / MB], o[i % MB]);
+        if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf, rest[i / MB], o[i % MB]);
+        if (i + kAhead < kSums) vc[i % kAhead] = vcodes(i + kAhead);
+      }
+    } else {
+      auto vfrag = [&](int i) {
+        const uint16_t* p = vu + vread[i % MB] + (16 * (i / MB)) * D;
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(p), lds_read_tr(p + 8 * D), 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      bf16x8 vf[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) vf[i] = vfrag(i);
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        o[i % MB] = mfma32(vf[i % kAhead], pf[i / MB], o[i % MB]);
+        if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf[i % kAhead], rest[i / MB], o[i % MB]);
+        if (i + kAhead < kSums) vf[i % kAhead] = vfrag(i + kAhead);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -529,7 +654,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
   // with one barrier per unit, which also says that the unit before it is read.  Page
   // ids are read one unit ahead of the transfers that need them.
   static_assert(DEPTH == 2, "the loop is unrolled by stage");
-  int now = dma(0, 0, page_of(0)), next = page_of(1);
+  auto scales_of = [&](int it) -> int { return E8 ? exps[place_of(it)] : 0; };
+  int now = dma(0, 0, page_of(0)), next = page_of(1), scales = scales_of(0);
   auto step = [&](int it, auto stage) {
     constexpr int kOther = 1 - decltype(stage)::value;
     int after;
@@ -545,8 +671,10 @@ __global__ __launch_bounds__((64 * Shape<D, RT>::NW), (Shape<D, RT>::WAVES)) voi
       after = dma(it + 1, kOther, next);
     }
     next = page_of(it + 2);
-    if (now >= 0) compute(it, stage);
+    const int scales_next = scales_of(it + 1);
+    if (now >= 0) compute(it, stage, scales);
     now = after;
+    scales = scales_next;
   };
   for (int it = 0; it < n_it; it += 2) {
     step(it, std::integral_constant<int, 0>{});
@@ -728,24 +856,31 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a)
 
 }  // namespace
 
-hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
+namespace {
+
+template <bool E8, bool SC>
+hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.n_wgs);
 #define DA_PAGED(DD, RT, LS)                                                                       \
-  hipLaunchKernelGGL((paged_attn_kernel<DD, RT, LS>), grid, dim3(64 * Shape<DD, RT>::NW),          \
-                     (Shape<DD, RT>::ldsBytes), s, a)
+  hipLaunchKernelGGL((paged_attn_kernel<DD, RT, LS, E8, SC>), grid, dim3(64 * Shape<DD, RT, E8>::NW), \
+                     (Shape<DD, RT, E8>::ldsBytes), s, a)
 #define DA_PAGED_RT(DD, LS)                                                                        \
   switch (a.row_tiles) {                                                                           \
     case 1: DA_PAGED(DD, 1, LS); break;                                                            \
     case 2: DA_PAGED(DD, 2, LS); break;                                                            \
     default: DA_PAGED(DD, 4, LS); break;                                                           \
   }
-  if (a.lists) {
-    if (a.d == 128) {
-      DA_PAGED_RT(128, true)
-    } else {
-      DA_PAGED_RT(64, true)
+  if constexpr (!SC) {
+    if (a.lists) {
+      if (a.d == 128) {
+        DA_PAGED_RT(128, true)
+      } else {
+        DA_PAGED_RT(64, true)
+      }
+      return hipGetLastError();
     }
-  } else if (a.d == 128) {
+  }
+  if (a.d == 128) {
     if (a.row_tiles == 8)
       DA_PAGED(128, 8, false);
     else
@@ -755,6 +890,18 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   }
 #undef DA_PAGED_RT
 #undef DA_PAGED
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
+  hipError_t e;
+  if (a.k_scales)
+    e = a.scored ? launch_paged_as<true, true>(a, s) : launch_paged_as<true, false>(a, s);
+  else
+    e = a.scored ? launch_paged_as<false, true>(a, s) : launch_paged_as<false, false>(a, s);
+  if (e != hipSuccess) return e;
   if (!a.units) return hipGetLastError();  // no rows are cut
   const int64_t rows = (int64_t)a.B * a.N * a.Hq;
   const bool many = rows >= kManyRows;

@@ -48,7 +48,8 @@ __device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
 // 8.1 us, 87302 (179 MB) in 50 us, 3.6 TB/s, right after the pages were written; with sums
 // in 32 bits the same: not the arithmetic bounds it, but that a wave ends with its block and
 // reads nothing while it reduces.
-template <int D>
+// Of codes the sums are of the codes themselves, whose scale enters once at the end.
+template <int D, bool E8>
 __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kSteps = kPage / kRows;
   const int lane = threadIdx.x & 63;
@@ -59,8 +60,7 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
   int j = (int)(x - (uint32_t)b * (uint32_t)a.nblk);
   if (b >= a.B) return;
   int64_t block;  // where the summary goes
-  const uint16_t* k;
-  int64_t stride;
+  int64_t at, stride;  // first value of the block, and values from a key to the next
   if (a.table) {
     const int s = a.slots ? a.slots[b] : b;
     if ((unsigned)s >= (unsigned)a.S) return;
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
     const int e = a.table[(int64_t)s * a.M + j];
     if ((unsigned)e >= (unsigned)a.P) return;
     block = e;
-    k = a.k + ((int64_t)e * a.Hkv + h) * kPage * D;
+    at = ((int64_t)e * a.Hkv + h) * kPage * D;
     stride = D;
   } else {
     const int64_t base = a.cu ? a.cu[b] : (int64_t)b * a.N;
@@ -79,20 +79,39 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
     if ((j + 1) * (int64_t)kPage > L) return;
     block = base / kPage + b + j;
     stride = (int64_t)a.Hkv * D;
-    k = a.k + (base + (int64_t)j * kPage) * stride + h * D;
+    at = (base + (int64_t)j * kPage) * stride + h * D;
   }
   const int c = lane % kLanes, r = lane / kLanes;
-  u32x4 w[kSteps];
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) w[i] = *(const u32x4*)(k + (i * kRows + r) * stride + c * 8);
   double sum[8] = {};
+  if constexpr (E8) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint8_t* const k = (const uint8_t*)a.k + at;
+    u32x2 w[kSteps];
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i) w[i] = *(const u32x2*)(k + (i * kRows + r) * stride + c * 8);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      sum[2 * q] += (double)bf16_float(w[i][q] & 0xffffu);
-      sum[2 * q + 1] += (double)__uint_as_float(w[i][q] & 0xffff0000u);
-    }
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i][q], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i][q], true);
+        sum[4 * q] += (double)lo[0];
+        sum[4 * q + 1] += (double)lo[1];
+        sum[4 * q + 2] += (double)hi[0];
+        sum[4 * q + 3] += (double)hi[1];
+      }
+  } else {
+    const uint16_t* const k = (const uint16_t*)a.k + at;
+    u32x4 w[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) w[i] = *(const u32x4*)(k + (i * kRows + r) * stride + c * 8);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        sum[2 * q] += (double)bf16_float(w[i][q] & 0xffffu);
+        sum[2 * q + 1] += (double)__uint_as_float(w[i][q] & 0xffff0000u);
+      }
+  }
   // Lanes a power of two apart exchange the halves that the other keeps: those with the
   // bit set keep the upper one.
   int q0 = 0;
@@ -119,7 +138,10 @@ __global__ __launch_bounds__(256) void summary_kernel(SummaryArgs a) {
     *(uint16_t*)out = (uint16_t)(code(sum[0]) | code(sum[1]) << 8);
   else
     *out = (uint8_t)code(sum[0]);
-  if (lane == 0) a.scales[block * a.Hkv + h] = (float)(top / (127. * kPage));
+  if (lane == 0) {
+    if (E8) top *= (double)a.k_scales[block * a.Hkv + h];
+    a.scales[block * a.Hkv + h] = (float)(top / (127. * kPage));
+  }
 }
 
 // ------------------------------------------------------------------- top_k
@@ -867,10 +889,16 @@ __global__ __launch_bounds__(NT) void pick_pages_kernel(SelectArgs a) {
 hipError_t launch_summary(const SummaryArgs& a, hipStream_t s) {
   const int64_t items = (int64_t)a.B * a.nblk * a.Hkv;
   const dim3 grid((unsigned)((items + 3) / 4));
+#define DA_SUMMARY(D)                                                                  \
+  do {                                                                                 \
+    if (a.k_scales) hipLaunchKernelGGL((summary_kernel<D, true>), grid, dim3(256), 0, s, a); \
+    else hipLaunchKernelGGL((summary_kernel<D, false>), grid, dim3(256), 0, s, a);     \
+  } while (0)
   if (a.d == 128)
-    hipLaunchKernelGGL(summary_kernel<128>, grid, dim3(256), 0, s, a);
+    DA_SUMMARY(128);
   else
-    hipLaunchKernelGGL(summary_kernel<64>, grid, dim3(256), 0, s, a);
+    DA_SUMMARY(64);
+#undef DA_SUMMARY
   return hipGetLastError();
 }
 
