@@ -598,18 +598,12 @@ def _halves(name, t, dev):
         _on_device(name, t, dev, torch.bfloat16)
 
 
-def _codes8(name, t, dev):
-    """t is a contiguous tensor of e4m3 codes on `dev`."""
-    if t.dtype is not torch.float8_e4m3fn or t.device != dev or not t.is_contiguous():
-        _on_device(name, t, dev, torch.float8_e4m3fn)
-
-
-def _pages(k_pages, v_pages, layered=False, check=_halves):
+def _pages(k_pages, v_pages, layered=False):
     """(dev, layers, P, Hkv, d) of a cache's pages."""
     dev, shape = k_pages.device, k_pages.shape
-    check("k_pages", k_pages, dev)
+    _halves("k_pages", k_pages, dev)
     if v_pages is not None:
-        check("v_pages", v_pages, dev)
+        _halves("v_pages", v_pages, dev)
         if v_pages.shape != shape:
             raise ValueError("k_pages and v_pages must have the same shape")
     n = len(shape)
@@ -621,16 +615,24 @@ def _pages(k_pages, v_pages, layered=False, check=_halves):
 
 
 def _pages8(k_pages, v_pages, k_scales, v_scales, layered=False):
-    """The same of pages of codes and their scales."""
-    got = _pages(k_pages, v_pages, layered, _codes8)
-    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
-        if t is None:
-            continue
-        if t.dtype is not torch.float32 or t.device != got[0] or not t.is_contiguous():
-            _on_device(name, t, got[0], torch.float32)
-        if t.shape != k_pages.shape[:-2]:
-            raise ValueError(f"{name} must be {list(k_pages.shape[:-2])} (got {list(t.shape)})")
-    return got
+    """The same of pages of codes and their scales (v_pages and v_scales may be None)."""
+    dev, shape = k_pages.device, k_pages.shape
+    for name, t, dtype in (("k_pages", k_pages, torch.float8_e4m3fn), ("v_pages", v_pages, torch.float8_e4m3fn),
+                           ("k_scales", k_scales, torch.float32), ("v_scales", v_scales, torch.float32)):
+        if t is not None and (t.dtype is not dtype or t.device != dev or not t.is_contiguous()):
+            _on_device(name, t, dev, dtype)
+    n = len(shape)
+    if n != 4 and not (layered and n == 5):
+        raise ValueError("pages must be [P, Hkv, 64, d]" + (" or [layers, P, Hkv, 64, d]" if layered else ""))
+    P, Hkv, tokens, d = shape[-4:]
+    if tokens != PAGE_TOKENS:
+        raise ValueError(f"pages must hold {PAGE_TOKENS} tokens")
+    heads = shape[:-2]
+    if v_pages is not None and v_pages.shape != shape:
+        raise ValueError("k_pages and v_pages must have the same shape")
+    if k_scales.shape != heads or (v_scales is not None and v_scales.shape != heads):
+        raise ValueError(f"k_scales and v_scales must be {list(heads)}")
+    return dev, (shape[0] if n == 5 else 1), P, Hkv, d
 
 
 def _slots(slots, B, S, dev):
@@ -683,11 +685,7 @@ def pages_resize(k_pages, v_pages, table, lens, refs, slots, new_lens=None, *, r
     """Slots get the lengths ``new_lens`` (None: 0, they are freed): pages are given back, taken,
     and copied where a shared one will be written.  Returns ``result`` int32 [n, 4], whose first
     column is the new length or -1 where a request was refused (da_pages_resize)."""
-    return _resize("da_pages_resize", (k_pages, v_pages), (), table, lens, refs, slots, new_lens, result, stream)
-
-
-def _resize(name, pages, scales, table, lens, refs, slots, new_lens, result, stream):
-    dev, layers, P, Hkv, d = _pages8(*pages, *scales, layered=True) if scales else _pages(*pages, layered=True)
+    dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
     _ints("refs", refs, dev, (P,))
@@ -696,8 +694,8 @@ def _resize(name, pages, scales, table, lens, refs, slots, new_lens, result, str
     if new_lens is not None:
         _ints("new_lens", new_lens, dev, (n,))
     result = _requests(result, (n, 4), slots, on)
-    on.call(name, *map(_ptr, pages + scales), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M, P, _ptr(slots),
-            _ptr(new_lens), n, _ptr(result))
+    on.call("da_pages_resize", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
+            P, _ptr(slots), _ptr(new_lens), n, _ptr(result))
     return result
 
 
@@ -705,8 +703,18 @@ def pages8_resize(k_pages, v_pages, k_scales, v_scales, table, lens, refs, slots
                   stream=None):
     """pages_resize of a cache in 8 bits: k_pages and v_pages float8_e4m3fn, k_scales and v_scales
     fp32 [P, Hkv] or [layers, P, Hkv] (da_pages8_resize)."""
-    return _resize("da_pages8_resize", (k_pages, v_pages), (k_scales, v_scales), table, lens, refs, slots, new_lens, result,
-                   stream)
+    dev, layers, P, Hkv, d = _pages8(k_pages, v_pages, k_scales, v_scales, layered=True)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _ints("refs", refs, dev, (P,))
+    n = slots.numel()
+    _ints("slots", slots, dev, (n,))
+    if new_lens is not None:
+        _ints("new_lens", new_lens, dev, (n,))
+    result = _requests(result, (n, 4), slots, on)
+    on.call("da_pages8_resize", _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), layers, Hkv, d, _ptr(table),
+            _ptr(lens), _ptr(refs), S, M, P, _ptr(slots), _ptr(new_lens), n, _ptr(result))
+    return result
 
 
 def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_seqlens=None, max_seqlen=None,
@@ -736,29 +744,38 @@ def pages_append(k, v, k_pages, v_pages, table, lens, *, slots=None, B=None, cu_
         on.call("da_pages_append_to", *args, _ptr(new_lens))
 
 
-def _rows8(k, v, pages, scales, table, lens, T, B, cu_seqlens, max_seqlen, stream):
-    """Rows k, v that go into pages of codes or come from them: (on, T, layers, Hkv, d, S, M, P, B, N)."""
-    dev, layers, P, Hkv, d = _pages8(*pages, *scales, layered=True)
+def _rows8(name, k, v, cache, table, lens, T, slots, B, cu_seqlens, max_seqlen, ints, stream):
+    """Rows k, v of T tokens go into pages of codes, or come from them (None: into new ones, which are returned)."""
+    dev, layers, P, Hkv, d = _pages8(*cache, layered=True)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
-    shape = tuple(pages[0].shape[:-4]) + (T, Hkv, d)
-    for name, t in (("k", k), ("v", v)):
-        _halves(name, t, dev)
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
-    return (on, layers, Hkv, d, S, M, P) + _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    shape = (T, Hkv, d) if len(cache[0].shape) == 4 else (layers, T, Hkv, d)
+    if k is None:
+        k = on.empty(shape, torch.bfloat16)
+    if v is None:
+        v = on.like(k)
+    for what, t in (("k", k), ("v", v)):
+        _halves(what, t, dev)
+        if t.shape != shape:
+            raise ValueError(f"{what} must be {list(shape)} (got {list(t.shape)})")
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    if ints is not None:
+        _ints(*ints, dev, (B,))
+        ints = ints[1].data_ptr()
+    kp, vp, ks, vs = cache
+    on.call(name, k.data_ptr(), v.data_ptr(), T, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), layers, Hkv, d,
+            table.data_ptr(), lens.data_ptr(), S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, ints)
+    return k, v
 
 
 def pages8_append(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, *, slots=None, B=None, cu_seqlens=None,
                   max_seqlen=None, new_lens=None, stream=None):
     """pages_append to a cache in 8 bits: the keys and values are quantised as they are written, with
     a power of two for each page and kv head (da_pages8_append)."""
-    pages, scales, T = (k_pages, v_pages), (k_scales, v_scales), k.shape[-3] if k.dim() >= 3 else 0
-    on, layers, Hkv, d, S, M, P, B, N = _rows8(k, v, pages, scales, table, lens, T, B, cu_seqlens, max_seqlen, stream)
-    if new_lens is not None:
-        _ints("new_lens", new_lens, on.dev, (B,))
-    on.call("da_pages8_append", _ptr(k), _ptr(v), T, *map(_ptr, pages + scales), layers, Hkv, d, _ptr(table), _ptr(lens), S,
-            M, P, _slots(slots, B, S, on.dev), _ptr(cu_seqlens), B, N, _ptr(new_lens))
+    if k.dim() < 3:
+        raise ValueError("k must be [T, Hkv, d] for pages of one layer, [layers, T, Hkv, d] for more")
+    _rows8("da_pages8_append", k, v, (k_pages, v_pages, k_scales, v_scales), table, lens, k.shape[-3], slots, B, cu_seqlens,
+           max_seqlen, None if new_lens is None else ("new_lens", new_lens), stream)
 
 
 def pages8_read(k_pages, v_pages, k_scales, v_scales, table, lens, T, *, first=None, slots=None, B=None, cu_seqlens=None,
@@ -766,37 +783,15 @@ def pages8_read(k_pages, v_pages, k_scales, v_scales, table, lens, T, *, first=N
     """Tokens of a cache in 8 bits as bf16 rows: (k, v) [T, Hkv, d], or [layers, T, Hkv, d].  Row i of
     sequence b (B sequences of T / B rows, or cu_seqlens and max_seqlen) is its token first[b] + i
     (default 0 on); rows of tokens it does not hold are left as they are (da_pages8_read)."""
-    pages, scales, T = (k_pages, v_pages), (k_scales, v_scales), int(T)
-    if k is None or v is None:
-        on = _On(k_pages.device, stream)
-        shape = tuple(k_pages.shape[:-4]) + (T,) + tuple(k_pages.shape[-3:-2]) + tuple(k_pages.shape[-1:])
-        k = on.empty(shape, torch.bfloat16) if k is None else k
-        v = on.empty(shape, torch.bfloat16) if v is None else v
-    on, layers, Hkv, d, S, M, P, B, N = _rows8(k, v, pages, scales, table, lens, T, B, cu_seqlens, max_seqlen, stream)
-    if first is not None:
-        _ints("first", first, on.dev, (B,))
-    on.call("da_pages8_read", _ptr(k), _ptr(v), T, *map(_ptr, pages + scales), layers, Hkv, d, _ptr(table), _ptr(lens), S, M,
-            P, _slots(slots, B, S, on.dev), _ptr(cu_seqlens), B, N, _ptr(first))
-    return k, v
+    return _rows8("da_pages8_read", k, v, (k_pages, v_pages, k_scales, v_scales), table, lens, int(T), slots, B, cu_seqlens,
+                  max_seqlen, None if first is None else ("first", first), stream)
 
 
 def pages_compact(k_pages, v_pages, table, lens, refs, slots, start, keep, cu_keep, *, result=None, stream=None):
     """Of the tokens of slots[i] from start[i] on, those at start[i] + keep[cu_keep[i]:cu_keep[i + 1]]
     move up to start[i]; the rest is dropped.  Returns ``result`` int32 [n, 4], whose first column is
     the number kept or -1 where a request was refused (da_pages_compact)."""
-    return _compact("da_pages_compact", (k_pages, v_pages), (), table, lens, refs, slots, start, keep, cu_keep, result,
-                    stream)
-
-
-def pages8_compact(k_pages, v_pages, k_scales, v_scales, table, lens, refs, slots, start, keep, cu_keep, *, result=None,
-                   stream=None):
-    """pages_compact of a cache in 8 bits (da_pages8_compact)."""
-    return _compact("da_pages8_compact", (k_pages, v_pages), (k_scales, v_scales), table, lens, refs, slots, start, keep,
-                    cu_keep, result, stream)
-
-
-def _compact(name, pages, scales, table, lens, refs, slots, start, keep, cu_keep, result, stream):
-    dev, layers, P, Hkv, d = _pages8(*pages, *scales, layered=True) if scales else _pages(*pages, layered=True)
+    dev, layers, P, Hkv, d = _pages(k_pages, v_pages, layered=True)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
     _ints("refs", refs, dev, (P,))
@@ -811,8 +806,31 @@ def _compact(name, pages, scales, table, lens, refs, slots, start, keep, cu_keep
         n_keep = 0
     else:
         n_keep = keep.numel()
-    on.call(name, *map(_ptr, pages + scales), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M, P, _ptr(slots),
-            _ptr(start), _ptr(keep), n_keep, _ptr(cu_keep), n, _ptr(result))
+    on.call("da_pages_compact", _ptr(k_pages), _ptr(v_pages), layers, Hkv, d, _ptr(table), _ptr(lens), _ptr(refs), S, M,
+            P, _ptr(slots), _ptr(start), _ptr(keep), n_keep, _ptr(cu_keep), n, _ptr(result))
+    return result
+
+
+def pages8_compact(k_pages, v_pages, k_scales, v_scales, table, lens, refs, slots, start, keep, cu_keep, *, result=None,
+                   stream=None):
+    """pages_compact of a cache in 8 bits (da_pages8_compact)."""
+    dev, layers, P, Hkv, d = _pages8(k_pages, v_pages, k_scales, v_scales, layered=True)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _ints("refs", refs, dev, (P,))
+    n = slots.numel()
+    _ints("slots", slots, dev, (n,))
+    _ints("start", start, dev, (n,))
+    _ints("keep", keep, dev, (keep.numel(),))
+    _ints("cu_keep", cu_keep, dev, (n + 1,))
+    result = _requests(result, (n, 4), slots, on)
+    if not keep.numel():  # (an empty tensor has no address; no place is read)
+        keep = cu_keep
+        n_keep = 0
+    else:
+        n_keep = keep.numel()
+    on.call("da_pages8_compact", _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), layers, Hkv, d, _ptr(table),
+            _ptr(lens), _ptr(refs), S, M, P, _ptr(slots), _ptr(start), _ptr(keep), n_keep, _ptr(cu_keep), n, _ptr(result))
     return result
 
 
@@ -850,13 +868,13 @@ def paged8_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k=0) -> int:
     return int(load_library().da_paged8_workspace_bytes(B, max_seqlen, Hq, Hkv, d, max_len, top_k))
 
 
-def _tree(name, q, pages, scales, table, lens, mask, scores, slots, B, cu_seqlens, max_seqlen, max_len, out, lse,
+def _tree(name, q, cache, eight, table, lens, mask, cap, slopes, slots, B, cu_seqlens, max_seqlen, max_len, out, lse,
           workspace, stream):
-    """The attention calls over all pages: `scales` of pages of codes, `scores` (cap, slopes) or None."""
-    dev, _, P, Hkv, d = _pages8(*pages, *scales) if scales else _pages(*pages)
+    """The calls under changed scores, over bf16 pages or (eight) pages of codes and their scales."""
+    dev, _, P, Hkv, d = _pages8(*cache) if eight else _pages(*cache)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
-    out = _queries(q, *pages, out, lse, Hkv, d, on)
+    out = _queries(q, cache[0], cache[1], out, lse, Hkv, d, on)
     T, Hq = q.shape[:2]
     B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
     words = 0
@@ -867,11 +885,13 @@ def _tree(name, q, pages, scales, table, lens, mask, scores, slots, B, cu_seqlen
         words = mask.shape[1]
     room = M * PAGE_TOKENS
     max_len = room if max_len is None else min(int(max_len), room)
-    need = (paged8_workspace_bytes if scales else paged_workspace_bytes)(B, N, Hq, Hkv, d, max_len) if workspace is None else 0
+    need = 0
+    if workspace is None:
+        need = (paged8_workspace_bytes if eight else paged_workspace_bytes)(B, N, Hq, Hkv, d, max_len)
     ws, ptr, size = on.workspace(workspace, need)
-    more = () if scores is None else (float(scores[0]), _slopes(scores[1], Hq, dev))
-    on.call(name, _ptr(q), *map(_ptr, pages + scales), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), S, M, P,
-            _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, max_len, Hq, Hkv, d, _ptr(mask), words, *more, ptr, size)
+    on.call(name, _ptr(q), *[t.data_ptr() for t in cache], _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), S, M, P,
+            _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, max_len, Hq, Hkv, d, _ptr(mask), words, cap,
+            _slopes(slopes, Hq, dev), ptr, size)
     return out
 
 
@@ -883,42 +903,40 @@ def tree_attn_paged(q, k_pages, v_pages, table, lens, *, mask=None, slots=None, 
     the work is shared out as for sequences that long, which suits short ones in a table with far more
     room less well (8 of 500 tokens, room for 262144: 13.4 us, with max_len 500 11.5).  Returns ``out``
     [T, Hq, d] (tree_attn_paged)."""
-    return _tree("tree_attn_paged", q, (k_pages, v_pages), (), table, lens, mask, None, slots, B, cu_seqlens, max_seqlen,
-                 max_len, out, lse, workspace, stream)
+    dev, _, P, Hkv, d = _pages(k_pages, v_pages)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    out = _queries(q, k_pages, v_pages, out, lse, Hkv, d, on)
+    T, Hq = q.shape[:2]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    words = 0
+    if mask is not None:
+        _on_device("mask", mask, dev, torch.int64)
+        if mask.dim() != 2 or mask.shape[0] != T or mask.shape[1] * 64 < N:
+            raise ValueError("mask must be [T, words] with a bit for each of max_seqlen tokens")
+        words = mask.shape[1]
+    room = M * PAGE_TOKENS
+    max_len = room if max_len is None else min(int(max_len), room)
+    ws, ptr, size = on.workspace(workspace, paged_workspace_bytes(B, N, Hq, Hkv, d, max_len) if workspace is None else 0)
+    on.call("tree_attn_paged", _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), S, M,
+            P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, max_len, Hq, Hkv, d, _ptr(mask), words, ptr, size)
+    return out
 
 
 def tree_attn_paged_scored(q, k_pages, v_pages, table, lens, *, cap=0.0, slopes=None, mask=None, slots=None, B=None,
                            cu_seqlens=None, max_seqlen=None, max_len=None, out=None, lse=None, workspace=None,
                            stream=None):
     """tree_attn_paged under changed scores; no ``slopes`` with a ``mask`` (tree_attn_paged_scored)."""
-    return _tree("tree_attn_paged_scored", q, (k_pages, v_pages), (), table, lens, mask, (cap, slopes), slots, B, cu_seqlens,
-                 max_seqlen, max_len, out, lse, workspace, stream)
+    return _tree("tree_attn_paged_scored", q, (k_pages, v_pages), False, table, lens, mask, cap, slopes, slots, B,
+                 cu_seqlens, max_seqlen, max_len, out, lse, workspace, stream)
 
 
 def tree_attn_paged8(q, k_pages, v_pages, k_scales, v_scales, table, lens, *, cap=0.0, slopes=None, mask=None, slots=None,
                      B=None, cu_seqlens=None, max_seqlen=None, max_len=None, out=None, lse=None, workspace=None,
                      stream=None):
     """tree_attn_paged_scored over a cache in 8 bits (tree_attn_paged8)."""
-    return _tree("tree_attn_paged8", q, (k_pages, v_pages), (k_scales, v_scales), table, lens, mask, (cap, slopes), slots, B,
-                 cu_seqlens, max_seqlen, max_len, out, lse, workspace, stream)
-
-
-def _selected(name, q, cache, scales, table, lens, pages, slots, B, cu_seqlens, max_seqlen, out, lse, workspace, stream):
-    dev, _, P, Hkv, d = _pages8(*cache, *scales) if scales else _pages(*cache)
-    on = _On(dev, stream)
-    S, M = _table(table, lens, dev)
-    out = _queries(q, *cache, out, lse, Hkv, d, on)
-    T, Hq = q.shape[:2]
-    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
-    _ints("pages", pages, dev)
-    if pages.dim() != 3 or tuple(pages.shape[:2]) != (T, Hkv):
-        raise ValueError("pages must be [T, Hkv, top_k]")
-    top_k = pages.shape[2]
-    need = (paged8_workspace_bytes if scales else paged_workspace_bytes)(B, N, Hq, Hkv, d, 1, top_k) if workspace is None else 0
-    ws, ptr, size = on.workspace(workspace, need)
-    on.call(name, _ptr(q), *map(_ptr, cache + scales), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), S, M, P,
-            _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, Hq, Hkv, d, _ptr(pages), top_k, ptr, size)
-    return out
+    return _tree("tree_attn_paged8", q, (k_pages, v_pages, k_scales, v_scales), True, table, lens, mask, cap, slopes, slots,
+                 B, cu_seqlens, max_seqlen, max_len, out, lse, workspace, stream)
 
 
 def selected_attn_paged(q, k_pages, v_pages, table, lens, pages, *, slots=None, B=None, cu_seqlens=None,
@@ -926,15 +944,41 @@ def selected_attn_paged(q, k_pages, v_pages, table, lens, pages, *, slots=None, 
     """Attention of the last tokens of each sequence over the pages that ``pages`` [T, Hkv, top_k]
     lists for them (as select_pages does) and the page each of them is in.  Returns ``out``
     [T, Hq, d] (selected_attn_paged)."""
-    return _selected("selected_attn_paged", q, (k_pages, v_pages), (), table, lens, pages, slots, B, cu_seqlens, max_seqlen,
-                     out, lse, workspace, stream)
+    dev, _, P, Hkv, d = _pages(k_pages, v_pages)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    out = _queries(q, k_pages, v_pages, out, lse, Hkv, d, on)
+    T, Hq = q.shape[:2]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    _ints("pages", pages, dev)
+    if pages.dim() != 3 or tuple(pages.shape[:2]) != (T, Hkv):
+        raise ValueError("pages must be [T, Hkv, top_k]")
+    top_k = pages.shape[2]
+    ws, ptr, size = on.workspace(workspace, paged_workspace_bytes(B, N, Hq, Hkv, d, 1, top_k) if workspace is None else 0)
+    on.call("selected_attn_paged", _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens),
+            S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, Hq, Hkv, d, _ptr(pages), top_k, ptr, size)
+    return out
 
 
 def selected_attn_paged8(q, k_pages, v_pages, k_scales, v_scales, table, lens, pages, *, slots=None, B=None,
                          cu_seqlens=None, max_seqlen=None, out=None, lse=None, workspace=None, stream=None):
     """selected_attn_paged over a cache in 8 bits (selected_attn_paged8)."""
-    return _selected("selected_attn_paged8", q, (k_pages, v_pages), (k_scales, v_scales), table, lens, pages, slots, B,
-                     cu_seqlens, max_seqlen, out, lse, workspace, stream)
+    dev, _, P, Hkv, d = _pages8(k_pages, v_pages, k_scales, v_scales)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    out = _queries(q, k_pages, v_pages, out, lse, Hkv, d, on)
+    T, Hq = q.shape[:2]
+    B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
+    _ints("pages", pages, dev)
+    if pages.dim() != 3 or tuple(pages.shape[:2]) != (T, Hkv):
+        raise ValueError("pages must be [T, Hkv, top_k]")
+    top_k = pages.shape[2]
+    need = paged8_workspace_bytes(B, N, Hq, Hkv, d, 1, top_k) if workspace is None else 0
+    ws, ptr, size = on.workspace(workspace, need)
+    on.call("selected_attn_paged8", _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(out),
+            _ptr(lse), _ptr(table), _ptr(lens), S, M, P, _slots(slots, B, S, dev), _ptr(cu_seqlens), B, N, Hq, Hkv, d,
+            _ptr(pages), top_k, ptr, size)
+    return out
 
 
 def _summaries(codes, scales, blocks, Hkv, d, dev):
@@ -965,30 +1009,34 @@ def key_summary(k, *, B=None, cu_seqlens=None, max_seqlen=None, codes=None, scal
     return codes, scales
 
 
-def _page_summary(name, k_pages, k_scales, table, lens, codes, scales, slots, first, max_new, stream):
-    dev, _, P, Hkv, d = _pages(k_pages, None) if k_scales is None else _pages8(k_pages, None, k_scales, None)
+def page_summary(k_pages, table, lens, codes, scales, *, slots=None, first=None, max_new=None, stream=None):
+    """Updates the summaries codes int8 [P, Hkv, d] and scales fp32 [P, Hkv] of the whole pages of
+    each sequence, those from token ``first`` [B] (default 0) on and at most ``max_new`` tokens
+    further (default: all; a decoding step that has added n tokens passes the lengths before it and
+    n) (da_page_summary)."""
+    dev, _, P, Hkv, d = _pages(k_pages, None)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
     _summaries(codes, scales, P, Hkv, d, dev)
     B = S if slots is None else slots.numel()
     if first is not None:
         _ints("first", first, dev, (B,))
-    on.call(name, _ptr(k_pages), *(() if k_scales is None else (_ptr(k_scales),)), Hkv, d, _ptr(table), _ptr(lens), S, M, P,
-            _slots(slots, B, S, dev), _ptr(first), B, M * PAGE_TOKENS if max_new is None else int(max_new), _ptr(codes),
-            _ptr(scales))
-
-
-def page_summary(k_pages, table, lens, codes, scales, *, slots=None, first=None, max_new=None, stream=None):
-    """Updates the summaries codes int8 [P, Hkv, d] and scales fp32 [P, Hkv] of the whole pages of
-    each sequence, those from token ``first`` [B] (default 0) on and at most ``max_new`` tokens
-    further (default: all; a decoding step that has added n tokens passes the lengths before it and
-    n) (da_page_summary)."""
-    _page_summary("da_page_summary", k_pages, None, table, lens, codes, scales, slots, first, max_new, stream)
+    on.call("da_page_summary", _ptr(k_pages), Hkv, d, _ptr(table), _ptr(lens), S, M, P, _slots(slots, B, S, dev),
+            _ptr(first), B, M * PAGE_TOKENS if max_new is None else int(max_new), _ptr(codes), _ptr(scales))
 
 
 def page8_summary(k_pages, k_scales, table, lens, codes, scales, *, slots=None, first=None, max_new=None, stream=None):
     """page_summary of a cache in 8 bits (da_page8_summary)."""
-    _page_summary("da_page8_summary", k_pages, k_scales, table, lens, codes, scales, slots, first, max_new, stream)
+    dev, _, P, Hkv, d = _pages8(k_pages, None, k_scales, None)
+    on = _On(dev, stream)
+    S, M = _table(table, lens, dev)
+    _summaries(codes, scales, P, Hkv, d, dev)
+    B = S if slots is None else slots.numel()
+    if first is not None:
+        _ints("first", first, dev, (B,))
+    on.call("da_page8_summary", _ptr(k_pages), _ptr(k_scales), Hkv, d, _ptr(table), _ptr(lens), S, M, P,
+            _slots(slots, B, S, dev), _ptr(first), B, M * PAGE_TOKENS if max_new is None else int(max_new), _ptr(codes),
+            _ptr(scales))
 
 
 def select_blocks(q, codes, scales, *, top_k, block_q, n_sink=1, n_recent=1, B=None, cu_seqlens=None, max_seqlen=None,

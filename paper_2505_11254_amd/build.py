@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -36,11 +37,22 @@ def compile_flags() -> list:
 
 
 def build_library(verbose: bool = False) -> str:
+    """Compiles the sources side by side and links them."""
     tmp = LIB + ".tmp"
-    cmd = [hipcc()] + compile_flags() + SOURCES + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    flags = [f for f in compile_flags() if f != "-shared"]
+    with tempfile.TemporaryDirectory() as td:
+        objects = [os.path.join(td, os.path.basename(s) + ".o") for s in SOURCES]
+        cmds = [[hipcc()] + flags + ["-c", s, "-o", o] for s, o in zip(SOURCES, objects)]
+        if verbose:
+            print("\n".join(" ".join(c) for c in cmds), flush=True)
+        jobs = [subprocess.Popen(c) for c in cmds]
+        for job, cmd in zip(jobs, cmds):
+            if job.wait():
+                for other in jobs:
+                    other.wait()
+                raise subprocess.CalledProcessError(job.returncode, cmd)
+        link = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC"] + objects + ["-o", tmp]
+        subprocess.run(link, check=True)
     os.replace(tmp, LIB)
     return LIB
 

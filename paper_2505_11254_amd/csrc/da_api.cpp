@@ -453,8 +453,8 @@ Args base_args(const Problem& P) {
   a.gamma = P.gamma > 0 ? P.gamma : 1;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)P.d));
   a.head_chunk = 8192 / P.d;
-  a.scored = P.cap != 0.f || P.slopes || P.prefix;
-  set_cap(P.cap, P.d, &a.cap2, &a.cap_in);
+  a.scored = P.cap != 0.f ? kCapped : P.slopes || P.prefix ? kBiased : kPlain;
+  a.cap = make_cap(P.cap, P.d);
   a.slopes = P.slopes;
   a.prefix = P.prefix;
   return a;

@@ -35,12 +35,32 @@ inline bool cap_ok(float cap) {
   const int exponent = (int)(bits >> 23);  // of a positive one
   return bits << 1 == 0 || (exponent >= 127 - 10 && exponent < 127 + 10) || bits == 0x44800000u;
 }
-// Its coefficients: log2(e) cap, and 2 log2(e) / (cap sqrt(d)).
-inline void set_cap(float cap, int d, float* cap2, float* cap_in) {
-  *cap2 = *cap_in = 0.f;
-  if (cap == 0.f) return;
-  *cap2 = (float)(1.4426950408889634 * cap);
-  *cap_in = (float)(2 * 1.4426950408889634 / (cap * (d == 128 ? 11.313708498984761 : 8.)));
+
+// What the scored kernels know of scores: as they are, biased by distance (or seen past their row, up
+// to a prefix), or capped (biased or not).
+enum Scores { kPlain = 0, kBiased = 1, kCapped = 2 };
+// A cap of raw scores s = q.k, in base-2 units of the logits: cap2 tanh(s / (cap sqrt d)) with cap2 =
+// log2(e) cap, from exp2(in s), or as s P(s^2) of degree 5 or 7 while |s| <= limit[0] or limit[1].
+struct Cap {
+  float cap2, in, limit[2], p[2][4];
+};
+inline Cap make_cap(float cap, int d) {
+  Cap c{};
+  if (cap == 0.f) return c;
+  // x P(x^2) is nearest to tanh x over |x| <= kTo among odd polynomials of its degree: 4.9e-7 and 2.9e-7
+  // (least squares, weighted until the largest errors were alike).
+  static const double kTo[2] = {0.35, 0.55};
+  static const double kP[2][4] = {{0.9999902051741603, -0.33268410580631114, 0.12248037511995744},
+                                  {0.9999952677750817, -0.3331189777905361, 0.13068741145683763, -0.0415186653692223}};
+  const double cap2 = 1.4426950408889634 * cap, unit = 1. / (cap * (d == 128 ? 11.313708498984761 : 8.));
+  c.cap2 = (float)cap2;
+  c.in = (float)(2 * 1.4426950408889634 * unit);
+  for (int i = 0; i < 2; ++i) {
+    c.limit[i] = (float)(kTo[i] / unit);
+    double scale = cap2 * unit;
+    for (int j = 0; j < 4; ++j, scale *= unit * unit) c.p[i][j] = (float)(kP[i][j] * scale);
+  }
+  return c;
 }
 
 // Division by a divisor fixed for a launch, for numerators below 2^31.  With
@@ -78,10 +98,9 @@ struct Args {
   int Hq, Hkv, d;
   int window, n_sink, gamma;
   float scale_log2;   // log2(e) / sqrt(d): scores are exponentiated with exp2
-  // Changed scores (scored: the kernels that know them; see delta_attn.h)
-  int scored;
-  float cap2;             // log2(e) cap, or 0
-  float cap_in;           // 2 log2(e) / (cap sqrt(d))
+  // Changed scores (see delta_attn.h)
+  int scored;             // of Scores
+  Cap cap;
   const float* slopes;    // [Hq], or nullptr
   const int32_t* prefix;  // [B], or nullptr (dense causal rows only)
   // Anchors a < cover have a sparse key set equal to [0, a], so Delta = 0 there

@@ -134,9 +134,8 @@ constexpr int lds_bytes(int pre_bytes) {
          (MODE == kSparse ? pre_bytes + (NW > 4 ? (NW - 4) * kRowsPerWave * D * 2 : 0) : 0);
 }
 
-// One attention workgroup, block `bid` of the launch's `nblk`.  SC: scores are capped, biased by
-// distance, or (dense) a prefix of the keys is seen by every row.
-template <int D, int MODE, int NW, bool SC>
+// One attention workgroup, block `bid` of the launch's `nblk`.  SC: of Scores.
+template <int D, int MODE, int NW, int SC>
 __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t nblk) {
   using LD = Lds<D, NW>;
   constexpr int NS = kAttnStages;
@@ -361,7 +360,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // list entries outside [0, diag0) are not part of the key set (-1: skipped)
   // (biased scores fall with the distance: the nearest keys first, so that the reference of the
   // softmax, which only moves up, stays where they put it)
-  const bool back = SC && a.slopes;
+  const bool back = SC != kPlain && a.slopes;
   auto tile_at = [&](int it) -> int {
     if (back) it = n_iter - 1 - it;
     if (it >= n_a) return tb0 + (it - n_a);
@@ -399,8 +398,20 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // score accumulators start from, so that c times them is logit - ref.
   // (Scaling the queries by c ahead of the MFMA would round c q to bf16 once
   // more, an error proportional to the logits themselves.)
-  // (Changed scores are in base-2 units, with ref subtracted, as they come.)
-  const float qscale = SC ? 1.f : a.scale_log2, inv_qscale = SC ? 1.f : 1.f / a.scale_log2;
+  // Biased scores start from the bias of their offset in the tile, over c, and the rest of it goes with
+  // -ref into the exponential's fma (`off`), so that a bias costs no instruction per score.  Capped ones come
+  // in base-2 units with ref subtracted.
+  const float qscale = SC == kCapped ? 1.f : a.scale_log2, inv_qscale = SC == kCapped ? 1.f : 1.f / a.scale_log2;
+  const float slope = back ? a.slopes[h] * 1.4426950408889634f : 0.f;
+  f32x16 bias0, bias1;
+  float off = 0.f;
+  if constexpr (SC == kBiased) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      bias0[r] = slope * inv_qscale * (float)(8 * (r >> 2) + (r & 3));
+      bias1[r] = slope * inv_qscale * (float)(8 * (r >> 2) + (r & 3) + 32);
+    }
+  }
   float ref = 0.f;
   bool has_ref = false;
   f32x16 nref = f32x16{};
@@ -420,14 +431,10 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
 
-  // Changed scores, in base-2 units: cap tanh(q.k / (cap sqrt d)) - slope |i - j| - ref.  With
-  // e = exp2(2 log2(e) x), tanh x = 1 - 2 / (1 + e), whose error, some 2^-22, counts cap times:
-  // 2e-5 of a logit at cap 50.
-  const float slope = back ? a.slopes[h] * 1.4426950408889634f : 0.f;
+  // What changes the scores of a tile beyond that: cap tanh(q.k / (cap sqrt d)) - slope |i - j|.
   auto change = [&](int tile, f32x16& s0, f32x16& s1) {
     const float dist0 = (float)(tile * kKeyTile + 4 * half - my_pos);  // j - i of offset 0
-    const bool ahead = see >= 0;  // some rows see keys past them
-    const float base = (back && !ahead ? slope * dist0 : 0.f) - ref;
+    const float base = (back ? slope * dist0 : 0.f) - ref;
     auto each = [&](auto f) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -436,25 +443,28 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
         s1[r] = f(s1[r], o0 + 32.f);
       }
     };
-    if (a.cap2 > 0.f) {
-      const float c = a.cap_in, m = -2.f * a.cap2, top = a.cap2 + base;
-      each([&](float x, float) { return __builtin_fmaf(m, __builtin_amdgcn_rcpf(1.f + fast_exp2(c * x)), top); });
+    if constexpr (SC == kCapped) {
+      f32x16 s[2] = {s0, s1};
+      cap_scores(s, a.cap, base);
+      s0 = s[0];
+      s1 = s[1];
+      if (back) each([&](float x, float o) { return __builtin_fmaf(slope, o, x); });
     } else {
-      const float c = a.scale_log2;
-      each([&](float x, float) { return __builtin_fmaf(c, x, base); });
+      off = base;
     }
-    if (back && !ahead)
-      each([&](float x, float o) { return __builtin_fmaf(slope, o, x); });
-    else if (back)
-      each([&](float x, float o) { return __builtin_fmaf(-slope, fabsf(dist0 + o), x); });
+    // (keys past their row, which a prefix shows: their distance is the other way round)
+    if (back && see >= 0 && tile * kKeyTile + kKeyTile - 1 > wr0) {
+      const float twice = -2.f * slope * inv_qscale;
+      each([&](float x, float o) { return __builtin_fmaf(twice, fmaxf(dist0 + o, 0.f), x); });
+    }
   };
 
   // S^T of one tile against the wave's rows (register r of lane half h holds
   // key 8*(r/4) + 4*h + r%4 in s0, that key + 32 in s1); keys outside a row's
   // key set read -inf when `masked`.
   auto qk = [&](const uint16_t* ks, int tile, int masked, f32x16& s0, f32x16& s1) {
-    s0 = SC ? f32x16{} : nref;
-    s1 = SC ? f32x16{} : nref;
+    s0 = SC == kPlain ? nref : SC == kBiased ? bias0 : f32x16{};
+    s1 = SC == kPlain ? nref : SC == kBiased ? bias1 : f32x16{};
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const bf16x8 ka = *(const bf16x8*)(ks + kread[kk]);
@@ -517,6 +527,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
     float mx = fmaxf(fmaxf(fmaxf(t3[0], t3[1]), fmaxf(t3[2], t3[3])),
                      fmaxf(fmaxf(t3[4], t3[5]), fmaxf(t3[6], t3[7])));
     mx = fmaxf(mx, fmaxf(t3[8], fmaxf(t3[9], t3[10])));
+    if constexpr (SC == kBiased) mx += off * inv_qscale;
     const auto pr = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx),
                                                      false, false);
     return qscale * fmaxf(__uint_as_float(pr[0]), __uint_as_float(pr[1]));
@@ -545,8 +556,8 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
       f32x16 p0, p1;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        p0[i] = fast_exp2(qscale * s0[i]);
-        p1[i] = fast_exp2(qscale * s1[i]);
+        p0[i] = fast_exp2(SC == kBiased ? __builtin_fmaf(qscale, s0[i], off) : qscale * s0[i]);
+        p1[i] = fast_exp2(SC == kBiased ? __builtin_fmaf(qscale, s1[i], off) : qscale * s1[i]);
       }
       pf[0] = __builtin_convertvector(p0.lo, bf16x8);
       pf[1] = __builtin_convertvector(p0.hi, bf16x8);
@@ -592,11 +603,15 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
 #pragma unroll
         for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
         const float dr = dm * inv_qscale;
+        if constexpr (SC == kBiased) {
+          off -= dm;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s0[i] -= dr;
-          s1[i] -= dr;
-          nref[i] = -ref * inv_qscale;
+          for (int i = 0; i < 16; ++i) {
+            s0[i] -= dr;
+            s1[i] -= dr;
+            nref[i] = -ref * inv_qscale;
+          }
         }
       }
       t = weights();
@@ -988,7 +1003,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
 #define DA_ATTN_KERNEL(D, NW) \
   __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 64 && NW == 4 ? 3 : 2)))
 
-template <int D, int MODE, int NW, bool SC>
+template <int D, int MODE, int NW, int SC>
 DA_ATTN_KERNEL(D, NW) void attn_kernel(Args a) {
   attn_body<D, MODE, NW, SC>(a, blockIdx.x, gridDim.x);
 }
@@ -1002,7 +1017,7 @@ DA_ATTN_KERNEL(D, NW) void attn_kernel(Args a) {
 // tokens 36.0 -> 27.5 us, 4000 tokens 89 -> 77 us, 16000 tokens 302 -> 279 us;
 // Delta, GQA 3, gamma 48, 20K tokens 433 -> 402 us; EMA 64K tokens 2791 -> 2763
 // us; 131K tokens, 32 heads 6622 -> 6697 us (64 rounds of the CUs: not taken).
-template <int D, int NW, bool SC>
+template <int D, int NW, int SC>
 DA_ATTN_KERNEL(D, NW) void attn_pair_kernel(Args ar, Args as, uint32_t nr, uint32_t nr8) {
   if (blockIdx.x >= nr8)
     attn_body<D, kSparse, NW, SC>(as, blockIdx.x - nr8, gridDim.x - nr8);
@@ -1520,7 +1535,7 @@ int pre_bytes(const Args& a) {
   return a.fuse && a.gamma > 1 ? a.hpw * (kRowsPerWave * a.ppw / a.gamma) * a.d * 4 : 0;
 }
 
-template <int MODE, bool SC>
+template <int MODE, int SC>
 hipError_t launch_attn_as(const Args& a0, hipStream_t s, int64_t nblocks) {
   if (nblocks <= 0) return hipSuccess;
   if (nblocks > INT32_MAX) return hipErrorInvalidValue;
@@ -1546,7 +1561,11 @@ hipError_t launch_attn_as(const Args& a0, hipStream_t s, int64_t nblocks) {
 
 template <int MODE>
 hipError_t launch_attn(const Args& a, hipStream_t s, int64_t nblocks) {
-  return a.scored ? launch_attn_as<MODE, true>(a, s, nblocks) : launch_attn_as<MODE, false>(a, s, nblocks);
+  switch (a.scored) {
+    case kPlain: return launch_attn_as<MODE, kPlain>(a, s, nblocks);
+    case kBiased: return launch_attn_as<MODE, kBiased>(a, s, nblocks);
+    default: return launch_attn_as<MODE, kCapped>(a, s, nblocks);
+  }
 }
 
 constexpr int kScratchDevices = 64;
@@ -1651,8 +1670,9 @@ hipError_t launch_sparse(const Args& a0, hipStream_t s) {
                      s, ar, as, (uint32_t)nr, (uint32_t)nr8)
 #define DA_PAIR(DD, W)              \
   do {                              \
-    if (as.scored) DA_PAIR_AS(DD, W, true); \
-    else DA_PAIR_AS(DD, W, false);  \
+    if (as.scored == kPlain) DA_PAIR_AS(DD, W, kPlain); \
+    else if (as.scored == kBiased) DA_PAIR_AS(DD, W, kBiased); \
+    else DA_PAIR_AS(DD, W, kCapped); \
   } while (0)
   if (as.d == 128) {
     if (waves == 8) DA_PAIR(128, 8);

@@ -130,9 +130,9 @@ struct PagedArgs {
   const void* v;
   const float* k_scales;  // [P][Hkv] powers of two of the codes, or nullptr: bf16
   const float* v_scales;
-  // Changed scores (scored: the kernels that know them; see delta_attn.h)
-  int scored;
-  float cap2, cap_in;    // log2(e) cap, or 0; 2 log2(e) / (cap sqrt(d))
+  // Changed scores (see delta_attn.h)
+  int scored;            // of Scores
+  Cap cap;
   const float* slopes;   // [Hq], or nullptr
   uint16_t* out;         // [T][Hq][d]
   float* lse;            // [T][Hq], or nullptr

@@ -138,8 +138,8 @@ da_status paged_attn(PagedArgs a, int n_list, float cap, void* workspace, size_t
   if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   st = check_device();
   if (st != DA_OK) return st;
-  a.scored = cap != 0.f || a.slopes;
-  set_cap(cap, a.d, &a.cap2, &a.cap_in);
+  a.scored = cap != 0.f ? kCapped : a.slopes ? kBiased : kPlain;
+  a.cap = make_cap(cap, a.d);
   a.scale_log2 = 1.4426950408889634f / (a.d == 128 ? 11.313708498984761f : 8.f);
   a.G = a.Hq / a.Hkv;
   a.fd_G = make_fastdiv(a.G);

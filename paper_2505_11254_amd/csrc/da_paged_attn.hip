@@ -134,8 +134,8 @@ __device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
   return a.whole ? x.segs : x.segs * x.np;
 }
 
-// SC: scores are capped or biased by distance (see delta_attn.h).
-template <int D, int RT, bool LISTS, bool E8, bool SC>
+// SC: of Scores.
+template <int D, int RT, bool LISTS, bool E8, int SC>
 __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAVES)) void paged_attn_kernel(PagedArgs a) {
   using SH = Shape<D, RT, E8>;
   static_assert(!(LISTS && SC), "lists have plain scores");
@@ -327,8 +327,17 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
   // Online softmax against a lagging reference, as in the prefill kernels: `ref` in
   // base-2 units of the logits, -ref / c in every register of nref, from which the score
   // accumulators start, so that c times them is logit - ref.
-  // (Changed scores are in base-2 units, with ref subtracted, as they come.)
-  const float c2 = SC ? 1.f : a.scale_log2, inv_c2 = SC ? 1.f : 1.f / a.scale_log2;
+  // Changed scores as there: biased ones start from the bias of their offset in the unit, over c,
+  // and `off` has the rest of it and -ref; capped ones come in base-2 units with ref subtracted.
+  const float c2 = SC == kCapped ? 1.f : a.scale_log2, inv_c2 = SC == kCapped ? 1.f : 1.f / a.scale_log2;
+  f32x16 bias[NB];
+  float off = 0.f;
+  if constexpr (SC == kBiased) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) bias[nb][q] = slope * inv_c2 * (float)(32 * nb + 8 * (q >> 2) + (q & 3));
+  }
   float ref = 0.f, l = 0.f;
   bool has_ref = false;
   f32x16 nref = f32x16{};
@@ -468,7 +477,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     const float k_scale = __uint_as_float((se & 255u) << 23), v_scale = __uint_as_float((se >> 8) << 23);
     f32x16 sc[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sc[nb] = SC ? f32x16{} : nref;
+    for (int nb = 0; nb < NB; ++nb) sc[nb] = SC == kPlain ? nref : SC == kBiased ? bias[nb] : f32x16{};
     // K reads kAhead MFMAs ahead of their use, an order that the scheduling barriers hold
     // (left to itself the compiler pairs each MFMA with its own read and a wait)
     constexpr int kAhead = 4;
@@ -509,24 +518,21 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     const int at = q0 + u / UPP;
     const int k0 = (LISTS ? own : at) * kPage + u % UPP * UNIT;
     if constexpr (SC) {
-      // In base-2 units: cap tanh(q.k / (cap sqrt d)) - slope (i - j) - ref, tanh as in the prefill
-      // kernels.  (Biased rows see no key past their own.)
+      // cap tanh(q.k / (cap sqrt d)) - slope (i - j)  (biased rows see no key past their own)
       const float dist0 = (float)(k0 + 4 * half - pos);  // j - i of offset 0
       const float base = (biased ? slope * dist0 : 0.f) - ref;
-      auto each = [&](auto f) {
+      if constexpr (SC == kCapped) {
+        cap_scores(sc, a.cap, base);
+        if (biased) {
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
+          for (int q = 0; q < 16; ++q)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) sc[nb][q] = f(sc[nb][q], (float)(32 * nb + 8 * (q >> 2) + (q & 3)));
-      };
-      if (a.cap2 > 0.f) {
-        const float c = a.cap_in, m = -2.f * a.cap2, top = a.cap2 + base;
-        each([&](float x, float) { return __builtin_fmaf(m, __builtin_amdgcn_rcpf(1.f + fast_exp2(c * x)), top); });
+            for (int nb = 0; nb < NB; ++nb)
+              sc[nb][q] = __builtin_fmaf(slope, (float)(32 * nb + 8 * (q >> 2) + (q & 3)), sc[nb][q]);
+        }
       } else {
-        const float c = a.scale_log2;
-        each([&](float x, float) { return __builtin_fmaf(c, x, base); });
+        off = base;
       }
-      if (biased) each([&](float x, float o) { return __builtin_fmaf(slope, o, x); });
     }
     // mask the units that some row does not see whole
     if (LISTS ? at >= a.n_list : k0 + UNIT > first) {
@@ -549,7 +555,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
 #pragma unroll
       for (int q = 0; q < 16; ++q)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) p[nb][q] = fast_exp2(c2 * sc[nb][q]);
+        for (int nb = 0; nb < NB; ++nb)
+          p[nb][q] = fast_exp2(SC == kBiased ? __builtin_fmaf(c2, sc[nb][q], off) : c2 * sc[nb][q]);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         pf[2 * nb] = __builtin_convertvector(p[nb].lo, bf16x8);
@@ -590,6 +597,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int q = 0; q < 16; ++q) mx = fmaxf(mx, sc[nb][q]);
+      if constexpr (SC == kBiased) mx += off * inv_c2;
       const auto pr = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = c2 * fmaxf(__uint_as_float(pr[0]), __uint_as_float(pr[1]));
       // a lane without a reference takes the unit's maximum (if it sees a key); one with a
@@ -605,11 +613,15 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
         const float dr = dm * inv_c2;
+        if constexpr (SC == kBiased) {
+          off -= dm;
+        } else {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
+          for (int q = 0; q < 16; ++q) {
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) sc[nb][q] -= dr;
-          nref[q] = -ref * inv_c2;
+            for (int nb = 0; nb < NB; ++nb) sc[nb][q] -= dr;
+            nref[q] = -ref * inv_c2;
+          }
         }
       }
       tsum = weights();
@@ -858,7 +870,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a)
 
 namespace {
 
-template <bool E8, bool SC>
+template <bool E8, int SC>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.n_wgs);
 #define DA_PAGED(DD, RT, LS)                                                                       \
@@ -870,7 +882,7 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
     case 2: DA_PAGED(DD, 2, LS); break;                                                            \
     default: DA_PAGED(DD, 4, LS); break;                                                           \
   }
-  if constexpr (!SC) {
+  if constexpr (SC == kPlain) {
     if (a.lists) {
       if (a.d == 128) {
         DA_PAGED_RT(128, true)
@@ -897,10 +909,12 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
 
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   hipError_t e;
-  if (a.k_scales)
-    e = a.scored ? launch_paged_as<true, true>(a, s) : launch_paged_as<true, false>(a, s);
-  else
-    e = a.scored ? launch_paged_as<false, true>(a, s) : launch_paged_as<false, false>(a, s);
+  const bool eight = a.k_scales != nullptr;
+  switch (a.scored) {
+    case kPlain: e = eight ? launch_paged_as<true, kPlain>(a, s) : launch_paged_as<false, kPlain>(a, s); break;
+    case kBiased: e = eight ? launch_paged_as<true, kBiased>(a, s) : launch_paged_as<false, kBiased>(a, s); break;
+    default: e = eight ? launch_paged_as<true, kCapped>(a, s) : launch_paged_as<false, kCapped>(a, s);
+  }
   if (e != hipSuccess) return e;
   if (!a.units) return hipGetLastError();  // no rows are cut
   const int64_t rows = (int64_t)a.B * a.N * a.Hq;

@@ -8,9 +8,10 @@ most 1 + x, the output moves by at most x sum_j p_j |v_j - out| (to first order;
 the rest), and that sum is at most dev = sqrt(sum_j p_j v_j^2 - out^2).  So
   tol = 2^-8 |out| + (2^-8 + dl) (1 + 2^-7) dev + 1e-6 max |v|    (the sums' own rounding in fp32).
 A score q.k / sqrt d is a sum of d products in fp32, off by at most d 2^-24 sum |q_c k_c| / sqrt d; a cap's
-tanh by 2^-21 of the cap; scaling, bias, reference and the exponential add a few steps (2^-22 together) of
+tanh by 2^-20 of the cap; scaling, bias, reference and the exponential add a few steps (2^-22 together) of
 the logits' size, of which only those within some 64 of the row's largest have weight; and a bias is
-added up from the first key of a tile of 64, up to 128 slopes away (2^-24 of that, twice).
+that of a tile's first key, up to 128 slopes, and what its 63 others add, from which the d products' sum
+starts: (d 63 + 128) 2^-24 < 2^-10.9 slopes.
 """
 from __future__ import annotations
 
@@ -43,7 +44,7 @@ def attend(q, k, v, vis, cap=0.0, bias=None):
     sums = d * 2.0 ** -24 * float((q.abs() @ k.abs().T).max()) / d ** 0.5 if a.numel() else 0.0
     size = float(top.abs().max()) if len(top) else 0.0
     slope = float((bias[:, 1:] - bias[:, :-1]).abs().max()) if bias is not None and bias.shape[1] > 1 else 0.0
-    dl = 2 * (sums + cap * 2.0 ** -21 + 2.0 ** -22 * (2 * size + 64) + slope * 2.0 ** -16)
+    dl = 2 * (sums + cap * 2.0 ** -20 + 2.0 ** -22 * (2 * size + 64) + slope * (63 * d + 128) * 2.0 ** -24)
     return out, torch.where(z > 0, top + torch.log(z), torch.full_like(z, float("-inf"))), dev, dl
 
 
