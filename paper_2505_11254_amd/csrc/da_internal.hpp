@@ -98,11 +98,6 @@ struct Args {
   int Hq, Hkv, d;
   int window, n_sink, gamma;
   float scale_log2;   // log2(e) / sqrt(d): scores are exponentiated with exp2
-  // Changed scores (see delta_attn.h)
-  int scored;             // of Scores
-  Cap cap;
-  const float* slopes;    // [Hq], or nullptr
-  const int32_t* prefix;  // [B], or nullptr (dense causal rows only)
   // Anchors a < cover have a sparse key set equal to [0, a], so Delta = 0 there
   // and their groups keep the sparse rows: n_sink + window for sink + window
   // attention, 0 for key-block lists.
@@ -165,6 +160,12 @@ struct Args {
   // Fused schedule: the sparse kernel stores the corrected rows itself from the
   // merged dense rows (0: plain sparse store; 1: Delta correction; 2: recompute).
   int fuse;
+
+  // Changed scores (see delta_attn.h)
+  int scored;             // of Scores
+  Cap cap;
+  const float* slopes;    // [Hq], or nullptr
+  const int32_t* prefix;  // [B], or nullptr (dense causal rows only)
 };
 
 // Sizes of the Delta path's workspace for a problem; all in elements/bytes.

@@ -128,12 +128,6 @@ struct PagedArgs {
   const uint16_t* q;     // [T][Hq][d]
   const void* k;         // [P][Hkv][64][d] bf16, or e4m3 codes
   const void* v;
-  const float* k_scales;  // [P][Hkv] powers of two of the codes, or nullptr: bf16
-  const float* v_scales;
-  // Changed scores (see delta_attn.h)
-  int scored;            // of Scores
-  Cap cap;
-  const float* slopes;   // [Hq], or nullptr
   uint16_t* out;         // [T][Hq][d]
   float* lse;            // [T][Hq], or nullptr
   const int32_t* table;  // [S][M]
@@ -157,6 +151,12 @@ struct PagedArgs {
   int32_t* units;        // [B + 3] pages before each sequence's, the share, whether aligned, team
   float* part_o;         // [n_wgs][2][row_tiles * 32][d] partial results of cut segments
   float* part_ml;        // [n_wgs][2][row_tiles * 32][2]
+  const float* k_scales;  // [P][Hkv] powers of two of the codes, or nullptr: bf16
+  const float* v_scales;
+  // Changed scores (see delta_attn.h)
+  int scored;            // of Scores
+  Cap cap;
+  const float* slopes;   // [Hq], or nullptr
 };
 // Units per workgroup or team, of `total` for n of them (up to the largest int: the sum is unsigned).
 __host__ __device__ __forceinline__ int share_of(int min_units, int total, int n) {

@@ -67,6 +67,10 @@ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 //    kAlignPages pages, less than a second start and its partial results: one sequence of
 //    9000 keys, 14 drafts 26.5 -> 21.8 us; six of them 40.4 -> 37.3; 16 of 24 drafts, 6000
 //    keys 60.5 -> 58.7; eight of 2000 keys, 8 heads on 2, d 64, one token 13.0 -> 10.6.
+//  - Pages of codes are half as long and take two thirds of the time in workgroups of one and two row
+//    tiles, of which two fit a CU with two tiles or d = 64 (us, with the numbers of bf16 and these: 64 of
+//    up to 8192 keys, d 64 80, 68.5; 16 of up to 2000, d 128 23.1, 19.1; 64 of up to 900, d 64 14.6 to
+//    18.8, 13.5; 16 trees of 12 over up to 6000 42, 38.7).
 constexpr int kAlignPages = 8;
 struct PagedPlan {
   int row_tiles, n_wgs, min_units, whole, align_pages, row_groups;
@@ -79,6 +83,8 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   const int rt = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || d == 64 || n_list ? 4 : 8;
   const int c = rt == 1 ? 0 : rt == 2 ? 1 : rt == 4 ? 2 : 3;
   static const int kSlots[2][4] = {{256, 256, 512, 256}, {256, 256, 512, 512}};
+  static const int kSlots8[2][4] = {{256, 512, 512, 256}, {512, 512, 512, 512}};
+  constexpr double kPage8 = 0.65;  // (one and two row tiles)
   static const double kPageUs[2][4] = {{0.46, 0.9, 1.08, 1.54}, {0.29, 0.55, 0.8, 0.8}};
   static const double kCutUs[4] = {6., 8., 17., 35.};
   const int64_t groups = (rows + 32 * rt - 1) / (32 * rt);
@@ -86,8 +92,8 @@ da_status paged_plan(int B, int N, int Hq, int Hkv, int d, int64_t pages, int n_
   if (n_list) pages = (int64_t)n_list + 1;
   if (pages < 1) pages = 1;
   if ((double)segs * (double)pages > (double)INT32_MAX) return DA_ERR_SHAPE;
-  const int64_t slots = kSlots[d == 64][c];
-  const double page_us = kPageUs[d == 64][c], seg_us = (double)pages * page_us;
+  const int64_t slots = (eight ? kSlots8 : kSlots)[d == 64][c];
+  const double page_us = kPageUs[d == 64][c] * (eight && c < 2 ? kPage8 : 1.), seg_us = (double)pages * page_us;
   // (lengths below the longest are taken to make four fifths of the work)
   const double rounds = (double)segs / (double)slots;
   p->row_tiles = rt;

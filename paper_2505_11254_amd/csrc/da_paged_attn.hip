@@ -26,6 +26,13 @@
 // GFLOP in 234 to 256 us, 0.93 to 1.02 PFLOP/s, the matrix cores busy half the time.  (There
 // rings of 3 and 4 stages took as long as 2: not the latency of the transfers.)  With keys
 // that stay in the L2 it takes a fifth less.
+//
+// Pages of e4m3 codes have half the bytes.  K fragments are 16 codes a lane, two products' worth, V^T
+// fragments one transposing read of 8-bit elements; v_cvt_scalef32_pk_bf16_fp8 turns two codes at a time into
+// bf16 and applies the page's power of two, without rounding, so that everything behind it is as for
+// bf16.  Every wave converts what it reads: with few rows that hides behind HBM but for a tenth, with
+// eight row tiles it costs 5 % against bf16.  64 single tokens over up to 8192 keys 0.68 GB in 140 us, 4.9
+// TB/s, over 5120 each 133 us, 5.0; the transfers alone 122 (5.5), rings of four half-size units 153.
 #include "da_device.hpp"
 #include "da_paged.hpp"
 
@@ -55,8 +62,7 @@ struct Shape {
   static constexpr int ringElems = KS * DEPTH * unitElems;
   static constexpr int regions = UNIT * RB / 1024;  // 1 KB DMA regions per tile
   static constexpr int RPW = regions / RT;          // of a wave
-  // (behind the ring: page ids, the pages' scales, a few sums)
-  static constexpr int ldsBytes = ringElems * 2 + kIdPages * (E8 ? 8 : 4) + 256;
+  static constexpr int ldsBytes = ringElems * 2 + kIdPages * 4 + 256;
   // Weights as two bf16 parts, the nearest value and what it leaves (2^-16 of a weight is lost
   // instead of 2^-8): the root mean square error of the outputs is that of their own rounding.
   // One row tile has matrix cores to spare behind HBM: 64 single tokens over 8192 keys 239.8 -> 241.1
@@ -67,8 +73,6 @@ struct Shape {
   static constexpr bool TWO_PARTS = RT == 1;
   // waves per SIMD that LDS has room for
   static constexpr int WAVES = ldsBytes > 81920 ? 1 : 2;
-  // Rows of codes: the 16 rows of a lane group that reads one chunk of each, keys in order and
-  // values four by four, cover all banks.
   __device__ static constexpr int kswz(int r) {
     if (E8) return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
     return D == 128 ? (r & 15) : ((r >> 1) & 7);
@@ -134,17 +138,21 @@ __device__ __forceinline__ int units_of(const PagedArgs& a, const SeqWork& x) {
   return a.whole ? x.segs : x.segs * x.np;
 }
 
-// SC: of Scores.
-template <int D, int RT, bool LISTS, bool E8, int SC>
-__global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAVES)) void paged_attn_kernel(PagedArgs a) {
+// SC: of Scores.  TWICE: every row of a tile of 32 twice, lanes 16 apart, where a segment has at most
+// 16 of them: the first has the weights' nearest values, the second what those leave, so that one product
+// sums both parts.  (Its wavefronts hold themselves to half of the registers even where they are alone
+// on a SIMD: with all of them the compiler moves the outputs between the two halves, 130 instructions per
+// unit.)
+template <int D, int RT, bool LISTS, bool E8, int SC, bool TWICE>
+__global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (TWICE && SC != kBiased ? 2 : Shape<D, RT, E8>::WAVES))
+void paged_attn_kernel(PagedArgs a) {
   using SH = Shape<D, RT, E8>;
-  static_assert(!(LISTS && SC), "lists have plain scores");
+  static_assert(!(LISTS && SC) && (!TWICE || SH::TWO_PARTS));
   constexpr int NW = SH::NW, KS = SH::KS, DEPTH = SH::DEPTH, RPW = SH::RPW, MB = D / 32;
   constexpr int UNIT = SH::UNIT, UPP = SH::UPP, NB = SH::NB;
   constexpr int kThreads = 64 * NW;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
   int* const ids = (int*)(smem + SH::ringElems);
-  int* const exps = ids + kIdPages;  // (of codes) exponents of the pages' scales: keys' | values' << 8
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -223,7 +231,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     b = __builtin_ctzll(__ballot(before <= x0 && x0 < upto));
     off = (int)x0 - __builtin_amdgcn_readlane(before, b);
   } else {
-    int* const red = ids + kIdPages * (E8 ? 2 : 1);  // [NW] sums, then what is found
+    int* const red = ids + kIdPages;  // [NW] sums, then what is found
     auto block_scan = [&](int x, int* total) {
       x = wave_scan_add(x);
       __syncthreads();
@@ -304,7 +312,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
   const int last_key = LISTS ? first + tok : sq.L - 1;
 
   // ---- this lane's row
-  const int r = row0 + rt * 32 + col;
+  const int r = TWICE ? col & 15 : row0 + rt * 32 + col;
   const int rc = min(r, n_rows - 1);
   const int i_tok = LISTS ? tok : (int)fdiv(rc, a.fd_G);
   const int64_t t = base + i_tok;
@@ -328,7 +336,9 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
   // base-2 units of the logits, -ref / c in every register of nref, from which the score
   // accumulators start, so that c times them is logit - ref.
   // Changed scores as there: biased ones start from the bias of their offset in the unit, over c,
-  // and `off` has the rest of it and -ref; capped ones come in base-2 units with ref subtracted.
+  // and `off` has the rest of it and -ref (OFF); capped ones come in base-2 units with ref subtracted.
+  // Those of codes start from 0 likewise, which leaves registers to the codes' conversion.
+  constexpr bool OFF = SC == kBiased || (SC == kPlain && E8);
   const float c2 = SC == kCapped ? 1.f : a.scale_log2, inv_c2 = SC == kCapped ? 1.f : 1.f / a.scale_log2;
   f32x16 bias[NB];
   float off = 0.f;
@@ -356,14 +366,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       if (at < 0 || at > own || (at == own && q0 + j < a.n_list)) at = -1;
     }
     const int e = at >= 0 ? a.table[(int64_t)sq.s * a.M + at] : -1;
-    const bool there = (unsigned)e < (unsigned)a.P;
-    ids[j] = there ? e : -1;  // (-1: no such page, its keys are not seen)
-    if constexpr (E8) {
-      if (there) {
-        const int64_t i = (int64_t)e * a.Hkv + g;
-        exps[j] = (int)(__float_as_uint(a.k_scales[i]) >> 23 & 255u) | (int)(__float_as_uint(a.v_scales[i]) >> 23 & 255u) << 8;
-      }
-    }
+    ids[j] = (unsigned)e < (unsigned)a.P ? e : -1;  // (-1: no such page, its keys are not seen)
   }
   // the queries have landed: the loop's products must not wait for them behind the
   // transfers issued there
@@ -469,15 +472,14 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     return (uint32_t)(sh ? (lo >> sh) | (hi << (64 - sh)) : lo);
   };
 
-  auto compute = [&](int it, auto stage, int scales) {
+  auto compute = [&](int it, auto stage, uint32_t scales) {
     const int u = unit_of(it);
     const uint16_t* ku = smem + decltype(stage)::value * SH::unitElems;
     const uint16_t* vu = ku + UNIT * SH::RB / 2;
-    const uint32_t se = E8 ? (uint32_t)__builtin_amdgcn_readfirstlane(scales) : 0u;
-    const float k_scale = __uint_as_float((se & 255u) << 23), v_scale = __uint_as_float((se >> 8) << 23);
+    const float k_scale = __uint_as_float((scales & 255u) << 23), v_scale = __uint_as_float(scales >> 8 << 23);
     f32x16 sc[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sc[nb] = SC == kPlain ? nref : SC == kBiased ? bias[nb] : f32x16{};
+    for (int nb = 0; nb < NB; ++nb) sc[nb] = SC == kBiased ? bias[nb] : SC == kPlain && !OFF ? nref : f32x16{};
     // K reads kAhead MFMAs ahead of their use, an order that the scheduling barriers hold
     // (left to itself the compiler pairs each MFMA with its own read and a wait)
     constexpr int kAhead = 4;
@@ -517,7 +519,9 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     __builtin_amdgcn_sched_barrier(0);
     const int at = q0 + u / UPP;
     const int k0 = (LISTS ? own : at) * kPage + u % UPP * UNIT;
-    if constexpr (SC) {
+    if constexpr (SC == kPlain) {
+      off = -ref;
+    } else {
       // cap tanh(q.k / (cap sqrt d)) - slope (i - j)  (biased rows see no key past their own)
       const float dist0 = (float)(k0 + 4 * half - pos);  // j - i of offset 0
       const float base = (biased ? slope * dist0 : 0.f) - ref;
@@ -550,19 +554,37 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     // fp32 ones; or the nearest value, and the normaliser sums those, so that the rounding
     // cancels where one key dominates.
     bf16x8 pf[2 * NB], rest[2 * NB];
+    const float less = col >= 16 ? -1.f : 0.f;  // (TWICE)
     auto weights = [&]() {
       f32x16 p[NB];
 #pragma unroll
       for (int q = 0; q < 16; ++q)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
-          p[nb][q] = fast_exp2(SC == kBiased ? __builtin_fmaf(c2, sc[nb][q], off) : c2 * sc[nb][q]);
+          p[nb][q] = fast_exp2(OFF ? __builtin_fmaf(c2, sc[nb][q], off) : c2 * sc[nb][q]);
+      float ta = 0.f, tb = 0.f;
+      if constexpr (TWICE) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int q = 0; q < 16; q += 2) {
+            const float a0 = p[nb][q], a1 = p[nb][q + 1];
+            ta += a0;
+            tb += a1;
+            const uint32_t near = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a0, a1}, bf16x2));
+            const f32x2 x = {__builtin_fmaf(__uint_as_float(near << 16), less, a0),
+                             __builtin_fmaf(__uint_as_float(near & 0xffff0000u), less, a1)};
+            const bf16x2 y = __builtin_convertvector(x, bf16x2);
+            pf[2 * nb + q / 8][q % 8] = y[0];
+            pf[2 * nb + q / 8][q % 8 + 1] = y[1];
+          }
+        return ta + tb;
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         pf[2 * nb] = __builtin_convertvector(p[nb].lo, bf16x8);
         pf[2 * nb + 1] = __builtin_convertvector(p[nb].hi, bf16x8);
       }
-      float ta = 0.f, tb = 0.f;
       if constexpr (SH::TWO_PARTS) {
         auto left = [](f32x8 x, bf16x8 y) { return __builtin_convertvector(x - __builtin_convertvector(y, f32x8), bf16x8); };
 #pragma unroll
@@ -597,7 +619,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int q = 0; q < 16; ++q) mx = fmaxf(mx, sc[nb][q]);
-      if constexpr (SC == kBiased) mx += off * inv_c2;
+      if constexpr (OFF) mx += off * inv_c2;
       const auto pr = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = c2 * fmaxf(__uint_as_float(pr[0]), __uint_as_float(pr[1]));
       // a lane without a reference takes the unit's maximum (if it sees a key); one with a
@@ -613,7 +635,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
         const float dr = dm * inv_c2;
-        if constexpr (SC == kBiased) {
+        if constexpr (OFF) {
           off -= dm;
         } else {
 #pragma unroll
@@ -639,7 +661,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
         __builtin_amdgcn_sched_barrier(0);
         const bf16x8 vf = values_of((uint32_t)vc[i % kAhead][0], (uint32_t)vc[i % kAhead][1], v_scale);
         o[i % MB] = mfma32(vf, pf[i / MB], o[i % MB]);
-        if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf, rest[i / MB], o[i % MB]);
+        if constexpr (SH::TWO_PARTS && !TWICE) o[i % MB] = mfma32(vf, rest[i / MB], o[i % MB]);
         if (i + kAhead < kSums) vc[i % kAhead] = vcodes(i + kAhead);
       }
     } else {
@@ -654,7 +676,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       for (int i = 0; i < kSums; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         o[i % MB] = mfma32(vf[i % kAhead], pf[i / MB], o[i % MB]);
-        if constexpr (SH::TWO_PARTS) o[i % MB] = mfma32(vf[i % kAhead], rest[i / MB], o[i % MB]);
+        if constexpr (SH::TWO_PARTS && !TWICE) o[i % MB] = mfma32(vf[i % kAhead], rest[i / MB], o[i % MB]);
         if (i + kAhead < kSums) vf[i % kAhead] = vfrag(i + kAhead);
       }
     }
@@ -666,8 +688,18 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
   // with one barrier per unit, which also says that the unit before it is read.  Page
   // ids are read one unit ahead of the transfers that need them.
   static_assert(DEPTH == 2, "the loop is unrolled by stage");
-  auto scales_of = [&](int it) -> int { return E8 ? exps[place_of(it)] : 0; };
-  int now = dma(0, 0, page_of(0)), next = page_of(1), scales = scales_of(0);
+  int now = dma(0, 0, page_of(0)), next = page_of(1);
+  // (of codes) The exponents of a page's scales, keys' and values', by scalar loads while its unit is
+  // under way: nothing waits for them ahead of the first transfer, and no LDS is needed (64 single
+  // tokens over up to 8192 keys 143 to 145 us; with the ids in LDS, ahead of it or behind, 146 to 148).
+  const int g_s = __builtin_amdgcn_readfirstlane(g);
+  auto scales_of = [&](int e) -> uint32_t {
+    if constexpr (!E8) return 0;
+    const int64_t i = (int64_t)max(e, 0) * a.Hkv + g_s;
+    auto exponent = [&](const float* s) { return *(const __attribute__((address_space(4))) uint32_t*)(uint64_t)(s + i) >> 23 & 255u; };
+    return exponent(a.k_scales) | exponent(a.v_scales) << 8;
+  };
+  uint32_t scales = scales_of(now);
   auto step = [&](int it, auto stage) {
     constexpr int kOther = 1 - decltype(stage)::value;
     int after;
@@ -683,7 +715,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       after = dma(it + 1, kOther, next);
     }
     next = page_of(it + 2);
-    const int scales_next = scales_of(it + 1);
+    const uint32_t scales_next = scales_of(after);
     if (now >= 0) compute(it, stage, scales);
     now = after;
     scales = scales_next;
@@ -727,7 +759,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
         if (mb % KS != ks) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const f32x4 x = xo[(((rt * KS + w) * MB + mb) * 4 + q) * 64 + lane];
+          const f32x4* const part = xo + (((rt * KS + w) * MB + mb) * 4 + q) * 64;
+          const f32x4 x = TWICE ? part[lane] + part[lane ^ 16] : part[lane];
 #pragma unroll
           for (int z = 0; z < 4; ++z) o[mb][4 * q + z] += f * x[z];
         }
@@ -741,7 +774,8 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
     l = __uint_as_float(pr[0]) + __uint_as_float(pr[1]);
   }
   const int64_t orow = t * a.Hq + h;
-  if (direct && r < n_rows) {
+  const bool writes = r < n_rows && (!TWICE || col < 16);
+  if (direct && writes) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -754,7 +788,7 @@ __global__ __launch_bounds__((64 * Shape<D, RT, E8>::NW), (Shape<D, RT, E8>::WAV
       }
     }
     if (a.lse && ks == 0 && half == 0) a.lse[orow] = l > 0.f ? (ref + __log2f(l)) * 0.6931471805599453f : -INFINITY;
-  } else if (r < n_rows) {
+  } else if (writes) {
     // A workgroup cuts at most the first and the last of its segments: place 1 holds one
     // that begins with its rows' first page, place 0 one that does not.
     const int64_t prow = (int64_t)(2 * w + (p0 == 0 ? 1 : 0)) * (RT * 32) + rt * 32 + col;
@@ -873,14 +907,21 @@ namespace {
 template <bool E8, int SC>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.n_wgs);
-#define DA_PAGED(DD, RT, LS)                                                                       \
-  hipLaunchKernelGGL((paged_attn_kernel<DD, RT, LS, E8, SC>), grid, dim3(64 * Shape<DD, RT, E8>::NW), \
+  // Rows twice in a tile, of codes, where instructions count beside HBM: with keys and values that stay in
+  // the L2, 64 single tokens over 5120 keys take 87 us with rows twice, 99 with two products (and 77 where
+  // the registers hold the outputs in place), of which HBM alone takes 122.  Of bf16 HBM hides them.
+  const bool twice = E8 && (int64_t)(a.lists ? 1 : a.N) * a.G <= 16;
+#define DA_PAGED(DD, RT, LS, TW)                                                                   \
+  hipLaunchKernelGGL((paged_attn_kernel<DD, RT, LS, E8, SC, TW>), grid, dim3(64 * Shape<DD, RT, E8>::NW), \
                      (Shape<DD, RT, E8>::ldsBytes), s, a)
 #define DA_PAGED_RT(DD, LS)                                                                        \
   switch (a.row_tiles) {                                                                           \
-    case 1: DA_PAGED(DD, 1, LS); break;                                                            \
-    case 2: DA_PAGED(DD, 2, LS); break;                                                            \
-    default: DA_PAGED(DD, 4, LS); break;                                                           \
+    case 1:                                                                                        \
+      if (twice) DA_PAGED(DD, 1, LS, E8);                                                          \
+      else DA_PAGED(DD, 1, LS, false);                                                             \
+      break;                                                                                       \
+    case 2: DA_PAGED(DD, 2, LS, false); break;                                                     \
+    default: DA_PAGED(DD, 4, LS, false); break;                                                    \
   }
   if constexpr (SC == kPlain) {
     if (a.lists) {
@@ -894,7 +935,7 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   }
   if (a.d == 128) {
     if (a.row_tiles == 8)
-      DA_PAGED(128, 8, false);
+      DA_PAGED(128, 8, false, false);
     else
       DA_PAGED_RT(128, false)
   } else {
