@@ -626,8 +626,9 @@ da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void*
  *   the m rows of sequence b is token first[b] + i (first NULL: 0); rows of tokens that the
  *   slot does not hold are left as they are.
  * da_page8_summary: as da_page_summary, of the values.
- * append and read take one workgroup of 256 threads per sequence, page touched (up to
- * (max_seqlen + 62) / 64 + 1), layer, keys or values and kv head: more than 2^24 - 1 is DA_ERR_SHAPE.
+ * append and read are refused (DA_ERR_SHAPE) where B * layers * 2 times Hkv * ((max_seqlen + 62) / 64 + 1),
+ * the pages of a sequence that may be touched, or times ceil(max_seqlen * Hkv * d / 4096), is more than
+ * 2^24 - 1, or max_seqlen * Hkv * d / 16 more than 2^31 - 1.
  */
 da_status da_pages8_resize(void* k_pages, void* v_pages, float* k_scales, float* v_scales,
                            int layers, int Hkv, int d, int32_t* table, int32_t* lens,

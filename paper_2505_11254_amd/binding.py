@@ -557,12 +557,12 @@ class _On:
         with torch.cuda.stream(self.stream):
             return torch.full((n,), value, dtype=dtype, device=self.dev)
 
-    def like(self, t, shape=None):
-        """A new tensor of t's type (and shape); t lies on the device (cheaper than `empty`)."""
+    def like(self, t, shape=None, dtype=None):
+        """A new tensor of t's type (and shape) or another; t lies on the device (cheaper than `empty`)."""
         if self.stream is None:
-            return torch.empty_like(t) if shape is None else t.new_empty(shape)
+            return torch.empty_like(t) if shape is None else t.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(self.stream):
-            return torch.empty_like(t) if shape is None else t.new_empty(shape)
+            return torch.empty_like(t) if shape is None else t.new_empty(shape, dtype=dtype)
 
     def workspace(self, given, nbytes):
         """(tensor, address, size) of the caller's workspace, or of one that lasts for this call."""
@@ -615,11 +615,14 @@ def _pages(k_pages, v_pages, layered=False):
 
 
 def _pages8(k_pages, v_pages, k_scales, v_scales, layered=False):
-    """The same of pages of codes and their scales (v_pages and v_scales may be None)."""
+    """The same of pages of codes and their scales."""
     dev, shape = k_pages.device, k_pages.shape
-    for name, t, dtype in (("k_pages", k_pages, torch.float8_e4m3fn), ("v_pages", v_pages, torch.float8_e4m3fn),
-                           ("k_scales", k_scales, torch.float32), ("v_scales", v_scales, torch.float32)):
-        if t is not None and (t.dtype is not dtype or t.device != dev or not t.is_contiguous()):
+    f8, f32 = torch.float8_e4m3fn, torch.float32
+    if not (k_pages.dtype is f8 and v_pages.dtype is f8 and k_scales.dtype is f32 and v_scales.dtype is f32
+            and v_pages.device == dev and k_scales.device == dev and v_scales.device == dev and k_pages.is_contiguous()
+            and v_pages.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+        for name, t, dtype in (("k_pages", k_pages, f8), ("v_pages", v_pages, f8), ("k_scales", k_scales, f32),
+                               ("v_scales", v_scales, f32)):
             _on_device(name, t, dev, dtype)
     n = len(shape)
     if n != 4 and not (layered and n == 5):
@@ -628,9 +631,9 @@ def _pages8(k_pages, v_pages, k_scales, v_scales, layered=False):
     if tokens != PAGE_TOKENS:
         raise ValueError(f"pages must hold {PAGE_TOKENS} tokens")
     heads = shape[:-2]
-    if v_pages is not None and v_pages.shape != shape:
+    if v_pages.shape != shape:
         raise ValueError("k_pages and v_pages must have the same shape")
-    if k_scales.shape != heads or (v_scales is not None and v_scales.shape != heads):
+    if k_scales.shape != heads or v_scales.shape != heads:
         raise ValueError(f"k_scales and v_scales must be {list(heads)}")
     return dev, (shape[0] if n == 5 else 1), P, Hkv, d
 
@@ -751,13 +754,13 @@ def _rows8(name, k, v, cache, table, lens, T, slots, B, cu_seqlens, max_seqlen, 
     S, M = _table(table, lens, dev)
     shape = (T, Hkv, d) if len(cache[0].shape) == 4 else (layers, T, Hkv, d)
     if k is None:
-        k = on.empty(shape, torch.bfloat16)
+        k = on.like(table, shape, torch.bfloat16)
     if v is None:
         v = on.like(k)
-    for what, t in (("k", k), ("v", v)):
-        _halves(what, t, dev)
-        if t.shape != shape:
-            raise ValueError(f"{what} must be {list(shape)} (got {list(t.shape)})")
+    _halves("k", k, dev)
+    _halves("v", v, dev)
+    if k.shape != shape or v.shape != shape:
+        raise ValueError(f"k and v must be {list(shape)} (got {list(k.shape)} and {list(v.shape)})")
     B, N = _new_rows(T, B, cu_seqlens, max_seqlen, dev)
     if ints is not None:
         _ints(*ints, dev, (B,))
@@ -1027,7 +1030,7 @@ def page_summary(k_pages, table, lens, codes, scales, *, slots=None, first=None,
 
 def page8_summary(k_pages, k_scales, table, lens, codes, scales, *, slots=None, first=None, max_new=None, stream=None):
     """page_summary of a cache in 8 bits (da_page8_summary)."""
-    dev, _, P, Hkv, d = _pages8(k_pages, None, k_scales, None)
+    dev, _, P, Hkv, d = _pages8(k_pages, k_pages, k_scales, k_scales)
     on = _On(dev, stream)
     S, M = _table(table, lens, dev)
     _summaries(codes, scales, P, Hkv, d, dev)

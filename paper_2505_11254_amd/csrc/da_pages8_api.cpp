@@ -25,9 +25,15 @@ da_status check_rows8(const Table& t, const Pages8& p, const void* k, const void
   if (st != DA_OK) return st;
   if (B < 1 || N < 1 || T < 0 || (!slots && B > t.S)) return DA_ERR_SHAPE;
   if (!cu && (int64_t)B * N != T) return DA_ERR_SHAPE;
-  // a workgroup for each page, layer, keys or values, and kv head
-  const double wgs = (double)B * pages8_parts(N) * p.layers * 2 * p.Hkv;
-  if (wgs > (double)(UINT32_MAX / 256)) return DA_ERR_SHAPE;
+  // Pieces of 16 values of a sequence and layer are counted in 32 bits, and a launch has less than 2^32
+  // threads: a read's one for each of them, an append's 256 for each page that may be touched, layer, keys
+  // or values, and kv head.
+  const int64_t row = (int64_t)p.Hkv * (p.d / 16);
+  if (row > INT32_MAX / N) return DA_ERR_SHAPE;
+  const double most = (double)(UINT32_MAX / 256);
+  const double of_pages = (double)B * pages8_parts(N) * p.layers * 2 * p.Hkv;
+  const double of_pieces = (double)B * ((N * row + 255) / 256) * p.layers * 2;
+  if (of_pages > most || of_pieces > most) return DA_ERR_SHAPE;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cu, 4) || !aligned(ints, 4))
     return DA_ERR_ALIGN;
   return check_device();
