@@ -307,3 +307,35 @@ def test_codes_of_the_host_are_e4m3():
     x = x[torch.isfinite(x) & (x.abs() <= 448)]
     assert torch.equal(codes(x), x.to(torch.float8_e4m3fn).view(torch.uint8))
     assert torch.equal(VALUES[:127].float(), torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float())
+
+
+def test_pages_past_four_gigabytes():
+    """Offsets inside the pages past 32 bits: written, read back, attended to, compacted."""
+    from paper_2505_11254_amd import binding
+    P, Hkv, d = 66_000, 8, 128
+    k8, v8 = (torch.zeros((P, Hkv, PAGE, d), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = (torch.ones((P, Hkv), device="cuda") for _ in range(2))
+    c = Cache8(1, 4, Hkv, d, 1, 3, seed=2)
+    put(c, 0, 150, [0, 1, 2])
+    far = [P - 1, P - 3, P - 2]
+    table, lens = i32([far]), i32([150])
+    refs = torch.zeros(P, dtype=torch.int32, device="cuda")
+    refs[far] = 1
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn((1, 150, Hkv, d), generator=g).to(torch.bfloat16) for _ in range(2))
+    cache = (k8, v8, ks, vs, table, lens)
+    binding.pages8_append(k[0].cuda(), v[0].cuda(), *cache)
+    c.append8([0], [0, 150], k, v)
+    q = torch.randn((1, Hkv, d), generator=g).to(torch.bfloat16)
+    out = binding.tree_attn_paged8(q.cuda(), *cache).float().cpu().double()
+    for h in range(Hkv):
+        kk, vv = (c.rows(x, 0, 0, h, 0, 150) for x in "kv")
+        want, _ = attend(q[:, h], kk, vv, torch.ones((1, 150), dtype=torch.bool))
+        assert (out[:, h] - want).abs().max() <= 2.0 ** -7 * max(1.0, float(vv.abs().max()))
+    got = binding.pages8_compact(*cache, refs, i32([0]), i32([10]), i32([3, 77, 139]), i32([0, 3]))
+    assert got[:, 0].cpu().tolist() == c.compact8([0], [10], [[3, 77, 139]]) == [3]
+    rk, rv = binding.pages8_read(*cache, 13)
+    for name, x in (("k", rk), ("v", rv)):
+        for h in range(Hkv):
+            assert torch.equal(x[:, h].float().cpu().double(), c.rows(name, 0, 0, h, 0, 13))
+    assert (k8.view(torch.uint8)[:P - 3] == 0).all()
