@@ -153,12 +153,13 @@ __device__ __forceinline__ i16x4 lds_read_tr(const uint16_t* p) {
 
 // Raw scores of NB blocks of 32 keys, capped, in base-2 units of the logits, and base added (see Cap).
 // Every instruction per score counts in the prefill kernels, whose vector instructions hide little behind
-// the matrix ones (capped Delta, 32K tokens, 32 heads: 1232 us plain, 1595 with an exponential and a reciprocal
-// for each score, 1558 with a degree of 9 throughout or with the shared reciprocal, 1481 so; the first block's
-// polynomial between the products of the second: no gain).  Where the wavefront has none past a limit, four or five at the full rate each, and half of one for the test.
-// Else tanh y = 1 - 2 / (1 + e^2y), four at a time: exponentials and reciprocals run at a quarter of that
-// rate, so four share the reciprocal of their denominators' product, whose factors are held below 2^31
-// (the tanh is 1 there to the last bit).
+// the matrix ones.  Delta, 32K tokens, 32 heads: 1232 us plain, 1481 capped; 1595 with an exponential and
+// a reciprocal for each score, 1558 with a degree of 9 throughout or with the shared reciprocal, and the
+// first block's polynomial between the products of the second: no gain.
+// Where the wavefront has none past a limit, four or five at the full rate each, and half of one for the
+// test.  Else tanh y = 1 - 2 / (1 + e^2y), four at a time: exponentials and reciprocals run at a quarter of
+// that rate, so four share the reciprocal of their denominators' product, whose factors are held below
+// 2^31 (the tanh is 1 there to the last bit).
 template <int NB>
 __device__ __forceinline__ void cap_scores(f32x16 (&s)[NB], const Cap& cap, float base) {
   float top = 0.f;

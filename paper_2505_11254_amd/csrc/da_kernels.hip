@@ -1543,7 +1543,7 @@ hipError_t launch_attn_as(const Args& a0, hipStream_t s, int64_t nblocks) {
   prepare_attn<MODE>(a, nblocks);
   const int pre = MODE == kSparse ? pre_bytes(a) : 0;
 #define DA_ATTN(DD, W)                                                                          \
-  hipLaunchKernelGGL((attn_kernel<DD, MODE, W, SC>), dim3((unsigned)nblocks), dim3(64 * W),         \
+  hipLaunchKernelGGL((attn_kernel<DD, MODE, W, SC>), dim3((unsigned)nblocks), dim3(64 * W),     \
                      (lds_bytes<DD, MODE, W>(pre)), s, a)
   const int waves = a.hpw * a.ppw;
   if (a.d == 128) {
@@ -1665,14 +1665,14 @@ hipError_t launch_sparse(const Args& a0, hipStream_t s) {
   prepare_attn<kSparse>(as, ns);
   const dim3 g((unsigned)(nr8 + ns));
   const int pre = pre_bytes(as);
-#define DA_PAIR_AS(DD, W, SC)                                                                      \
-  hipLaunchKernelGGL((attn_pair_kernel<DD, W, SC>), g, dim3(64 * W), (lds_bytes<DD, kSparse, W>(pre)), \
-                     s, ar, as, (uint32_t)nr, (uint32_t)nr8)
-#define DA_PAIR(DD, W)              \
-  do {                              \
-    if (as.scored == kPlain) DA_PAIR_AS(DD, W, kPlain); \
-    else if (as.scored == kBiased) DA_PAIR_AS(DD, W, kBiased); \
-    else DA_PAIR_AS(DD, W, kCapped); \
+#define DA_PAIR_AS(DD, W, SC)                                                                   \
+  hipLaunchKernelGGL((attn_pair_kernel<DD, W, SC>), g, dim3(64 * W),                            \
+                     (lds_bytes<DD, kSparse, W>(pre)), s, ar, as, (uint32_t)nr, (uint32_t)nr8)
+#define DA_PAIR(DD, W)                                                                          \
+  do {                                                                                          \
+    if (as.scored == kPlain) DA_PAIR_AS(DD, W, kPlain);                                         \
+    else if (as.scored == kBiased) DA_PAIR_AS(DD, W, kBiased);                                  \
+    else DA_PAIR_AS(DD, W, kCapped);                                                            \
   } while (0)
   if (as.d == 128) {
     if (waves == 8) DA_PAIR(128, 8);
