@@ -235,8 +235,9 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   const int R1 = min(R0 + rows_per_block, n_rows);
   const int bpos_lo = row_pos<MODE>(R0, nA, Lc, a.gamma);
   const int bpos_hi = row_pos<MODE>(R1 - 1, nA, Lc, a.gamma);
-  // the last key that rows short of it see as well (-1: none)
-  const int see = SC && MODE == kDense && a.prefix ? min(a.prefix[b], L) - 1 : -1;
+  // the last key that rows short of it see as well (-1: none); any int stands for a prefix, so it is held
+  // to [0, L] before 1 is taken off
+  const int see = SC && MODE == kDense && a.prefix ? max(min(a.prefix[b], L), 0) - 1 : -1;
 
   // ---- key tiles the block visits: [ta0, ta1) then [tb0, tb1)
   int ta0 = 0, ta1 = 0, tb0 = 0, tb1 = 0;
