@@ -262,7 +262,8 @@ da_status dense_causal_attn_prefill_varlen(const void* q, const void* k, const v
  * The same attentions under changed scores, for models that cap them or bias them by distance:
  *   s_ij = q_i.k_j / sqrt d,  s' = cap tanh(s / cap) if cap > 0, else s,
  *   weight_ij = exp(s'_ij - slopes[h] |i - j|) over the keys that row i sees.
- * cap: 0 (none), or from 2^-10 to 2^10; a capped score is off by up to cap 2^-20.
+ * cap: 0 (none), or from 2^-10 to 2^10; a capped score is off by up to cap 2^-20.  A score that is NaN
+ *   stays NaN, and so does the row that sees its key, as without a cap.
  * slopes: fp32 [Hq] on the device, finite, or NULL (none); a biased score is off by up to |slope| 2^-11.
  * prefix (dense rows only): int32 [B] on the device, or NULL: rows of sequence b see its first
  *   prefix[b] tokens (as many as there are; none below 1) whole, and the others up to themselves.

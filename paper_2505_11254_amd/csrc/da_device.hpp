@@ -153,13 +153,14 @@ __device__ __forceinline__ i16x4 lds_read_tr(const uint16_t* p) {
 
 // Raw scores of NB blocks of 32 keys, capped, in base-2 units of the logits, and base added (see Cap).
 // Every instruction per score counts in the prefill kernels, whose vector instructions hide little behind
-// the matrix ones.  Delta, 32K tokens, 32 heads: 1232 us plain, 1481 capped; 1595 with an exponential and
-// a reciprocal for each score, 1558 with a degree of 9 throughout or with the shared reciprocal, and the
-// first block's polynomial between the products of the second: no gain.
+// the matrix ones.  Delta, 32K tokens, 32 heads: 1232 us plain, 1435 capped (1558 with a degree of 9
+// throughout), 1539 where every score is wide; the first block's polynomial between the products of the
+// second: no gain.
 // Where the wavefront has none past a limit, four or five at the full rate each, and half of one for the
-// test.  Else tanh y = 1 - 2 / (1 + e^2y), four at a time: exponentials and reciprocals run at a quarter of
-// that rate, so four share the reciprocal of their denominators' product, whose factors are held below
-// 2^31 (the tanh is 1 there to the last bit).
+// test.  Else tanh y = 1 - 2 / (1 + e^2y), each score by itself: past the range of e^2y that is -1 or 1, and a
+// NaN stays one, as it does in the polynomials, without reaching the scores of other keys.  (One reciprocal
+// for four scores needs e^2y held below 2^31 and 13 to 27 registers more, and took longer: the call above with
+// wide scores 1585 us against 1539, dense rows of 8192 tokens 633 against 614.)
 template <int NB>
 __device__ __forceinline__ void cap_scores(f32x16 (&s)[NB], const Cap& cap, float base) {
   float top = 0.f;
@@ -191,19 +192,11 @@ __device__ __forceinline__ void cap_scores(f32x16 (&s)[NB], const Cap& cap, floa
     return;
   }
   const float c = cap.in, m = -2.f * cap.cap2, one = cap.cap2 + base;
-  auto denom = [&](float x) { return 1.f + fast_exp2(fminf(c * x, 30.f)); };
 #pragma unroll
-  for (int q = 0; q < 16; q += 4)
+  for (int q = 0; q < 16; ++q)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const float e0 = denom(s[nb][q]), e1 = denom(s[nb][q + 1]), e2 = denom(s[nb][q + 2]), e3 = denom(s[nb][q + 3]);
-      const float a = e0 * e1, b = e2 * e3, r = m * __builtin_amdgcn_rcpf(a * b);
-      const float ra = r * b, rb = r * a;
-      s[nb][q] = __builtin_fmaf(ra, e1, one);
-      s[nb][q + 1] = __builtin_fmaf(ra, e0, one);
-      s[nb][q + 2] = __builtin_fmaf(rb, e3, one);
-      s[nb][q + 3] = __builtin_fmaf(rb, e2, one);
-    }
+    for (int nb = 0; nb < NB; ++nb)
+      s[nb][q] = __builtin_fmaf(m, __builtin_amdgcn_rcpf(1.f + fast_exp2(c * s[nb][q])), one);
 }
 
 }  // namespace

@@ -5,8 +5,11 @@ from __future__ import annotations
 import pytest
 import torch
 
-from scored import slopes_of
-from test_gpu_scored import check_dense, i32, inputs
+from paged_sim import PAGE
+from pages8_sim import NAN
+from scored import HALF, attend, slopes_of, tolerance
+from test_gpu_paged8_attn import Case8, call, upto
+from test_gpu_scored import bias_of, check_dense, i32, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +29,62 @@ def test_every_int_is_a_prefix(d, cap, biased):
                                             slopes=slopes.cuda() if biased else None, prefix=i32(prefix),
                                             cu_seqlens=i32(cu), max_seqlen=130)
     check_dense(out, q, k, v, cu, cap, slopes, prefix)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 2, 64), (8, 2, 128)])
+@pytest.mark.parametrize("cap,std,biased", [(50.0, 0.5, False), (2.0, 4.0, False), (1.0, 30.0, False), (1.0, 30.0, True),
+                                            (0.0, 4.0, True)])
+@pytest.mark.parametrize("bad", [0, 37, 129])
+def test_rows_that_see_a_nan_key_are_nan_and_the_others_as_without_it(Hq, Hkv, d, cap, std, biased, bad):
+    """(the cap's three forms: small, wide and mixed scores)"""
+    from paper_2505_11254_amd import binding
+    n, window = 200, 50
+    q, k, v, cu = inputs((n,), Hq, Hkv, d, seed=bad + d, std=std)
+    slopes = slopes_of(Hq) if biased else None
+    broken = k.clone()
+    broken[bad, 1, 5] = float("nan")
+    kw = dict(cap=cap, slopes=slopes.cuda() if biased else None)
+    dev = [x.cuda() for x in (q, broken, v)]
+    i, top = torch.arange(n), float(v.double().abs().max())
+    causal = i <= i[:, None]
+    for out, vis in ((binding.dense_attn_prefill_scored(*dev, **kw), causal),
+                     (binding.sparse_attn_prefill_scored(*dev, window=window, n_sink=3, **kw),
+                      causal & ((i < 3) | (i[:, None] - i < window)))):
+        out = out.float().cpu().double()
+        for h in range(Hq):
+            g = h * Hkv // Hq
+            sees = vis[:, bad] if g == 1 else torch.zeros(n, dtype=torch.bool)
+            want, _, dev_, dl = attend(q[:, h], k[:, g], v[:, g], vis, cap, bias_of(slopes, h, n))
+            assert torch.isnan(out[sees, h]).all(), h
+            assert ((out[:, h] - want).abs() <= tolerance(want, dev_, dl, top))[~sees].all(), h
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,m", [(8, 2, 64, 1), (8, 2, 128, 1), (32, 8, 128, 3), (16, 2, 128, 12)])
+@pytest.mark.parametrize("cap,std", [(50.0, 0.5), (0.25, 20.0), (0.0, 2.0)])
+def test_a_nan_key_in_the_cache(eight, Hq, Hkv, d, m, cap, std):
+    """Of three sequences two have a broken key: one that all rows see, one that only the last row does."""
+    lens = [300, 300, 90 + m]
+    c = Case8(lens, [m] * 3, Hq, Hkv, d, seed=m + d, eight=eight, std=std)
+    bad = {1: 70, 2: 90 + m - 1}
+    for b, j in bad.items():
+        page = int(c.table[c.slots[b], j // PAGE])
+        if eight:
+            c.k8.view(torch.uint8)[page, 0, j % PAGE, 9] = NAN
+        else:
+            c.k[page, 0, j % PAGE, 9] = float("nan")
+    lse = torch.zeros((c.cu[-1], Hq), device="cuda")
+    out = call(c, lse=lse, cap=cap).float().cpu().double()
+    lse, G = lse.cpu().double(), Hq // Hkv
+    for b, n in enumerate(lens):
+        for g in range(Hkv):
+            k, v = c.keys(b, g)
+            k = torch.nan_to_num(k.double(), nan=0.0)
+            s = slice(c.cu[b], c.cu[b + 1])
+            vis = torch.stack([upto(c)(b, i, g) for i in range(m)])
+            sees = vis[:, bad[b]] if b in bad and g == 0 else torch.zeros(m, dtype=torch.bool)
+            for h in range(g * G, (g + 1) * G):
+                want, wlse, dev, dl = attend(c.q[s, h], k, v, vis, cap)
+                assert torch.isnan(out[s, h][sees]).all(), (b, h)
+                assert ((out[s, h] - want).abs() <= tolerance(want, dev, dl, float(v.double().abs().max())))[~sees].all()
+                assert ((lse[s, h] - wlse).abs() <= HALF * (1 + 2 ** -7) + dl)[~sees].all()
