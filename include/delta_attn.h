@@ -610,9 +610,12 @@ da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void*
  *   k_scales, v_scales  fp32 [P, Hkv] or [layers, P, Hkv]
  * the power of two that the codes of each page and kv head count in: value = code * scale,
  * which bf16 holds exactly.  A scale is 2^e with the least e, from -110 to 119, for which no value
- * of its page passes 448 * 2^e; codes are the nearest, ties to even, and so a value is off
- * by at most 2^-4 of itself, or 2^-10 of the scale if that is more.  Magnitudes past 448 * 2^119
- * count as that; what is not finite becomes NaN and does not count for the scale.
+ * of its page passes 448 * 2^e; codes are the nearest, ties to even, and so a value as it is
+ * written is off by at most 2^-4 of itself, or 2^-10 of the scale if that is more.  Where the scale of
+ * its page has grown since, that holds for values from 2^-6 of the scale on, and smaller ones, which are
+ * rounded again, are off by less than 2^-4 of themselves plus 2^-9 of the scale, however often it
+ * grew.  Magnitudes past 448 * 2^119 count as that; what is not finite becomes NaN and does not
+ * count for the scale.
  * Table, lens, refs, slots and requests are as above: da_pages_fork serves both kinds of cache.
  * The scales are what these calls leave there; a page that holds no token needs none.
  *

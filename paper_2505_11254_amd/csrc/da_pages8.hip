@@ -9,7 +9,9 @@
 // bf16 without rounding, and codes that have to count in a larger scale, because a later token
 // of the page needs it or because they move into another page, only shift their exponents:
 // nothing is lost until they fall below e4m3's normal range (2^-14 of the page's largest).
-// So the error of a cached value is its own rounding, 2^-4 of it at most, whatever came later.
+// So the error of a cached value is its own rounding, 2^-4 of it at most, whatever came later, while it
+// is 2^-6 of its scale or more.  Below, each growth rounds it to a multiple of 2^-9 of the new scale, by 2^-10
+// of it at most; a growth doubles the scale or more, so all of them together stay under 2^-9 of the last one.
 //
 // A workgroup takes the rows that one page and kv head has of the keys or of the values: it
 // alone writes them and their scale.  Bound by HBM where there are many, by a chain of reads
