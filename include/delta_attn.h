@@ -609,8 +609,10 @@ da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void*
  * (OCP "fn", a byte each) in the same layout, [P, Hkv, 64, d] or [layers, P, Hkv, 64, d], and
  *   k_scales, v_scales  fp32 [P, Hkv] or [layers, P, Hkv]
  * the power of two that the codes of each page and kv head count in: value = code * scale,
- * which bf16 holds exactly.  A scale is 2^e with the least e, from -110 to 119, for which no value
- * of its page passes 448 * 2^e; codes are the nearest, ties to even, and so a value as it is
+ * which bf16 holds exactly.  An append to a new page makes its scale the least 2^e, e from -110 to
+ * 119, for which no value passes 448 * 2^e; later ones raise it to that, and nothing lowers it while the
+ * page keeps tokens, not even that its largest ones leave (by a resize down or a compaction).
+ * Codes are the nearest, ties to even, and so a value as it is
  * written is off by at most 2^-4 of itself, or 2^-10 of the scale if that is more.  Where the scale of
  * its page has grown since, that holds for values from 2^-6 of the scale on, and smaller ones, which are
  * rounded again, are off by less than 2^-4 of themselves plus 2^-9 of the scale, however often it
@@ -625,7 +627,7 @@ da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void*
  *   older codes then count in the new one (exactly, as long as they stay above 2^-6 of it, the
  *   range in which e4m3 keeps its 4 bits; below they are rounded to multiples of 2^-9).
  * In a compaction a page that tokens move into gets the largest of the scales that its tokens
- *   had, and their codes count in that likewise.
+ *   had (those of their pages), and their codes count in that likewise.
  * da_pages8_read: the values of cached tokens as rows k, v [layers, T, Hkv, d] of bf16: row i of
  *   the m rows of sequence b is token first[b] + i (first NULL: 0); rows of tokens that the
  *   slot does not hold are left as they are.

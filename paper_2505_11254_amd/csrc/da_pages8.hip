@@ -4,7 +4,9 @@
 // A page holds e4m3 codes of 64 tokens for each kv head, keys and values apart, and for
 // each (page, kv head) a power of two 2^e that its codes count in:
 //   code = x 2^-e rounded to e4m3 (to nearest, ties to even), value = code 2^e
-//   e = the least with max |x| <= 448 2^e, held to [kLeastExp, kMostExp]
+//   e = the least with max |x| <= 448 2^e, held to [kLeastExp, kMostExp], over all tokens since the page was
+//       last begun, those among them that have left it too: to lower it would take a pass over the page
+//       and give back no bit that its codes have lost
 // A floating point code loses nothing by a scale that is only a power of two, its values are
 // bf16 without rounding, and codes that have to count in a larger scale, because a later token
 // of the page needs it or because they move into another page, only shift their exponents:

@@ -83,3 +83,34 @@ def test_scales_that_grow(Hkv, d, step):
         elif len(s.k) > 40:
             s.resize(len(s.k) - 7)
             s.check()
+
+
+@pytest.mark.parametrize("Hkv,d", [(2, 64), (1, 128)])
+@pytest.mark.parametrize("leave", ["resize", "compact"])
+def test_a_scale_stays_when_the_tokens_that_set_it_leave(Hkv, d, leave):
+    """A dropped draft of large values leaves its page's scale; a page begun anew gets its own."""
+    g = torch.Generator().manual_seed(d)
+    s = Slot(3, Hkv, d)
+    small, big = rows(g, 10, Hkv, d, 0), torch.full((1, Hkv, d), 448.0 * 2 ** 9, dtype=torch.bfloat16)
+    s.append(small, small)
+    page = int(s.table[0, 0])
+    first = s.ks[page].clone()
+    s.append(big, -big)
+    assert (s.ks[page] == 512.0).all() and (s.vs[page] == 512.0).all() and (first < 1.0).all()
+    if leave == "resize":
+        s.resize(10)
+    else:
+        s.compact(4, [0, 1, 2, 3, 4, 5])
+    s.check()
+    more = rows(g, 53, Hkv, d, 0)
+    s.append(more, more)
+    assert (s.ks[page] == 512.0).all() and (s.vs[page] == 512.0).all()
+    s.check()
+    more = rows(g, 20, Hkv, d, 0)
+    s.append(more, more)  # one ends the page, the others begin the next
+    assert (s.ks[int(s.table[0, 1])] < 1.0).all()
+    s.check()
+    s.resize(0)
+    s.append(small, small)
+    assert torch.equal(s.ks[int(s.table[0, 0])], first)
+    s.check()
