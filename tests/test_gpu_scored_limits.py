@@ -88,3 +88,24 @@ def test_a_nan_key_in_the_cache(eight, Hq, Hkv, d, m, cap, std):
                 assert torch.isnan(out[s, h][sees]).all(), (b, h)
                 assert ((out[s, h] - want).abs() <= tolerance(want, dev, dl, float(v.double().abs().max())))[~sees].all()
                 assert ((lse[s, h] - wlse).abs() <= HALF * (1 + 2 ** -7) + dl)[~sees].all()
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("slope", [-0.84, -0.0123, 0.0123, 3e-5])
+def test_biased_scores_of_far_keys(eight, slope):
+    """The log-sum-exp of a single token over 131075 keys: off by no more than its scores may be (the bound:
+    test_scored_error.py), and by its own steps in 32 bits, 2^-22 of it and of 1, with 2^-12 for the weights' sum (that
+    many keys have weight, in sums of some 2^11 terms a lane)."""
+    n, d = 131075, 64
+    c = Case8([n], [1], 4, 1, d, seed=8, eight=eight)
+    slopes = torch.full((4,), slope)
+    lse = torch.zeros((1, 4), device="cuda")
+    c.verify(call(c, lse=lse, slopes=slopes.cuda()), None, upto(c), 0.0, slopes)
+    k, v = c.keys(0, 0)
+    bias = -float(slopes[0]) * torch.arange(n - 1, -1, -1).double()[None]
+    for h in range(4):
+        _, want, _, _ = attend(c.q[:, h], k, v, torch.ones((1, n), dtype=torch.bool), 0.0, bias)
+        products = d * 2.0 ** -24 * float((c.q[0, h].double().abs() @ k.double().abs().T).max()) / d ** 0.5 + 2.0 ** -20
+        top = float((c.q[0, h].double() @ k.double().T / d ** 0.5 + bias).abs().max())
+        bound = 2.0 ** -10 * abs(slope) + 2.0 ** -21 * (float(bias.abs().max()) + top) + products
+        assert abs(float(lse[0, h]) - float(want)) <= bound + 2.0 ** -22 * (abs(float(want)) + 1) + 2.0 ** -12
