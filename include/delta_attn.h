@@ -264,7 +264,7 @@ da_status dense_causal_attn_prefill_varlen(const void* q, const void* k, const v
  *   weight_ij = exp(s'_ij - slopes[h] |i - j|) over the keys that row i sees.
  * cap: 0 (none), or from 2^-10 to 2^10; a capped score is off by up to cap 2^-20.  A score that is NaN
  *   stays NaN, and so does the row that sees its key, as without a cap.
- * slopes: fp32 [Hq] on the device, finite, or NULL (none); a bias adds to a score's error up to
+ * slopes: fp32 [Hq] on the device, from -2^10 to 2^10, or NULL (none); a bias adds to a score's error up to
  *   |slope| 2^-10, and 2^-21 of |slope (i - j)| and of the row's largest score.
  * prefix (dense rows only): int32 [B] on the device, or NULL: rows of sequence b see its first
  *   prefix[b] tokens (as many as there are; none below 1) whole, and the others up to themselves.

@@ -90,6 +90,41 @@ def test_a_nan_key_in_the_cache(eight, Hq, Hkv, d, m, cap, std):
                 assert ((lse[s, h] - wlse).abs() <= HALF * (1 + 2 ** -7) + dl)[~sees].all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("slope", [1024.0, -1024.0])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_the_steepest_slopes(d, slope, cap):
+    """One key has all the weight: the nearest, or the farthest that a row sees."""
+    from paper_2505_11254_amd import binding
+    lens, Hq = (700, 0, 1, 65), 4
+    q, k, v, cu = inputs(lens, Hq, 2, d, seed=d)
+    slopes = torch.full((Hq,), slope)
+    dev = [x.cuda() for x in (q, k, v)]
+    kw = dict(cap=cap, slopes=slopes.cuda(), cu_seqlens=i32(cu), max_seqlen=700)
+    for prefix in (None, (130, 5, 1, 64)):
+        out = binding.dense_attn_prefill_scored(*dev, prefix=i32(prefix) if prefix else None, **kw)
+        check_dense(out, q, k, v, cu, cap, slopes, prefix)
+    # (sinks and window: the first key is among those seen; the correction's three attentions agree)
+    for out in (binding.sparse_attn_prefill_scored(*dev, window=100, n_sink=2, **kw),
+                binding.delta_attn_prefill_scored(*dev, window=100, n_sink=2, gamma=32, **kw)):
+        out = out.float().cpu()
+        for b in range(len(lens)):
+            rows = torch.arange(cu[b], cu[b + 1]) if slope > 0 else torch.full((lens[b],), cu[b])
+            for h in range(Hq):
+                want = v[rows, h // 2].float()
+                assert ((out[cu[b]:cu[b + 1], h] - want).abs() <= HALF * 2 * want.abs()).all()
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,m", [(8, 2, 64, 1), (8, 2, 128, 1), (32, 8, 128, 3), (16, 2, 128, 12)])
+@pytest.mark.parametrize("slope,cap", [(1024.0, 0.0), (-1024.0, 0.0), (1024.0, 20.0), (-1024.0, 20.0)])
+def test_the_steepest_slopes_over_the_cache(eight, Hq, Hkv, d, m, slope, cap):
+    c = Case8([300, 64 + m, 5000, m], [m] * 4, Hq, Hkv, d, seed=m + d, eight=eight)
+    slopes = torch.full((Hq,), slope)
+    lse = torch.zeros((c.cu[-1], Hq), device="cuda")
+    c.verify(call(c, lse=lse, cap=cap, slopes=slopes.cuda()), lse, upto(c), cap, slopes)
+
+
 @pytest.mark.parametrize("eight", [True, False])
 @pytest.mark.parametrize("slope", [-0.84, -0.0123, 0.0123, 3e-5])
 def test_biased_scores_of_far_keys(eight, slope):
