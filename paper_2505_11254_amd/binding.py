@@ -59,17 +59,6 @@ SIGNATURES = {
     "da_page8_summary": "ppiippiiippiippp",
     "tree_attn_paged8": "pppppppppiiippiiiiiipifppzp",
     "selected_attn_paged8": "pppppppppiiippiiiiipipzp",
-    "dense_attn_prefill_scored": "pppppiiiiifppp",
-    "sparse_attn_prefill_scored": "pppppiiiiiiifpp",
-    "delta_attn_prefill_scored": "pppppiiiiiiiifppzp",
-    "tree_attn_paged_scored": "pppppppiiippiiiiiipifppzp",
-    "da_pages8_resize": "ppppiiipppiiippipp",
-    "da_pages8_append": "pplppppiiippiiippiipp",
-    "da_pages8_compact": "ppppiiipppiiippplpipp",
-    "da_pages8_read": "pplppppiiippiiippiipp",
-    "da_page8_summary": "ppiippiiippiippp",
-    "tree_attn_paged8": "pppppppppiiippiiiiiipifppzp",
-    "selected_attn_paged8": "pppppppppiiippiiiiipipzp",
 }
 
 
