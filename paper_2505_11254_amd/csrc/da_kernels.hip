@@ -427,6 +427,8 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
   // error 0.00246, as in one chunk, in place of 0.00296; 4021 tokens, window 2048
   // 0.00245, 0.00274 in two long chunks).  It costs the keys of one more tile per
   // workgroup, 0-1 % of a whole call.
+  // Rows with slopes, which begin with their nearest tile instead, have whole numbers for
+  // references in every chunk and in the sparse rows, so that they differ likewise.
   const bool split = MODE == kDenseRows && a.split_ref && c > 0 && !back;
   float ref0 = 0.f;
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -595,6 +597,7 @@ __device__ __forceinline__ void attn_body(const Args& a, uint32_t bid, uint32_t 
       if (__any(grow)) {
         float up = mx;
         if (split) up = has_ref ? ceilf(mx) : ref0 + ceilf(mx - ref0);
+        if (SC != kPlain && back) up = ceilf(mx);
         float dm = has_ref ? fmaxf(up, 0.f) : (seen ? up : 0.f);
         if constexpr (SC) dm = (ref + dm) - ref;  // (a bias may be large: what the sum rounds off counts)
         const float alpha = has_ref ? fast_exp2(-dm) : 0.f;  // l and O are still zero without one
