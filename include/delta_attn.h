@@ -593,8 +593,8 @@ da_status selected_attn_paged(const void* q, const void* k_pages, const void* v_
 
 /*
  * As tree_attn_paged, under the changed scores of dense_attn_prefill_scored (lse is of those).
- * The distance is that of the tokens' places, which a tree of drafts does not tell: slopes with
- * a mask give DA_ERR_PARAM.
+ * The distance is that of the tokens' places in the cache, which in a tree of drafts is not that
+ * along a path: slopes with a mask give DA_ERR_PARAM.
  */
 da_status tree_attn_paged_scored(const void* q, const void* k_pages, const void* v_pages,
                                  void* out, float* lse, const int32_t* table, const int32_t* lens,

@@ -128,7 +128,7 @@ da_status paged_attn(PagedArgs a, int n_list, float cap, void* workspace, size_t
   st = check_rows(a.B, a.N, a.Hq, a.Hkv, a.d);
   if (st != DA_OK) return st;
   if (!a.slots && a.B > a.S) return DA_ERR_SHAPE;
-  // (the places of a tree's drafts do not tell their distances)
+  // (in a tree of drafts the distance of two places is not that along a path)
   if (!cap_ok(cap) || (a.slopes && a.mask)) return DA_ERR_PARAM;
   if (!aligned(a.slopes, 4)) return DA_ERR_ALIGN;
   if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.out, 16) ||
