@@ -372,7 +372,7 @@ def dense_causal_attn_prefill(q, k, v, *, B=None, cu_seqlens=None, max_seqlen=No
 
 
 # Attention under changed scores, cap tanh(q.k / sqrt d / cap) - slopes[h] |i - j| (see
-# include/delta_attn.h).  ``cap`` 0: none; ``slopes``: fp32 [Hq] on the GPU, None: none.
+# include/delta_attn.h).  ``cap`` 0: none; ``slopes``: fp32 [Hq] on the GPU, from -2^10 to 2^10, None: none.
 
 def _slopes(slopes, Hq, dev):
     if slopes is None:

@@ -28,7 +28,8 @@ def compile_flags() -> list:
     return [
         f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
         "-Wall", "-Wno-unused-function",
-        # no kernel produces or consumes NaN: lets max() skip NaN quieting
+        # no kernel's decisions depend on NaN, which passes through their arithmetic: lets max() skip
+        # NaN quieting
         "-fno-honor-nans",
         # never let the compiler form packed fp32 VALU ops (v_pk_*_f32)
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

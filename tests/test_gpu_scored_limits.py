@@ -17,7 +17,7 @@ INT_MIN, INT_MAX = -2 ** 31, 2 ** 31 - 1
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("cap,biased", [(0.0, False), (0.0, True), (6.0, True)])
+@pytest.mark.parametrize("cap,biased", [(0.0, False), (0.0, True), (6.0, True), (6.0, False)])
 def test_every_int_is_a_prefix(d, cap, biased):
     """Below 1: no token; past the sequence: all of them."""
     from paper_2505_11254_amd import binding
